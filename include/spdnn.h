@@ -291,6 +291,92 @@ int spdnn_row_kernel(spdnn_t h, int32_t* kind);
  * takes: 1, or for a general layer whose longest neuron has K > 32 connections ceil(K/32) rounded up to a power of two. */
 int spdnn_layer_passes(spdnn_t h, int32_t l, int32_t* passes);
 
+/* ---- The ends of a mixture of networks -------------------------------------------------------------------------------
+ *
+ * Several networks ("experts") may share one batch of feature rows, each row going through a few of them.  What stands
+ * before and behind spdnn_infer then is again a product of the feature map with a very sparse matrix, one that changes with
+ * the data: rows of a table by token id (one 1 per row), rows sorted by expert (one 1 per copy of a row), outputs added up
+ * with their weights (k numbers per row).  These entry points compute those products, the choice of the experts, and the
+ * gradients of all of them.
+ *
+ * They hold no handle: every array is the caller's, in the memory of the current device.  They check their arguments before
+ * any HIP call, enqueue their kernels on hip_stream (NULL = default stream) and return without waiting; they allocate
+ * nothing, copy nothing to or from the host and may be captured into a HIP graph.  Results do not depend on timing: sums
+ * are formed in a fixed order, without floating-point atomics, in 32 bits whatever the rows' type, and rounded once.
+ *
+ * Rows are row-major with a stride in elements of their own (outputs: stride >= width; inputs: any stride >= 0, so that a
+ * row may stand for many) and any alignment that the element type has.
+ * Outputs must not overlap inputs, unless a comment says so.  Sizes may be 0 where a comment does not say more. */
+enum { SPDNN_F32 = 0, SPDNN_BF16 = 1, SPDNN_F16 = 2 }; /* types of rows */
+enum { SPDNN_I32 = 0, SPDNN_I64 = 1 };                 /* types of token ids */
+enum { SPDNN_SOFTMAX = 0, SPDNN_SIGMOID = 1 };         /* how logits become weights */
+#define SPDNN_MAX_EXPERTS 1024
+#define SPDNN_MAX_CHOSEN 16
+
+/* Rows by token id: out[t][d] = scale * table[ids[t]][d], t < n, d < width.  An id outside [0, vocab) -- padding is
+ * customarily -1 -- gives a row of zeros.  table and out may have different types. */
+int spdnn_embed(const void* table, int32_t table_type, int32_t vocab, int32_t width, int64_t table_stride,
+                const void* ids, int32_t ids_type, int32_t n, float scale, void* out, int32_t out_type,
+                int64_t out_stride, void* hip_stream);
+
+/* The table's gradient: dtable[v][d] = scale * sum of dout[t][d] over the t with ids[t] == v, in ascending order of t up to
+ * the grouping of the sum.  Ids outside [0, vocab) take no part.  accumulate == 0: all vocab rows are written, zeros where
+ * an id does not occur; otherwise the sum is added to what dtable holds (and rounded once), and only rows of ids that
+ * occur are touched.  work: device memory, 256-byte aligned, >= spdnn_embed_grad_bytes(vocab, width, n); contents scratch. */
+int spdnn_embed_grad_bytes(int32_t vocab, int32_t width, int32_t n, size_t* bytes);
+int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, const void* ids, int32_t ids_type, int32_t n,
+                     int32_t vocab, int32_t width, float scale, int32_t accumulate, void* dtable, int32_t dtable_type,
+                     int64_t dtable_stride, void* work, size_t work_bytes, void* hip_stream);
+
+/* The k experts of each row and their weights.
+ *   logits : rows x experts of `type`, 1 <= k <= experts <= SPDNN_MAX_EXPERTS, k <= SPDNN_MAX_CHOSEN.
+ *   bias   : experts floats that are added to the logits for the choice only (for example to even out the experts' loads),
+ *            or NULL.
+ *   keep   : rows bytes, 0 = the row goes to no expert and its logits are not read, or NULL.
+ * An expert is open to a row if logit + bias, added in 32 bits, is greater than minus infinity (a NaN is not).  The row's
+ * experts are the k open ones of the largest such sums, in descending order, the lower index first among equals; slots
+ * beyond the open ones hold expert -1 and weight 0.  Weights, with l the logits without bias:
+ *   SPDNN_SOFTMAX  scale * exp(l) / sum of exp(l), the sum over the open experts, or over the chosen ones if normalise;
+ *   SPDNN_SIGMOID  scale * s(l), s(l) = 1 / (1 + exp(-l)), divided by the sum of s over the chosen ones if normalise.
+ * (A softmax over a logit of plus infinity is NaN.)  chosen: rows x k int32; weight: rows x k floats. */
+int spdnn_route(const void* logits, int32_t type, int64_t stride, int32_t rows, int32_t experts, int32_t k,
+                const float* bias, const uint8_t* keep, int32_t score, int32_t normalise, float scale, int32_t* chosen,
+                float* weight, void* hip_stream);
+
+/* The gradient of weight with respect to logits, the choice held fixed: dweight rows x k floats, chosen as spdnn_route
+ * gives it for these logits (entries outside [0, experts) are slots without an expert; their dweight is not used),
+ * dlogits rows x experts of `type`, all of it written. */
+int spdnn_route_grad(const float* dweight, const void* logits, int32_t type, int64_t stride, const int32_t* chosen,
+                     int32_t rows, int32_t experts, int32_t k, const float* bias, int32_t score, int32_t normalise,
+                     float scale, void* dlogits, int64_t dstride, void* hip_stream);
+
+/* Rows sorted by expert.  A pair (t, j), j < k, has the expert chosen[t * k + j], or none if that is outside [0, experts).
+ *   place   : rows x k int32: position of the pair among all pairs sorted by expert, ties in order of t * k + j; -1 without
+ *             an expert.
+ *   offsets : experts + 1 int32: expert e has the positions offsets[e] .. offsets[e+1]-1; offsets[0] = 0.
+ *   xs      : rows * k rows: xs[place[t][j]] = x[t]; rows from offsets[experts] on are zero.
+ * 1 <= experts <= SPDNN_MAX_EXPERTS, 1 <= k <= SPDNN_MAX_CHOSEN, rows * k <= 2^30.  Every expert's rows are one
+ * contiguous batch, as spdnn_infer takes it.  work: device memory, 256-byte aligned, >= spdnn_dispatch_bytes; contents
+ * scratch. */
+int spdnn_dispatch_bytes(int32_t rows, int32_t k, int32_t experts, size_t* bytes);
+int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t experts, const void* x, int32_t type,
+                   int32_t width, int64_t x_stride, void* xs, int64_t xs_stride, int32_t* offsets, int32_t* place,
+                   void* work, size_t work_bytes, void* hip_stream);
+
+/* Back: out[t] = add[t] + sum over j of weight[t][j] * ys[place[t][j]], slots whose place is outside [0, rows * k) left out
+ * (neither ys nor weight is read for them), j ascending.  add may be NULL (zeros) and may be out itself; weight may be NULL
+ * (ones): with ys the gradient of xs, that is the gradient of x through spdnn_dispatch. */
+int spdnn_combine(const void* ys, int32_t type, int32_t width, int64_t ys_stride, const int32_t* place, const float* weight,
+                  int32_t rows, int32_t k, const void* add, int64_t add_stride, void* out, int64_t out_stride,
+                  void* hip_stream);
+
+/* Gradients of spdnn_combine (that of add is dout): dys[place[t][j]] = weight[t][j] * dout[t], rows from *count on zero;
+ * dweight[t][j] = sum over d of dout[t][d] * ys[place[t][j]][d], 0 for slots without a place.  count: device int32, the
+ * number of places in use, as offsets + experts of spdnn_dispatch points to it. */
+int spdnn_combine_grad(const void* dout, int32_t type, int32_t width, int64_t dout_stride, const void* ys, int64_t ys_stride,
+                       const int32_t* place, const float* weight, const int32_t* count, int32_t rows, int32_t k, void* dys,
+                       int64_t dys_stride, float* dweight, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

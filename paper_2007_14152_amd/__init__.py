@@ -34,13 +34,24 @@ SPDNN_ROWS_NONE = 0
 SPDNN_ROWS_RESIDENT = 1
 SPDNN_ROWS_FEW = 2
 SPDNN_ROWS_STRIDED = 3
+SPDNN_F32 = 0
+SPDNN_BF16 = 1
+SPDNN_F16 = 2
+SPDNN_I32 = 0
+SPDNN_I64 = 1
+SPDNN_SOFTMAX = 0
+SPDNN_SIGMOID = 1
+SPDNN_MAX_EXPERTS = 1024
+SPDNN_MAX_CHOSEN = 16
 
 EXPORTS = ("spdnn_weights_bytes", "spdnn_work_bytes", "spdnn_create", "spdnn_infer", "spdnn_destroy",
            "spdnn_last_error", "spdnn_set_profiling", "spdnn_get_profile", "spdnn_infer_static",
            "spdnn_host_work_bytes", "spdnn_infer_host",
            "spdnn_weights_bytes_for_window", "spdnn_scan_windows", "spdnn_layer_kernel",
            "spdnn_csr_passes", "spdnn_create_csr", "spdnn_layer_passes", "spdnn_ooc_bytes", "spdnn_create_ooc",
-           "spdnn_one_launch", "spdnn_get_launches", "spdnn_row_kernel")
+           "spdnn_one_launch", "spdnn_get_launches", "spdnn_row_kernel",
+           "spdnn_embed", "spdnn_embed_grad_bytes", "spdnn_embed_grad", "spdnn_route", "spdnn_route_grad",
+           "spdnn_dispatch_bytes", "spdnn_dispatch", "spdnn_combine", "spdnn_combine_grad")
 KERNEL_NAMES = {0: "fused_layer_kernel<false>", 1: "fused_layer_kernel<true>", 2: "fused_wide_kernel",
                 3: "fused_pair_kernel", 4: "fused_wide_pair_kernel", 5: "fused_wide_pair4_kernel", 6: "fused_row2_kernel",
                 7: "fused_flat_kernel"}
@@ -88,6 +99,16 @@ def lib():
                                        ctypes.POINTER(i32), ctypes.POINTER(i32)]
         L.spdnn_create_csr.argtypes = [ctypes.POINTER(vp), i32, i32, ctypes.POINTER(vp), ctypes.POINTER(vp),
                                        ctypes.POINTER(vp), vp, vp, sz, vp]
+        i64, f32, psz = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(sz)
+        L.spdnn_embed.argtypes = [vp, i32, i32, i32, i64, vp, i32, i32, f32, vp, i32, i64, vp]
+        L.spdnn_embed_grad_bytes.argtypes = [i32, i32, i32, psz]
+        L.spdnn_embed_grad.argtypes = [vp, i32, i64, vp, i32, i32, i32, i32, f32, i32, vp, i32, i64, vp, sz, vp]
+        L.spdnn_route.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp, i32, i32, f32, vp, vp, vp]
+        L.spdnn_route_grad.argtypes = [vp, vp, i32, i64, vp, i32, i32, i32, vp, i32, i32, f32, vp, i64, vp]
+        L.spdnn_dispatch_bytes.argtypes = [i32, i32, i32, psz]
+        L.spdnn_dispatch.argtypes = [vp, i32, i32, i32, vp, i32, i32, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.spdnn_combine.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, vp, i64, vp, i64, vp]
+        L.spdnn_combine_grad.argtypes = [vp, i32, i32, i64, vp, i64, vp, vp, vp, i32, i32, vp, i64, vp, vp]
         for n in EXPORTS:
             if n != "spdnn_last_error":
                 getattr(L, n).restype = ctypes.c_int
@@ -469,3 +490,15 @@ class Model:
             self.close()
         except Exception:
             pass
+
+
+# The ends of a mixture of networks, on tensors (rows.py; it imports torch).
+ROW_OPERATORS = ("embed", "embed_grad", "route", "route_grad", "dispatch", "dispatch_grad", "combine", "combine_grad")
+
+
+def __getattr__(name):
+    if name in ROW_OPERATORS:
+        from . import rows
+        globals().update({n: getattr(rows, n) for n in ROW_OPERATORS})
+        return globals()[name]
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

@@ -8,16 +8,14 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <cstdarg>
 #include <cstdint>
-#include <cstdio>
 #include <cstring>
 #include <mutex>
 #include <new>
 #include <numeric>
-#include <string>
 #include <vector>
 
+#include "spdnn_error.h"
 #include "spdnn_kernels.h"
 #include "spdnn_cut.h"
 #include "spdnn_profile.h"
@@ -30,27 +28,9 @@ static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
 namespace {
 
-thread_local std::string g_err;
-
-int fail(int code, const char* fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    g_err = buf;
-    return code;
-}
+using spdnn::fail;
 
 int static_scratch(void** out);  // defined below
-
-#define HIP_TRY(expr)                                                                         \
-    do {                                                                                      \
-        hipError_t e_ = (expr);                                                               \
-        if (e_ != hipSuccess)                                                                 \
-            return fail(SPDNN_EHIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_),    \
-                        __FILE__, __LINE__);                                                  \
-    } while (0)
 
 constexpr size_t kAlign = 256;
 inline size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -1747,7 +1727,7 @@ int infer_impl(spdnn_t h, const float* Y0_dev, int32_t batch, const WorkView& wv
 
 extern "C" {
 
-const char* spdnn_last_error(void) { return g_err.c_str(); }
+const char* spdnn_last_error(void) { return spdnn::last_error().c_str(); }
 
 int spdnn_weights_bytes(int32_t N, int32_t L, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");

@@ -1,0 +1,244 @@
+// Host side of the row operators (the second half of include/spdnn.h): argument checks and launches.
+#include "../../include/spdnn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "spdnn_error.h"
+#include "spdnn_rows_kernels.h"
+
+namespace {
+
+using spdnn::fail;
+
+constexpr size_t kAlign = 256;
+constexpr int64_t kMostPairs = 1 << 30;   // rows * k
+constexpr int64_t kMostGroups = 1 << 20;  // workgroups of a launch; more rows take turns
+
+int size_of(int32_t type) { return type == SPDNN_F32 ? 4 : type == SPDNN_BF16 || type == SPDNN_F16 ? 2 : 0; }
+
+// A matrix of rows: not NULL where there is a row, aligned to its elements; rows that are written are apart from each other.
+enum Access { kRead, kWritten };
+int check_rows(const char* what, const void* p, int32_t type, int64_t rows, int32_t width, int64_t stride, Access access) {
+    const int size = size_of(type);
+    if (!size) return fail(SPDNN_EINVAL, "%s: type must be SPDNN_F32, SPDNN_BF16 or SPDNN_F16", what);
+    if (stride < (access == kWritten ? width : 0))
+        return fail(SPDNN_EINVAL, "%s: a stride of %lld elements, width %d", what, (long long)stride, width);
+    if (rows > 0 && stride > INT64_MAX / 8 / rows) return fail(SPDNN_EINVAL, "%s: stride %lld is too large", what, (long long)stride);
+    if (rows > 0 && !p) return fail(SPDNN_EINVAL, "%s is NULL", what);
+    if (reinterpret_cast<uintptr_t>(p) % size) return fail(SPDNN_EINVAL, "%s is not aligned to its elements", what);
+    return SPDNN_OK;
+}
+int check_array(const char* what, const void* p, int64_t n, int size) {
+    if (n > 0 && !p) return fail(SPDNN_EINVAL, "%s is NULL", what);
+    if (reinterpret_cast<uintptr_t>(p) % size) return fail(SPDNN_EINVAL, "%s is not aligned to its elements", what);
+    return SPDNN_OK;
+}
+#define CHECK(expr)                        \
+    do {                                   \
+        const int rc_ = (expr);            \
+        if (rc_ != SPDNN_OK) return rc_;   \
+    } while (0)
+
+int check_pairs(int32_t rows, int32_t k, int32_t experts) {
+    if (rows < 0) return fail(SPDNN_EINVAL, "rows < 0");
+    if (k < 1 || k > SPDNN_MAX_CHOSEN) return fail(SPDNN_EINVAL, "need 1 <= k <= %d", SPDNN_MAX_CHOSEN);
+    if (experts < 1 || experts > SPDNN_MAX_EXPERTS) return fail(SPDNN_EINVAL, "need 1 <= experts <= %d", SPDNN_MAX_EXPERTS);
+    if ((int64_t)rows * k > kMostPairs) return fail(SPDNN_EINVAL, "rows * k exceeds 2^30");
+    return SPDNN_OK;
+}
+int check_route(int32_t rows, int32_t experts, int32_t k, const float* bias, int32_t score) {
+    CHECK(check_pairs(rows, k, experts));
+    if (k > experts) return fail(SPDNN_EINVAL, "k = %d of %d experts", k, experts);
+    if (score != SPDNN_SOFTMAX && score != SPDNN_SIGMOID) return fail(SPDNN_EINVAL, "score must be SPDNN_SOFTMAX or SPDNN_SIGMOID");
+    return check_array("bias", bias, 0, 4);
+}
+int check_work(const void* work, size_t bytes, size_t need) {
+    if (bytes < need) return fail(SPDNN_ESIZE, "work has %zu bytes, %zu needed", bytes, need);
+    if (need && !work) return fail(SPDNN_EINVAL, "work is NULL");
+    if (reinterpret_cast<uintptr_t>(work) % kAlign) return fail(SPDNN_EINVAL, "work must be 256-byte aligned");
+    return SPDNN_OK;
+}
+
+dim3 groups(int64_t n) { return dim3((unsigned)std::max<int64_t>(1, std::min(n, kMostGroups))); }
+
+// f(T{}) with the C++ type of an SPDNN_F32 ...
+template <typename F>
+void with_type(int32_t type, F f) {
+    if (type == SPDNN_F32) f(float{});
+    else if (type == SPDNN_BF16) f(__bf16{});
+    else f(_Float16{});
+}
+template <typename F>
+void with_ids(int32_t type, F f) {
+    if (type == SPDNN_I32) f(int32_t{});
+    else f(int64_t{});
+}
+
+int launched() {
+    HIP_TRY(hipGetLastError());
+    return SPDNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int spdnn_embed(const void* table, int32_t table_type, int32_t vocab, int32_t width, int64_t table_stride, const void* ids,
+                int32_t ids_type, int32_t n, float scale, void* out, int32_t out_type, int64_t out_stride, void* hip_stream) {
+    if (vocab < 1 || width < 1 || n < 0) return fail(SPDNN_EINVAL, "need vocab >= 1, width >= 1, n >= 0");
+    if (ids_type != SPDNN_I32 && ids_type != SPDNN_I64) return fail(SPDNN_EINVAL, "ids_type must be SPDNN_I32 or SPDNN_I64");
+    CHECK(check_rows("table", table, table_type, vocab, width, table_stride, kRead));
+    CHECK(check_rows("out", out, out_type, n, width, out_stride, kWritten));
+    CHECK(check_array("ids", ids, n, ids_type == SPDNN_I32 ? 4 : 8));
+    if (n == 0) return SPDNN_OK;
+    const hipStream_t s = (hipStream_t)hip_stream;
+    with_type(table_type, [&](auto tt) {
+        with_type(out_type, [&](auto to) {
+            with_ids(ids_type, [&](auto ti) {
+                using T = decltype(tt);
+                using S = decltype(to);
+                using I = decltype(ti);
+                spdnn::embed_kernel<T, S, I><<<groups(n), spdnn::kRowThreads, 0, s>>>((const T*)table, table_stride, (uint32_t)vocab, width, (const I*)ids, n, scale, (S*)out, out_stride);
+            });
+        });
+    });
+    return launched();
+}
+
+int spdnn_embed_grad_bytes(int32_t vocab, int32_t width, int32_t n, size_t* bytes) {
+    if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
+    if (vocab < 1 || width < 1 || n < 0) return fail(SPDNN_EINVAL, "need vocab >= 1, width >= 1, n >= 0");
+    *bytes = 0;
+    return SPDNN_OK;
+}
+
+int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, const void* ids, int32_t ids_type, int32_t n,
+                     int32_t vocab, int32_t width, float scale, int32_t accumulate, void* dtable, int32_t dtable_type,
+                     int64_t dtable_stride, void* work, size_t work_bytes, void* hip_stream) {
+    size_t need = 0;
+    CHECK(spdnn_embed_grad_bytes(vocab, width, n, &need));
+    if (ids_type != SPDNN_I32 && ids_type != SPDNN_I64) return fail(SPDNN_EINVAL, "ids_type must be SPDNN_I32 or SPDNN_I64");
+    CHECK(check_rows("dout", dout, dout_type, n, width, dout_stride, kRead));
+    CHECK(check_rows("dtable", dtable, dtable_type, vocab, width, dtable_stride, kWritten));
+    CHECK(check_array("ids", ids, n, ids_type == SPDNN_I32 ? 4 : 8));
+    CHECK(check_work(work, work_bytes, need));
+    const hipStream_t s = (hipStream_t)hip_stream;
+    with_type(dout_type, [&](auto tt) {
+        with_type(dtable_type, [&](auto to) {
+            with_ids(ids_type, [&](auto ti) {
+                using T = decltype(tt);
+                using S = decltype(to);
+                using I = decltype(ti);
+                spdnn::embed_grad_kernel<T, S, I><<<groups(vocab), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, scale, accumulate, (S*)dtable, dtable_stride);
+            });
+        });
+    });
+    return launched();
+}
+
+int spdnn_route(const void* logits, int32_t type, int64_t stride, int32_t rows, int32_t experts, int32_t k, const float* bias,
+                const uint8_t* keep, int32_t score, int32_t normalise, float scale, int32_t* chosen, float* weight,
+                void* hip_stream) {
+    CHECK(check_route(rows, experts, k, bias, score));
+    CHECK(check_rows("logits", logits, type, rows, experts, stride, kRead));
+    CHECK(check_array("chosen", chosen, rows, 4));
+    CHECK(check_array("weight", weight, rows, 4));
+    if (rows == 0) return SPDNN_OK;
+    with_type(type, [&](auto tt) {
+        using T = decltype(tt);
+        spdnn::route_kernel<T><<<groups(rows), 64, 0, (hipStream_t)hip_stream>>>((const T*)logits, stride, rows, experts, k, bias, keep, score, normalise, scale, chosen, weight);
+    });
+    return launched();
+}
+
+int spdnn_route_grad(const float* dweight, const void* logits, int32_t type, int64_t stride, const int32_t* chosen, int32_t rows,
+                     int32_t experts, int32_t k, const float* bias, int32_t score, int32_t normalise, float scale, void* dlogits,
+                     int64_t dstride, void* hip_stream) {
+    CHECK(check_route(rows, experts, k, bias, score));
+    CHECK(check_rows("logits", logits, type, rows, experts, stride, kRead));
+    CHECK(check_rows("dlogits", dlogits, type, rows, experts, dstride, kWritten));
+    CHECK(check_array("chosen", chosen, rows, 4));
+    CHECK(check_array("dweight", dweight, rows, 4));
+    if (rows == 0) return SPDNN_OK;
+    with_type(type, [&](auto tt) {
+        using T = decltype(tt);
+        spdnn::route_grad_kernel<T><<<groups(rows), 64, 0, (hipStream_t)hip_stream>>>(dweight, (const T*)logits, stride, chosen, rows, experts, k, bias, score, normalise, scale, (T*)dlogits, dstride);
+    });
+    return launched();
+}
+
+int spdnn_dispatch_bytes(int32_t rows, int32_t k, int32_t experts, size_t* bytes) {
+    if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
+    CHECK(check_pairs(rows, k, experts));
+    *bytes = sizeof(int32_t) * SPDNN_MAX_EXPERTS;
+    return SPDNN_OK;
+}
+
+int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t experts, const void* x, int32_t type, int32_t width,
+                   int64_t x_stride, void* xs, int64_t xs_stride, int32_t* offsets, int32_t* place, void* work,
+                   size_t work_bytes, void* hip_stream) {
+    size_t need = 0;
+    CHECK(spdnn_dispatch_bytes(rows, k, experts, &need));
+    if (width < 1) return fail(SPDNN_EINVAL, "need width >= 1");
+    const int n = rows * k;
+    CHECK(check_rows("x", x, type, rows, width, x_stride, kRead));
+    CHECK(check_rows("xs", xs, type, n, width, xs_stride, kWritten));
+    CHECK(check_array("chosen", chosen, rows, 4));
+    CHECK(check_array("place", place, rows, 4));
+    CHECK(check_array("offsets", offsets, 1, 4));
+    CHECK(check_work(work, work_bytes, need));
+    const hipStream_t s = (hipStream_t)hip_stream;
+    int32_t* counts = (int32_t*)work;
+    spdnn::expert_count_kernel<<<experts, spdnn::kRowThreads, 0, s>>>(chosen, n, counts);
+    spdnn::expert_place_kernel<<<experts + 1, 64, 0, s>>>(chosen, n, experts, counts, offsets, place);
+    if (n > 0)
+        with_type(type, [&](auto tt) {
+            using T = decltype(tt);
+            spdnn::dispatch_rows_kernel<T><<<groups(n), spdnn::kRowThreads, 0, s>>>((const T*)x, x_stride, rows, k, width, place, offsets + experts, (T*)xs, xs_stride);
+        });
+    return launched();
+}
+
+int spdnn_combine(const void* ys, int32_t type, int32_t width, int64_t ys_stride, const int32_t* place, const float* weight,
+                  int32_t rows, int32_t k, const void* add, int64_t add_stride, void* out, int64_t out_stride, void* hip_stream) {
+    CHECK(check_pairs(rows, k, 1));
+    if (width < 1) return fail(SPDNN_EINVAL, "need width >= 1");
+    const int n = rows * k;
+    CHECK(check_rows("ys", ys, type, n, width, ys_stride, kRead));
+    CHECK(check_rows("out", out, type, rows, width, out_stride, kWritten));
+    if (add) CHECK(check_rows("add", add, type, rows, width, add_stride, kRead));
+    CHECK(check_array("place", place, rows, 4));
+    CHECK(check_array("weight", weight, 0, 4));
+    if (rows == 0) return SPDNN_OK;
+    with_type(type, [&](auto tt) {
+        using T = decltype(tt);
+        spdnn::combine_kernel<T><<<groups(rows), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>((const T*)ys, ys_stride, place, weight, rows, k, width, (const T*)add, add_stride, (T*)out, out_stride);
+    });
+    return launched();
+}
+
+int spdnn_combine_grad(const void* dout, int32_t type, int32_t width, int64_t dout_stride, const void* ys, int64_t ys_stride,
+                       const int32_t* place, const float* weight, const int32_t* count, int32_t rows, int32_t k, void* dys,
+                       int64_t dys_stride, float* dweight, void* hip_stream) {
+    CHECK(check_pairs(rows, k, 1));
+    if (width < 1) return fail(SPDNN_EINVAL, "need width >= 1");
+    const int n = rows * k;
+    CHECK(check_rows("dout", dout, type, rows, width, dout_stride, kRead));
+    CHECK(check_rows("ys", ys, type, n, width, ys_stride, kRead));
+    CHECK(check_rows("dys", dys, type, n, width, dys_stride, kWritten));
+    CHECK(check_array("place", place, rows, 4));
+    CHECK(check_array("weight", weight, rows, 4));
+    CHECK(check_array("count", count, rows, 4));
+    CHECK(check_array("dweight", dweight, rows, 4));
+    if (rows == 0) return SPDNN_OK;
+    with_type(type, [&](auto tt) {
+        using T = decltype(tt);
+        spdnn::combine_grad_kernel<T><<<groups(n), 64, 0, (hipStream_t)hip_stream>>>((const T*)dout, dout_stride, (const T*)ys, ys_stride, place, weight, count, rows, k, width, (T*)dys, dys_stride, dweight);
+    });
+    return launched();
+}
+
+}  // extern "C"

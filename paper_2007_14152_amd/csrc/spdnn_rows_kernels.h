@@ -1,0 +1,293 @@
+// Kernels of the row operators (spdnn_embed ... spdnn_combine_grad of include/spdnn.h): rows by token id, the choice of
+// experts, rows sorted by expert and back, and the gradients.  T, S: types of rows (float, __bf16, _Float16).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+// Products and sums are rounded to 32 bits where they are written; fused ones are spelled fmaf.
+#pragma clang fp contract(off)
+
+namespace spdnn {
+
+constexpr int kRowThreads = 256;
+
+// A number of 32 bits rounded to the rows' type.  The empty asm keeps the compiler from making one v_fma_mixlo_f16 of the
+// operation that gave x and the conversion: that rounds once where every other type rounds twice.
+template <typename S>
+__device__ inline S rounded(float x) {
+    if constexpr (sizeof(S) == 2) asm("" : "+v"(x));
+    return (S)x;
+}
+
+// out[t] = scale * table[ids[t]]; a workgroup per row.
+template <typename T, typename S, typename I>
+__global__ __launch_bounds__(kRowThreads) void embed_kernel(const T* __restrict__ table, int64_t table_stride, uint32_t vocab, int width,
+                                                            const I* __restrict__ ids, int n, float scale, S* __restrict__ out, int64_t out_stride) {
+    for (int64_t t = blockIdx.x; t < n; t += gridDim.x) {
+        const I id = ids[t];
+        const bool in = id >= 0 && id < (I)vocab;
+        for (int d = threadIdx.x; d < width; d += kRowThreads)
+            out[t * out_stride + d] = rounded<S>(in ? scale * (float)table[(int64_t)id * table_stride + d] : 0.0f);
+    }
+}
+
+// dtable[v] = [dtable[v] +] scale * sum of the dout[t] with ids[t] == v; a workgroup per v looks through all ids.
+template <typename T, typename S, typename I>
+__global__ __launch_bounds__(kRowThreads) void embed_grad_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
+                                                                 int vocab, int width, float scale, int accumulate, S* __restrict__ dtable,
+                                                                 int64_t dtable_stride) {
+    for (int64_t v = blockIdx.x; v < vocab; v += gridDim.x) {
+        for (int d0 = 0; d0 < width; d0 += kRowThreads) {
+            const int d = d0 + threadIdx.x;
+            float sum = 0.0f;
+            bool any = false;
+            for (int t = 0; t < n; ++t) {
+                if (ids[t] != (I)v) continue;
+                any = true;
+                if (d < width) sum += (float)dout[t * dout_stride + d];
+            }
+            if (d >= width || (accumulate && !any)) continue;
+            S& to = dtable[v * dtable_stride + d];
+            to = rounded<S>(accumulate ? fmaf(scale, sum, (float)to) : scale * sum);
+        }
+    }
+}
+
+// --- choice of experts ------------------------------------------------------
+
+// A number whose order as an integer is the order of r, -0 beside +0; 0 for what is not greater than minus infinity.
+__device__ inline uint32_t rank_of(float r) {
+    if (!(r > -INFINITY)) return 0;
+    const uint32_t b = __float_as_uint(r + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+__device__ inline float wave_sum(float x) {
+    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
+    return x;
+}
+__device__ inline float wave_max(float x) {
+    for (int m = 32; m; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
+    return x;
+}
+
+__device__ inline float log_sigmoid(float x) { return fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); }
+
+__device__ inline float sigmoid(float x) {  // no overflow on the way: small values stay apart from zero
+    const float e = expf(-fabsf(x)), r = 1.0f / (1.0f + e);
+    return x >= 0.0f ? r : e * r;
+}
+
+// Weights of the chosen experts before the scale: lane j < k has the logit of slot j, valid says whether the slot has an expert.
+// Softmax over the open experts: top and total are the largest of their logits and the sum of exp(logit - top).
+__device__ inline float slot_weight(float l, bool valid, int score, int normalise, float top, float total) {
+    if (normalise) {
+        const float x = score == SPDNN_SIGMOID ? log_sigmoid(l) : l;
+        const float m = wave_max(valid ? x : -INFINITY);
+        const float e = valid ? expf(x - m) : 0.0f;
+        const float sum = wave_sum(e);
+        return valid ? e / sum : 0.0f;
+    }
+    if (!valid) return 0.0f;
+    return score == SPDNN_SIGMOID ? sigmoid(l) : expf(l - top) / total;
+}
+
+constexpr int kLaneExperts = SPDNN_MAX_EXPERTS / 64;
+
+// A wave per row; the lanes hold the row's logits, k rounds take the largest that is left.
+template <typename T>
+__global__ __launch_bounds__(64) void route_kernel(const T* __restrict__ logits, int64_t stride, int rows, int experts, int k,
+                                                   const float* __restrict__ bias, const uint8_t* __restrict__ keep, int score, int normalise,
+                                                   float scale, int32_t* __restrict__ chosen, float* __restrict__ weight) {
+    const int lane = threadIdx.x;
+    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x) {
+        uint32_t rank[kLaneExperts];
+        float top = -INFINITY, total = 0.0f;
+        const bool kept = !keep || keep[t];
+        for (int i = 0; i < kLaneExperts; ++i) {
+            const int e = i * 64 + lane;
+            rank[i] = 0;
+            if (!kept || e >= experts) continue;
+            const float l = (float)logits[t * stride + e];
+            rank[i] = rank_of(bias ? l + bias[e] : l);
+            if (rank[i]) top = fmaxf(top, l);
+        }
+        if (score == SPDNN_SOFTMAX && !normalise) {
+            top = wave_max(top);
+            for (int i = 0; i < kLaneExperts; ++i)
+                if (rank[i]) total += expf((float)logits[t * stride + i * 64 + lane] - top);
+            total = wave_sum(total);
+        }
+        int mine = -1;  // lane j: the expert of slot j
+        for (int j = 0; j < k; ++j) {
+            uint64_t best = 0;
+            for (int i = 0; i < kLaneExperts; ++i) {
+                const uint64_t c = (uint64_t)rank[i] << 32 | (uint32_t)~(i * 64 + lane);
+                if (rank[i] && c > best) best = c;
+            }
+            for (int m = 32; m; m >>= 1) {
+                const uint64_t o = __shfl_xor((unsigned long long)best, m);
+                best = o > best ? o : best;
+            }
+            if (!best) break;
+            const int e = (int)~(uint32_t)best;
+            if (lane == j) mine = e;
+            for (int i = 0; i < kLaneExperts; ++i)
+                if (i * 64 + lane == e) rank[i] = 0;
+        }
+        const float l = mine >= 0 ? (float)logits[t * stride + mine] : 0.0f;
+        const float w = slot_weight(l, mine >= 0, score, normalise, top, total);
+        if (lane < k) {
+            chosen[t * k + lane] = mine;
+            weight[t * k + lane] = scale * w;
+        }
+    }
+}
+
+// A wave per row.
+template <typename T>
+__global__ __launch_bounds__(64) void route_grad_kernel(const float* __restrict__ dweight, const T* __restrict__ logits, int64_t stride,
+                                                        const int32_t* __restrict__ chosen, int rows, int experts, int k,
+                                                        const float* __restrict__ bias, int score, int normalise, float scale,
+                                                        T* __restrict__ dlogits, int64_t dstride) {
+    const int lane = threadIdx.x;
+    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x) {
+        int mine = lane < k ? chosen[t * k + lane] : -1;
+        const bool valid = mine >= 0 && mine < experts;
+        const float l = valid ? (float)logits[t * stride + mine] : 0.0f;
+        const float g = valid ? scale * dweight[t * k + lane] : 0.0f;
+        const bool dense = score == SPDNN_SOFTMAX && !normalise;
+        const bool any = __ballot(valid) != 0;
+        float top = -INFINITY, total = 0.0f;
+        if (dense && any) {
+            for (int e = lane; e < experts; e += 64) {
+                const float x = (float)logits[t * stride + e];
+                if ((bias ? x + bias[e] : x) > -INFINITY) top = fmaxf(top, x);
+            }
+            top = wave_max(top);
+            for (int e = lane; e < experts; e += 64) {
+                const float x = (float)logits[t * stride + e];
+                if ((bias ? x + bias[e] : x) > -INFINITY) total += expf(x - top);
+            }
+            total = wave_sum(total);
+        }
+        const float w = slot_weight(l, valid, score, normalise, top, total);
+        const float mean = wave_sum(g * w);
+        float d = 0.0f;  // of the slot's logit, but for the dense form's part that every logit has
+        if (valid) {
+            if (dense) d = g;
+            else if (normalise) d = w * (g - mean) * (score == SPDNN_SIGMOID ? sigmoid(-l) : 1.0f);
+            else d = g * w * sigmoid(-l);
+        }
+        for (int e0 = 0; e0 < experts; e0 += 64) {
+            const int e = e0 + lane;
+            float at = 0.0f;
+            for (int j = 0; j < k; ++j) {
+                const int to = __shfl(valid ? mine : -1, j);
+                const float dj = __shfl(d, j);
+                if (to == e) at = dj;
+            }
+            if (e >= experts) continue;
+            if (dense) {
+                const float x = (float)logits[t * stride + e];
+                const bool open = any && (bias ? x + bias[e] : x) > -INFINITY;
+                at = open ? expf(x - top) / total * (at - mean) : 0.0f;
+            }
+            dlogits[t * dstride + e] = rounded<T>(at);
+        }
+    }
+}
+
+// --- rows by expert ---------------------------------------------------------
+
+// counts[e] = pairs with expert e; a workgroup per expert.
+__global__ __launch_bounds__(kRowThreads) void expert_count_kernel(const int32_t* __restrict__ chosen, int n, int32_t* __restrict__ counts) {
+    __shared__ int32_t total;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    int mine = 0;
+    for (int p = threadIdx.x; p < n; p += kRowThreads) mine += chosen[p] == (int)blockIdx.x;
+    atomicAdd(&total, mine);
+    __syncthreads();
+    if (threadIdx.x == 0) counts[blockIdx.x] = total;
+}
+
+// offsets from counts, places of expert blockIdx.x's pairs; workgroup `experts` does the pairs without an expert.
+__global__ __launch_bounds__(64) void expert_place_kernel(const int32_t* __restrict__ chosen, int n, int experts, const int32_t* __restrict__ counts,
+                                                          int32_t* __restrict__ offsets, int32_t* __restrict__ place) {
+    const int lane = threadIdx.x, me = blockIdx.x;
+    int before = 0;
+    for (int e = 0; e < me; ++e) before += counts[e];
+    if (lane == 0) offsets[me] = before;
+    for (int p0 = 0; p0 < n; p0 += 64) {
+        const int p = p0 + lane;
+        const int e = p < n ? chosen[p] : experts;
+        if (me == experts) {
+            if (p < n && (e < 0 || e >= experts)) place[p] = -1;
+            continue;
+        }
+        const uint64_t same = __ballot(e == me);
+        if (e == me) place[p] = before + __popcll(same & ((1ull << lane) - 1));
+        before += __popcll(same);
+    }
+}
+
+// xs[place[t][j]] = x[t] (of: pair -> row of x), zeros behind the rows in use.
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(const T* __restrict__ x, int64_t x_stride, int rows, int k, int width,
+                                                                    const int32_t* __restrict__ place, const int32_t* __restrict__ count,
+                                                                    T* __restrict__ xs, int64_t xs_stride) {
+    const int64_t n = (int64_t)rows * k;
+    for (int64_t p = blockIdx.x; p < n; p += gridDim.x) {
+        const int at = place[p];
+        if (at >= 0)
+            for (int d = threadIdx.x; d < width; d += kRowThreads) xs[at * xs_stride + d] = x[p / k * x_stride + d];
+        if (p >= *count)
+            for (int d = threadIdx.x; d < width; d += kRowThreads) xs[p * xs_stride + d] = (T)0.0f;
+    }
+}
+
+// out[t] = add[t] + sum of weight[t][j] * ys[place[t][j]]; a workgroup per row.
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void combine_kernel(const T* __restrict__ ys, int64_t ys_stride, const int32_t* __restrict__ place,
+                                                              const float* __restrict__ weight, int rows, int k, int width, const T* add,
+                                                              int64_t add_stride, T* out, int64_t out_stride) {
+    const int64_t n = (int64_t)rows * k;
+    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x)
+        for (int d = threadIdx.x; d < width; d += kRowThreads) {
+            float sum = 0.0f;
+            for (int j = 0; j < k; ++j) {
+                const int at = place[t * k + j];
+                if (at < 0 || at >= n) continue;
+                const float y = (float)ys[at * ys_stride + d];
+                sum = weight ? fmaf(weight[t * k + j], y, sum) : sum + y;
+            }
+            out[t * out_stride + d] = rounded<T>(add ? sum + (float)add[t * add_stride + d] : sum);
+        }
+}
+
+// dys[place[t][j]] = weight[t][j] * dout[t], dweight[t][j] = <dout[t], ys[place[t][j]]>; a wave per pair.
+template <typename T>
+__global__ __launch_bounds__(64) void combine_grad_kernel(const T* __restrict__ dout, int64_t dout_stride, const T* __restrict__ ys, int64_t ys_stride,
+                                                          const int32_t* __restrict__ place, const float* __restrict__ weight,
+                                                          const int32_t* __restrict__ count, int rows, int k, int width, T* __restrict__ dys,
+                                                          int64_t dys_stride, float* __restrict__ dweight) {
+    const int64_t n = (int64_t)rows * k;
+    for (int64_t p = blockIdx.x; p < n; p += gridDim.x) {
+        const int at = place[p];
+        float dot = 0.0f;
+        if (at >= 0 && at < n)
+            for (int d = threadIdx.x; d < width; d += 64) {
+                const float g = (float)dout[p / k * dout_stride + d];
+                dys[at * dys_stride + d] = rounded<T>(weight[p] * g);
+                dot = fmaf(g, (float)ys[at * ys_stride + d], dot);
+            }
+        dot = wave_sum(dot);
+        if (threadIdx.x == 0) dweight[p] = dot;
+        if (p >= *count)
+            for (int d = threadIdx.x; d < width; d += 64) dys[p * dys_stride + d] = (T)0.0f;
+    }
+}
+
+}  // namespace spdnn
