@@ -306,7 +306,7 @@ int spdnn_layer_passes(spdnn_t h, int32_t l, int32_t* passes);
  *
  * Rows are row-major with a stride in elements of their own (outputs: stride >= width; inputs: any stride >= 0, so that a
  * row may stand for many) and any alignment that the element type has.
- * Outputs must not overlap inputs, unless a comment says so.  Sizes may be 0 where a comment does not say more. */
+ * Outputs must not overlap inputs.  Sizes may be 0 where a comment does not say more. */
 enum { SPDNN_F32 = 0, SPDNN_BF16 = 1, SPDNN_F16 = 2 }; /* types of rows */
 enum { SPDNN_I32 = 0, SPDNN_I64 = 1 };                 /* types of token ids */
 enum { SPDNN_SOFTMAX = 0, SPDNN_SIGMOID = 1 };         /* how logits become weights */
@@ -364,8 +364,7 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
                    void* work, size_t work_bytes, void* hip_stream);
 
 /* Back: out[t] = add[t] + sum over j of weight[t][j] * ys[place[t][j]], slots whose place is outside [0, rows * k) left out
- * (neither ys nor weight is read for them), j ascending.  add may be NULL (zeros) and may be out itself; weight may be NULL
- * (ones): with ys the gradient of xs, that is the gradient of x through spdnn_dispatch. */
+ * (neither ys nor weight is read for them), j ascending.  add may be NULL (zeros); weight may be NULL (ones): with ys the gradient of xs, that is the gradient of x through spdnn_dispatch. */
 int spdnn_combine(const void* ys, int32_t type, int32_t width, int64_t ys_stride, const int32_t* place, const float* weight,
                   int32_t rows, int32_t k, const void* add, int64_t add_stride, void* out, int64_t out_stride,
                   void* hip_stream);

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "spdnn_error.h"
 #include "spdnn_rows_kernels.h"
@@ -64,6 +65,33 @@ int check_work(const void* work, size_t bytes, size_t need) {
 
 dim3 groups(int64_t n) { return dim3((unsigned)std::max<int64_t>(1, std::min(n, kMostGroups))); }
 
+// Tiles of rows x width elements in vectors of v: as many rows to a tile as fill its workgroup's turns best, but not so many
+// that less than two workgroups per CU are left.
+spdnn::Tiles tiles(int64_t rows, int32_t width, int v) {
+    spdnn::Tiles g;
+    g.rows = rows;
+    g.width = width;
+    g.vecs = (width - 1) / v + 1;
+    g.slab = std::min(g.vecs, spdnn::kTileVecs);
+    g.per = 1;
+    double best = 0;
+    constexpr int64_t turn = spdnn::kUnroll * spdnn::kRowThreads;
+    for (int64_t per = 1; per * g.slab <= spdnn::kTileVecs && (per == 1 || rows / per >= 512); ++per) {
+        const int64_t turns = (per * g.slab + turn - 1) / turn;
+        const double full = (double)(per * g.slab) / (double)(turns * turn);
+        if (full > best + 0.02) {
+            best = full;
+            g.per = (int32_t)per;
+        }
+    }
+    g.magic = (uint32_t)(((1ull << 32) + g.slab - 1) / g.slab);
+    return g;
+}
+dim3 groups(const spdnn::Tiles& g) {
+    const int64_t x = std::min((g.rows + g.per - 1) / g.per, kMostGroups);
+    return dim3((unsigned)x, (unsigned)std::min((g.vecs + g.slab - 1) / g.slab, 1024));
+}
+
 // f(T{}) with the C++ type of an SPDNN_F32 ...
 template <typename F>
 void with_type(int32_t type, F f) {
@@ -75,6 +103,13 @@ template <typename F>
 void with_ids(int32_t type, F f) {
     if (type == SPDNN_I32) f(int32_t{});
     else f(int64_t{});
+}
+
+// f(V) with the elements of a vector: V, or 1 where a row has less.
+template <int V, typename F>
+void with_vec(int32_t width, F f) {
+    if (width >= V) f(std::integral_constant<int, V>{});
+    else f(std::integral_constant<int, 1>{});
 }
 
 int launched() {
@@ -101,7 +136,11 @@ int spdnn_embed(const void* table, int32_t table_type, int32_t vocab, int32_t wi
                 using T = decltype(tt);
                 using S = decltype(to);
                 using I = decltype(ti);
-                spdnn::embed_kernel<T, S, I><<<groups(n), spdnn::kRowThreads, 0, s>>>((const T*)table, table_stride, (uint32_t)vocab, width, (const I*)ids, n, scale, (S*)out, out_stride);
+                with_vec<16 / std::max(sizeof(T), sizeof(S))>(width, [&](auto v) {
+                    constexpr int V = decltype(v)::value;
+                    const spdnn::Tiles g = tiles(n, width, V);
+                    spdnn::embed_kernel<T, S, I, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)table, table_stride, (uint32_t)vocab, (const I*)ids, scale, (S*)out, out_stride);
+                });
             });
         });
     });

@@ -20,16 +20,91 @@ __device__ inline S rounded(float x) {
     return (S)x;
 }
 
-// out[t] = scale * table[ids[t]]; a workgroup per row.
-template <typename T, typename S, typename I>
-__global__ __launch_bounds__(kRowThreads) void embed_kernel(const T* __restrict__ table, int64_t table_stride, uint32_t vocab, int width,
-                                                            const I* __restrict__ ids, int n, float scale, S* __restrict__ out, int64_t out_stride) {
-    for (int64_t t = blockIdx.x; t < n; t += gridDim.x) {
-        const I id = ids[t];
-        const bool in = id >= 0 && id < (I)vocab;
-        for (int d = threadIdx.x; d < width; d += kRowThreads)
-            out[t * out_stride + d] = rounded<S>(in ? scale * (float)table[(int64_t)id * table_stride + d] : 0.0f);
-    }
+// --- tiles of rows ----------------------------------------------------------
+//
+// Kernels that only move rows take them as vectors of V elements, 16 bytes of the wider type, or of one element where a row
+// has less than V.  The last vector of a row ends with the row, so that none is short: where V does not divide the width it
+// covers elements of the one before it again.  A workgroup's tile is `per` whole rows next to each other, so that rows of any
+// length keep all lanes busy (vectors are numbered through the tile), or `slab` vectors of one row where rows are long; lanes
+// beyond its end take its last vector once more.  What is covered twice is computed and stored twice, alike: there is no
+// branch around a load or a store, and none waits for another.
+struct Tiles {
+    int64_t rows;
+    int32_t width;
+    int32_t vecs;    // vectors of a row
+    int32_t per;     // rows of a tile
+    int32_t slab;    // vectors of a row in a tile
+    uint32_t magic;  // ceil(2^32 / slab): quotients by slab > 1 for what is less than 2^16
+};
+constexpr int kTileVecs = 4096;  // at most, of a tile
+constexpr int kUnroll = 4;       // vectors that a lane has under way
+
+// Rows may start at any element: vectors are only aligned like one (global memory takes such loads and stores whole).
+template <typename T, int V>
+using Pack __attribute__((ext_vector_type(V), aligned(sizeof(T)))) = T;
+
+template <int V, typename T>
+__device__ inline Pack<T, V> load_vec(const T* p) {
+    if constexpr (V == 1) return Pack<T, V>(*p);
+    else return *reinterpret_cast<const Pack<T, V>*>(p);
+}
+template <int V, typename T>
+__device__ inline void store_vec(T* p, const float (&from)[V]) {
+    Pack<T, V> x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = rounded<T>(from[i]);
+    *reinterpret_cast<Pack<T, V>*>(p) = x;
+}
+
+// f(places of kUnroll vectors of the tile) until the tile is done; f has the loads of all of them to overlap.
+struct At {
+    int64_t row;
+    int32_t col;
+};
+template <int V, typename F>
+__device__ inline void each_vec(const Tiles& g, F f) {
+    for (int64_t r0 = (int64_t)blockIdx.x * g.per; r0 < g.rows; r0 += (int64_t)gridDim.x * g.per)
+        for (int vec0 = blockIdx.y * g.slab; vec0 < g.vecs; vec0 += gridDim.y * g.slab) {
+            const int rows = (int)min((int64_t)g.per, g.rows - r0);
+            const int items = rows * g.slab;
+            for (int i0 = threadIdx.x; i0 < items; i0 += kUnroll * kRowThreads) {
+                At at[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    const uint32_t i = min(i0 + u * kRowThreads, items - 1);
+                    const uint32_t r = g.per == 1 ? 0 : g.slab == 1 ? i : __umulhi(i, g.magic);
+                    const int vec = min(vec0 + (int)(i - r * g.slab), g.vecs - 1);
+                    at[u].row = r0 + r;
+                    at[u].col = min(vec * V, g.width - V);
+                }
+                f(at);
+            }
+        }
+}
+
+// out[t] = scale * table[ids[t]].
+template <typename T, typename S, typename I, int V>
+__global__ __launch_bounds__(kRowThreads) void embed_kernel(Tiles g, const T* __restrict__ table, int64_t table_stride, uint32_t vocab,
+                                                            const I* __restrict__ ids, float scale, S* __restrict__ out, int64_t out_stride) {
+    each_vec<V>(g, [&](const At (&at)[kUnroll]) {
+        I id[kUnroll];
+        Pack<T, V> x[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) id[u] = ids[at[u].row];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const bool in = id[u] >= 0 && id[u] < (I)vocab;
+            x[u] = load_vec<V>(table + (in ? (int64_t)id[u] : 0) * table_stride + at[u].col);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const bool in = id[u] >= 0 && id[u] < (I)vocab;
+            float y[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = in ? scale * (float)x[u][i] : 0.0f;
+            store_vec<V>(out + at[u].row * out_stride + at[u].col, y);
+        }
+    });
 }
 
 // dtable[v] = [dtable[v] +] scale * sum of the dout[t] with ids[t] == v; a workgroup per v looks through all ids.
