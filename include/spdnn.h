@@ -364,7 +364,8 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
                    void* work, size_t work_bytes, void* hip_stream);
 
 /* Back: out[t] = add[t] + sum over j of weight[t][j] * ys[place[t][j]], slots whose place is outside [0, rows * k) left out
- * (neither ys nor weight is read for them), j ascending.  add may be NULL (zeros); weight may be NULL (ones): with ys the gradient of xs, that is the gradient of x through spdnn_dispatch. */
+ * (what ys and weight hold for them does not matter), j ascending.  add may be NULL (zeros); weight may be NULL (ones): with
+ * ys the gradient of xs, that is the gradient of x through spdnn_dispatch. */
 int spdnn_combine(const void* ys, int32_t type, int32_t width, int64_t ys_stride, const int32_t* place, const float* weight,
                   int32_t rows, int32_t k, const void* add, int64_t add_stride, void* out, int64_t out_stride,
                   void* hip_stream);

@@ -65,17 +65,23 @@ int check_work(const void* work, size_t bytes, size_t need) {
 
 dim3 groups(int64_t n) { return dim3((unsigned)std::max<int64_t>(1, std::min(n, kMostGroups))); }
 
-// Tiles of rows x width elements in vectors of v: as many rows to a tile as fill its workgroup's turns best, but not so many
+// Outputs of this many bytes go past the caches, for whoever reads them next does not find them there (256 MB at the most) anyway.
+// Rows of 4096 bf16 by id, alone and with a kernel behind that reads them, through -> past: 400 MB 128 -> 117 and 266 -> 256 us,
+// 200 MB 70 -> 62 and 141 -> 137, 128 MB 42 -> 41 and 83 -> 87, 16 MB 10.4 -> 11.8 and 15.9 -> 17.5.
+constexpr int64_t kPastBytes = 160 << 20;
+
+// Tiles of rows x width elements in vectors of v, out_bytes of output in all: as many rows to a tile as fill its workgroup's turns best, but not so many
 // that less than two workgroups per CU are left.
-spdnn::Tiles tiles(int64_t rows, int32_t width, int v) {
+spdnn::Tiles tiles(int64_t rows, int32_t width, int v, int unroll, int64_t out_bytes) {
     spdnn::Tiles g;
     g.rows = rows;
     g.width = width;
     g.vecs = (width - 1) / v + 1;
     g.slab = std::min(g.vecs, spdnn::kTileVecs);
+    g.past = out_bytes >= kPastBytes;
     g.per = 1;
     double best = 0;
-    constexpr int64_t turn = spdnn::kUnroll * spdnn::kRowThreads;
+    const int64_t turn = unroll * spdnn::kRowThreads;
     for (int64_t per = 1; per * g.slab <= spdnn::kTileVecs && (per == 1 || rows / per >= 512); ++per) {
         const int64_t turns = (per * g.slab + turn - 1) / turn;
         const double full = (double)(per * g.slab) / (double)(turns * turn);
@@ -112,6 +118,14 @@ void with_vec(int32_t width, F f) {
     else f(std::integral_constant<int, 1>{});
 }
 
+// f(J) with the slots of a row that are taken at a time.
+template <typename F>
+void with_places(int32_t k, F f) {
+    if (k == 1) f(std::integral_constant<int, 1>{});
+    else if (k == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 4>{});
+}
+
 int launched() {
     HIP_TRY(hipGetLastError());
     return SPDNN_OK;
@@ -138,7 +152,7 @@ int spdnn_embed(const void* table, int32_t table_type, int32_t vocab, int32_t wi
                 using I = decltype(ti);
                 with_vec<16 / std::max(sizeof(T), sizeof(S))>(width, [&](auto v) {
                     constexpr int V = decltype(v)::value;
-                    const spdnn::Tiles g = tiles(n, width, V);
+                    const spdnn::Tiles g = tiles(n, width, V, spdnn::kEmbedVecs, (int64_t)n * width * sizeof(S));
                     spdnn::embed_kernel<T, S, I, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)table, table_stride, (uint32_t)vocab, (const I*)ids, scale, (S*)out, out_stride);
                 });
             });
@@ -236,7 +250,11 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
     if (n > 0)
         with_type(type, [&](auto tt) {
             using T = decltype(tt);
-            spdnn::dispatch_rows_kernel<T><<<groups(n), spdnn::kRowThreads, 0, s>>>((const T*)x, x_stride, rows, k, width, place, offsets + experts, (T*)xs, xs_stride);
+            with_vec<16 / sizeof(T)>(width, [&](auto v) {
+                constexpr int V = decltype(v)::value;
+                const spdnn::Tiles g = tiles(rows, width, V, spdnn::kDispatchVecs, (int64_t)n * width * sizeof(T));
+                spdnn::dispatch_rows_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, place, offsets + experts, (T*)xs, xs_stride);
+            });
         });
     return launched();
 }
@@ -254,7 +272,17 @@ int spdnn_combine(const void* ys, int32_t type, int32_t width, int64_t ys_stride
     if (rows == 0) return SPDNN_OK;
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
-        spdnn::combine_kernel<T><<<groups(rows), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>((const T*)ys, ys_stride, place, weight, rows, k, width, (const T*)add, add_stride, (T*)out, out_stride);
+        with_vec<16 / sizeof(T)>(width, [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            const spdnn::Tiles g = tiles(rows, width, V, spdnn::kCombineVecs, (int64_t)rows * width * sizeof(T));
+            const auto run = [&](auto j, auto weighted) {
+                spdnn::combine_kernel<T, V, decltype(j)::value, decltype(weighted)::value><<<groups(g), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>(g, (const T*)ys, ys_stride, place, weight, k, (const T*)add, add_stride, (T*)out, out_stride);
+            };
+            with_places(k, [&](auto j) {
+                if (weight) run(j, std::true_type{});
+                else run(j, std::false_type{});
+            });
+        });
     });
     return launched();
 }

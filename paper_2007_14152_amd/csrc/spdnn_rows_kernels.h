@@ -35,9 +35,9 @@ struct Tiles {
     int32_t per;     // rows of a tile
     int32_t slab;    // vectors of a row in a tile
     uint32_t magic;  // ceil(2^32 / slab): quotients by slab > 1 for what is less than 2^16
+    bool past;       // stores that leave nothing in the caches
 };
 constexpr int kTileVecs = 4096;  // at most, of a tile
-constexpr int kUnroll = 4;       // vectors that a lane has under way
 
 // Rows may start at any element: vectors are only aligned like one (global memory takes such loads and stores whole).
 template <typename T, int V>
@@ -48,29 +48,54 @@ __device__ inline Pack<T, V> load_vec(const T* p) {
     if constexpr (V == 1) return Pack<T, V>(*p);
     else return *reinterpret_cast<const Pack<T, V>*>(p);
 }
+// past: the same for all lanes.  The empty asm on both sides of that branch keeps the compiler from making one store of the two,
+// an ordinary one.
 template <int V, typename T>
-__device__ inline void store_vec(T* p, const float (&from)[V]) {
+__device__ inline void store_vec(T* p, Pack<T, V> x, bool past) {
+    if (past) {
+        asm volatile("");
+        __builtin_nontemporal_store(x, reinterpret_cast<Pack<T, V>*>(p));
+        asm volatile("");
+    } else {
+        *reinterpret_cast<Pack<T, V>*>(p) = x;
+    }
+}
+template <typename T, int V>
+__device__ inline Pack<T, V> rounded_vec(const float (&from)[V]) {
     Pack<T, V> x;
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = rounded<T>(from[i]);
-    *reinterpret_cast<Pack<T, V>*>(p) = x;
+    return x;
+}
+// U of them, with one branch; at(u) is where vector u goes.
+template <int V, typename T, int U, typename F>
+__device__ inline void store_all(const Pack<T, V> (&x)[U], bool past, F at) {
+    if (past) {
+        asm volatile("");
+#pragma unroll
+        for (int u = 0; u < U; ++u) __builtin_nontemporal_store(x[u], reinterpret_cast<Pack<T, V>*>(at(u)));
+        asm volatile("");
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) *reinterpret_cast<Pack<T, V>*>(at(u)) = x[u];
+    }
 }
 
-// f(places of kUnroll vectors of the tile) until the tile is done; f has the loads of all of them to overlap.
+// f(places of U vectors of the tile) until the tile is done; f has the loads of all of them to overlap.
 struct At {
     int64_t row;
     int32_t col;
 };
-template <int V, typename F>
+template <int V, int U, typename F>
 __device__ inline void each_vec(const Tiles& g, F f) {
     for (int64_t r0 = (int64_t)blockIdx.x * g.per; r0 < g.rows; r0 += (int64_t)gridDim.x * g.per)
         for (int vec0 = blockIdx.y * g.slab; vec0 < g.vecs; vec0 += gridDim.y * g.slab) {
             const int rows = (int)min((int64_t)g.per, g.rows - r0);
             const int items = rows * g.slab;
-            for (int i0 = threadIdx.x; i0 < items; i0 += kUnroll * kRowThreads) {
-                At at[kUnroll];
+            for (int i0 = threadIdx.x; i0 < items; i0 += U * kRowThreads) {
+                At at[U];
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
+                for (int u = 0; u < U; ++u) {
                     const uint32_t i = min(i0 + u * kRowThreads, items - 1);
                     const uint32_t r = g.per == 1 ? 0 : g.slab == 1 ? i : __umulhi(i, g.magic);
                     const int vec = min(vec0 + (int)(i - r * g.slab), g.vecs - 1);
@@ -82,28 +107,32 @@ __device__ inline void each_vec(const Tiles& g, F f) {
         }
 }
 
+constexpr int kEmbedVecs = 4;  // vectors that a lane has under way
+
 // out[t] = scale * table[ids[t]].
 template <typename T, typename S, typename I, int V>
 __global__ __launch_bounds__(kRowThreads) void embed_kernel(Tiles g, const T* __restrict__ table, int64_t table_stride, uint32_t vocab,
                                                             const I* __restrict__ ids, float scale, S* __restrict__ out, int64_t out_stride) {
-    each_vec<V>(g, [&](const At (&at)[kUnroll]) {
-        I id[kUnroll];
-        Pack<T, V> x[kUnroll];
+    each_vec<V, kEmbedVecs>(g, [&](const At (&at)[kEmbedVecs]) {
+        I id[kEmbedVecs];
+        Pack<T, V> x[kEmbedVecs];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) id[u] = ids[at[u].row];
+        for (int u = 0; u < kEmbedVecs; ++u) id[u] = ids[at[u].row];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < kEmbedVecs; ++u) {
             const bool in = id[u] >= 0 && id[u] < (I)vocab;
             x[u] = load_vec<V>(table + (in ? (int64_t)id[u] : 0) * table_stride + at[u].col);
         }
+        Pack<S, V> y[kEmbedVecs];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < kEmbedVecs; ++u) {
             const bool in = id[u] >= 0 && id[u] < (I)vocab;
-            float y[V];
+            float to[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = in ? scale * (float)x[u][i] : 0.0f;
-            store_vec<V>(out + at[u].row * out_stride + at[u].col, y);
+            for (int i = 0; i < V; ++i) to[i] = in ? scale * (float)x[u][i] : 0.0f;
+            y[u] = rounded_vec<S, V>(to);
         }
+        store_all<V, S>(y, g.past, [&](int u) { return out + at[u].row * out_stride + at[u].col; });
     });
 }
 
@@ -308,38 +337,100 @@ __global__ __launch_bounds__(64) void expert_place_kernel(const int32_t* __restr
     }
 }
 
-// xs[place[t][j]] = x[t] (of: pair -> row of x), zeros behind the rows in use.
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(const T* __restrict__ x, int64_t x_stride, int rows, int k, int width,
-                                                                    const int32_t* __restrict__ place, const int32_t* __restrict__ count,
-                                                                    T* __restrict__ xs, int64_t xs_stride) {
-    const int64_t n = (int64_t)rows * k;
-    for (int64_t p = blockIdx.x; p < n; p += gridDim.x) {
-        const int at = place[p];
-        if (at >= 0)
-            for (int d = threadIdx.x; d < width; d += kRowThreads) xs[at * xs_stride + d] = x[p / k * x_stride + d];
-        if (p >= *count)
-            for (int d = threadIdx.x; d < width; d += kRowThreads) xs[p * xs_stride + d] = (T)0.0f;
-    }
+// J of a row's places at a time, -1 where there is none: all of them before the first load or store that needs one, for a wait
+// for a load is a wait for every load and store before it.
+template <int J, int U>
+__device__ inline void load_places(const int32_t* __restrict__ place, const At (&at)[U], int j0, int k, int64_t n, int (&to)[U][J]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < J; ++j) to[u][j] = place[at[u].row * k + min(j0 + j, k - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (j0 + j >= k || to[u][j] >= n) to[u][j] = -1;
 }
 
-// out[t] = add[t] + sum of weight[t][j] * ys[place[t][j]]; a workgroup per row.
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void combine_kernel(const T* __restrict__ ys, int64_t ys_stride, const int32_t* __restrict__ place,
-                                                              const float* __restrict__ weight, int rows, int k, int width, const T* add,
-                                                              int64_t add_stride, T* out, int64_t out_stride) {
-    const int64_t n = (int64_t)rows * k;
-    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x)
-        for (int d = threadIdx.x; d < width; d += kRowThreads) {
-            float sum = 0.0f;
-            for (int j = 0; j < k; ++j) {
-                const int at = place[t * k + j];
-                if (at < 0 || at >= n) continue;
-                const float y = (float)ys[at * ys_stride + d];
-                sum = weight ? fmaf(weight[t * k + j], y, sum) : sum + y;
-            }
-            out[t * out_stride + d] = rounded<T>(add ? sum + (float)add[t * add_stride + d] : sum);
+// xs[place[t][j]] = x[t], and zeros in those of the positions t * k .. t * k + k - 1 that no pair has.
+constexpr int kDispatchVecs = 2, kDispatchPlaces = 4;
+template <typename T, int V>
+__global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k,
+                                                                    const int32_t* __restrict__ place, const int32_t* __restrict__ count,
+                                                                    T* __restrict__ xs, int64_t xs_stride) {
+    constexpr int U = kDispatchVecs, J = kDispatchPlaces;
+    const int used = *count;
+    each_vec<V, U>(g, [&](const At (&at)[U]) {
+        Pack<T, V> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = load_vec<V>(x + at[u].row * x_stride + at[u].col);
+        for (int j0 = 0; j0 < k; j0 += J) {
+            int to[U][J];
+            load_places<J, U>(place, at, j0, k, g.rows * k, to);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    if (to[u][j] >= 0) store_vec<V, T>(xs + (int64_t)to[u][j] * xs_stride + at[u].col, v[u], g.past);
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            for (int64_t p = max(at[u].row * k, (int64_t)used); p < (at[u].row + 1) * k; ++p)
+                store_vec<V, T>(xs + p * xs_stride + at[u].col, Pack<T, V>{}, g.past);
+    });
+}
+
+// out[t] = add[t] + sum of weight[t][j] * ys[place[t][j]], j ascending, one fused multiply-add each.
+constexpr int kCombineVecs = 2;
+template <typename T, int V, int J, bool WEIGHTED>
+__global__ __launch_bounds__(kRowThreads) void combine_kernel(Tiles g, const T* __restrict__ ys, int64_t ys_stride, const int32_t* __restrict__ place,
+                                                              const float* __restrict__ weight, int k, const T* __restrict__ add,
+                                                              int64_t add_stride, T* __restrict__ out, int64_t out_stride) {
+    constexpr int U = kCombineVecs;
+    each_vec<V, U>(g, [&](const At (&at)[U]) {
+        float sum[U][V] = {};
+        Pack<T, V> r[U] = {};
+        for (int j0 = 0; j0 < k; j0 += J) {
+            int from[U][J];
+            float w[U][J];
+            Pack<T, V> y[U][J];
+            if (WEIGHTED) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) w[u][j] = weight[at[u].row * k + min(j0 + j, k - 1)];
+            }
+            load_places<J, U>(place, at, j0, k, g.rows * k, from);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    if (from[u][j] >= 0) y[u][j] = load_vec<V>(ys + (int64_t)from[u][j] * ys_stride + at[u].col);
+            if (add && j0 == 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) r[u] = load_vec<V>(add + at[u].row * add_stride + at[u].col);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float x = WEIGHTED ? fmaf(w[u][j], (float)y[u][j][i], sum[u][i]) : sum[u][i] + (float)y[u][j][i];
+                        sum[u][i] = from[u][j] >= 0 ? x : sum[u][i];
+                    }
+        }
+        Pack<T, V> y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (add) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[u][i] += (float)r[u][i];
+            }
+            y[u] = rounded_vec<T, V>(sum[u]);
+        }
+        store_all<V, T>(y, g.past, [&](int u) { return out + at[u].row * out_stride + at[u].col; });
+    });
 }
 
 // dys[place[t][j]] = weight[t][j] * dout[t], dweight[t][j] = <dout[t], ys[place[t][j]]>; a wave per pair.
