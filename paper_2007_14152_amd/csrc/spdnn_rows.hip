@@ -111,6 +111,17 @@ void with_ids(int32_t type, F f) {
     else f(int64_t{});
 }
 
+// How n pairs are cut for the sort.
+struct Chunks {
+    int64_t size;
+    int32_t count;  // 1 at least
+};
+Chunks chunks_of(int64_t n) {
+    const int64_t each = (n + spdnn::kMostChunks - 1) / spdnn::kMostChunks;
+    const int64_t size = std::max<int64_t>(spdnn::kLeastChunk, (each + spdnn::kSortThreads - 1) / spdnn::kSortThreads * spdnn::kSortThreads);
+    return {size, (int32_t)std::max<int64_t>(1, (n + size - 1) / size)};
+}
+
 // f(V) with the elements of a vector: V, or 1 where a row has less.
 template <int V, typename F>
 void with_vec(int32_t width, F f) {
@@ -226,7 +237,7 @@ int spdnn_route_grad(const float* dweight, const void* logits, int32_t type, int
 int spdnn_dispatch_bytes(int32_t rows, int32_t k, int32_t experts, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
     CHECK(check_pairs(rows, k, experts));
-    *bytes = sizeof(int32_t) * SPDNN_MAX_EXPERTS;
+    *bytes = sizeof(int32_t) * experts * chunks_of((int64_t)rows * k).count;
     return SPDNN_OK;
 }
 
@@ -244,9 +255,10 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
     CHECK(check_array("offsets", offsets, 1, 4));
     CHECK(check_work(work, work_bytes, need));
     const hipStream_t s = (hipStream_t)hip_stream;
-    int32_t* counts = (int32_t*)work;
-    spdnn::expert_count_kernel<<<experts, spdnn::kRowThreads, 0, s>>>(chosen, n, counts);
-    spdnn::expert_place_kernel<<<experts + 1, 64, 0, s>>>(chosen, n, experts, counts, offsets, place);
+    const Chunks c = chunks_of(n);
+    const spdnn::PairDigits digit{chosen, experts};
+    spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, experts, (int32_t*)work);
+    spdnn::expert_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, (const int32_t*)work, c.count, offsets, place);
     if (n > 0)
         with_type(type, [&](auto tt) {
             using T = decltype(tt);

@@ -305,36 +305,131 @@ __global__ __launch_bounds__(64) void route_grad_kernel(const float* __restrict_
 
 // --- rows by expert ---------------------------------------------------------
 
-// counts[e] = pairs with expert e; a workgroup per expert.
-__global__ __launch_bounds__(kRowThreads) void expert_count_kernel(const int32_t* __restrict__ chosen, int n, int32_t* __restrict__ counts) {
-    __shared__ int32_t total;
-    if (threadIdx.x == 0) total = 0;
+// A stable counting sort of pairs (or of ids, a digit of their bits at a time) by a number d < bins, in two launches: the pairs
+// are cut into chunks, a workgroup per chunk counts (count_kernel), then every workgroup adds up the counts of all chunks for
+// itself, which is cheaper than a launch for it, and places its chunk's pairs (place_kernel).  A chunk is cut into a segment per
+// wave; a wave takes 64 pairs at a time, whose rank among equals comes from ballots, a bit of d at a time: no pair's position
+// depends on which wave was first.
+constexpr int kSortWaves = 4, kSortThreads = 64 * kSortWaves;
+constexpr int kMostBins = 1024;
+constexpr int kMostChunks = 128;  // more pairs than these hold make the chunks longer
+constexpr int kLeastChunk = 1024;
+
+// The experts of pairs: -1 without one.
+struct PairDigits {
+    const int32_t* chosen;
+    int experts;
+    __device__ int operator()(int64_t p) const {
+        const int e = chosen[p];
+        return e >= 0 && e < experts ? e : -1;
+    }
+};
+
+struct SortLds {
+    int32_t start[kSortWaves][kMostBins];
+    int32_t total[kMostBins];
+    int32_t wave_sum[kSortWaves];
+};
+
+template <typename D>
+__global__ __launch_bounds__(kSortThreads) void count_kernel(D digit, int64_t n, int64_t chunk, int bins, int32_t* __restrict__ table) {
+    __shared__ int32_t count[kMostBins];
+    for (int e = threadIdx.x; e < bins; e += kSortThreads) count[e] = 0;
     __syncthreads();
-    int mine = 0;
-    for (int p = threadIdx.x; p < n; p += kRowThreads) mine += chosen[p] == (int)blockIdx.x;
-    atomicAdd(&total, mine);
+    const int64_t first = blockIdx.x * chunk, last = min(first + chunk, n);
+    for (int64_t p = first + threadIdx.x; p < last; p += kSortThreads) {
+        const int d = digit(p);
+        if (d >= 0) atomicAdd(&count[d], 1);
+    }
     __syncthreads();
-    if (threadIdx.x == 0) counts[blockIdx.x] = total;
+    for (int e = threadIdx.x; e < bins; e += kSortThreads) table[(int64_t)blockIdx.x * bins + e] = count[e];
 }
 
-// offsets from counts, places of expert blockIdx.x's pairs; workgroup `experts` does the pairs without an expert.
-__global__ __launch_bounds__(64) void expert_place_kernel(const int32_t* __restrict__ chosen, int n, int experts, const int32_t* __restrict__ counts,
-                                                          int32_t* __restrict__ offsets, int32_t* __restrict__ place) {
-    const int lane = threadIdx.x, me = blockIdx.x;
-    int before = 0;
-    for (int e = 0; e < me; ++e) before += counts[e];
-    if (lane == 0) offsets[me] = before;
-    for (int p0 = 0; p0 < n; p0 += 64) {
-        const int p = p0 + lane;
-        const int e = p < n ? chosen[p] : experts;
-        if (me == experts) {
-            if (p < n && (e < 0 || e >= experts)) place[p] = -1;
-            continue;
-        }
-        const uint64_t same = __ballot(e == me);
-        if (e == me) place[p] = before + __popcll(same & ((1ull << lane) - 1));
-        before += __popcll(same);
+// to(pair, position) for every pair of chunk `me`, position -1 without a digit; offsets (may be NULL): first positions of the
+// bins, and the end.  table: the counts of `chunks` chunks, or NULL if there is only this one.
+template <typename D, typename F>
+__device__ inline void place_chunk(D digit, int64_t first, int64_t last, int bins, const int32_t* __restrict__ table, int chunks, int me,
+                                   SortLds& lds, int32_t* __restrict__ offsets, F to) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t part = ((last - first + kSortThreads - 1) / kSortThreads) * 64;
+    const int64_t mine = min(first + wave * part, last), end = min(mine + part, last);
+    for (int e = threadIdx.x; e < kSortWaves * kMostBins; e += kSortThreads) lds.start[0][e] = 0;
+    __syncthreads();
+    for (int64_t p = mine + lane; p < end; p += 64) {
+        const int d = digit(p);
+        if (d >= 0) atomicAdd(&lds.start[wave][d], 1);
     }
+    __syncthreads();
+    // bin e's pairs in all chunks, and in start[0][e] .. start[3][e] where each wave's first one goes, within the bin
+    for (int e = threadIdx.x; e < bins; e += kSortThreads) {
+        int before = 0, total = 0;
+        for (int c = 0; table && c < chunks; ++c) {
+            const int x = table[(int64_t)c * bins + e];
+            total += x;
+            before += c < me ? x : 0;
+        }
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int x = lds.start[w][e];
+            lds.start[w][e] = before;
+            before += x;
+        }
+        lds.total[e] = table ? total : before;
+    }
+    __syncthreads();
+    // a thread's bins next to each other: their sum, the sums before it, then each bin's first position
+    constexpr int kEach = kMostBins / kSortThreads;
+    int x[kEach], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int e = threadIdx.x * kEach + i;
+        x[i] = e < bins ? lds.total[e] : 0;
+        sum += x[i];
+    }
+    int upto = sum;
+    for (int m = 1; m < 64; m <<= 1) {
+        const int o = __shfl_up(upto, m);
+        if (lane >= m) upto += o;
+    }
+    if (lane == 63) lds.wave_sum[wave] = upto;
+    __syncthreads();
+    int base = upto - sum;
+    for (int w = 0; w < wave; ++w) base += lds.wave_sum[w];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int e = threadIdx.x * kEach + i;
+        if (e < bins) {
+            if (offsets) offsets[e] = base;
+            for (int w = 0; w < kSortWaves; ++w) lds.start[w][e] += base;
+            base += x[i];
+            if (offsets && e == bins - 1) offsets[bins] = base;
+        }
+    }
+    __syncthreads();
+    const int bits = 32 - __clz(bins - 1 | 1);
+    volatile int32_t* start = lds.start[wave];  // read and written by this wave alone, in the order written here
+    for (int64_t p0 = mine; p0 < end; p0 += 64) {
+        const int64_t p = p0 + lane;
+        const int d = p < end ? digit(p) : -1;
+        uint64_t same = __ballot(d >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot(d >> b & 1);
+            same &= d >> b & 1 ? set : ~set;
+        }
+        int at = -1;
+        if (d >= 0) {
+            at = start[d] + __popcll(same & ((1ull << lane) - 1));
+            if (lane == 63 - __clzll(same)) start[d] = at + 1;  // the last of its kind leaves where the next one goes
+        }
+        if (p < end) to(p, at);
+    }
+}
+
+__global__ __launch_bounds__(kSortThreads) void expert_place_kernel(PairDigits digit, int64_t n, int64_t chunk, const int32_t* __restrict__ table,
+                                                                    int chunks, int32_t* __restrict__ offsets, int32_t* __restrict__ place) {
+    __shared__ SortLds lds;
+    const int64_t first = blockIdx.x * chunk;
+    place_chunk(digit, first, min(first + chunk, n), digit.experts, table, chunks, blockIdx.x, lds, blockIdx.x == 0 ? offsets : nullptr,
+                [&](int64_t p, int at) { place[p] = at; });
 }
 
 // J of a row's places at a time, -1 where there is none: all of them before the first load or store that needs one, for a wait
