@@ -255,17 +255,23 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
     CHECK(check_array("offsets", offsets, 1, 4));
     CHECK(check_work(work, work_bytes, need));
     const hipStream_t s = (hipStream_t)hip_stream;
-    const Chunks c = chunks_of(n);
     const spdnn::PairDigits digit{chosen, experts};
-    spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, experts, (int32_t*)work);
-    spdnn::expert_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, (const int32_t*)work, c.count, offsets, place);
+    const bool few = n > 0 && n <= spdnn::kFewPairs;
+    if (!few) {
+        const Chunks c = chunks_of(n);
+        spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, experts, (int32_t*)work);
+        spdnn::expert_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, (const int32_t*)work, c.count, offsets, place);
+    }
     if (n > 0)
         with_type(type, [&](auto tt) {
             using T = decltype(tt);
             with_vec<16 / sizeof(T)>(width, [&](auto v) {
                 constexpr int V = decltype(v)::value;
                 const spdnn::Tiles g = tiles(rows, width, V, spdnn::kDispatchVecs, (int64_t)n * width * sizeof(T));
-                spdnn::dispatch_rows_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, place, offsets + experts, (T*)xs, xs_stride);
+                if (few)
+                    spdnn::dispatch_few_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, digit, offsets, place, (T*)xs, xs_stride);
+                else
+                    spdnn::dispatch_rows_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, place, offsets + experts, (T*)xs, xs_stride);
             });
         });
     return launched();

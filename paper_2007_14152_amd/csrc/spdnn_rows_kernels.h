@@ -353,7 +353,8 @@ __device__ inline void place_chunk(D digit, int64_t first, int64_t last, int bin
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t part = ((last - first + kSortThreads - 1) / kSortThreads) * 64;
     const int64_t mine = min(first + wave * part, last), end = min(mine + part, last);
-    for (int e = threadIdx.x; e < kSortWaves * kMostBins; e += kSortThreads) lds.start[0][e] = 0;
+    for (int e = threadIdx.x; e < bins; e += kSortThreads)
+        for (int w = 0; w < kSortWaves; ++w) lds.start[w][e] = 0;
     __syncthreads();
     for (int64_t p = mine + lane; p < end; p += 64) {
         const int d = digit(p);
@@ -450,11 +451,9 @@ __device__ inline void load_places(const int32_t* __restrict__ place, const At (
 // xs[place[t][j]] = x[t], and zeros in those of the positions t * k .. t * k + k - 1 that no pair has.
 constexpr int kDispatchVecs = 2, kDispatchPlaces = 4;
 template <typename T, int V>
-__global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k,
-                                                                    const int32_t* __restrict__ place, const int32_t* __restrict__ count,
-                                                                    T* __restrict__ xs, int64_t xs_stride) {
+__device__ inline void dispatch_rows(const Tiles& g, const T* __restrict__ x, int64_t x_stride, int k, const int32_t* __restrict__ place, int used,
+                                     T* __restrict__ xs, int64_t xs_stride) {
     constexpr int U = kDispatchVecs, J = kDispatchPlaces;
-    const int used = *count;
     each_vec<V, U>(g, [&](const At (&at)[U]) {
         Pack<T, V> v[U];
 #pragma unroll
@@ -473,6 +472,34 @@ __global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(Tiles g, con
             for (int64_t p = max(at[u].row * k, (int64_t)used); p < (at[u].row + 1) * k; ++p)
                 store_vec<V, T>(xs + p * xs_stride + at[u].col, Pack<T, V>{}, g.past);
     });
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k,
+                                                                    const int32_t* __restrict__ place, const int32_t* __restrict__ count,
+                                                                    T* __restrict__ xs, int64_t xs_stride) {
+    dispatch_rows<T, V>(g, x, x_stride, k, place, *count, xs, xs_stride);
+}
+
+// Few pairs: every workgroup sorts all of them for itself and moves its tile of rows, one launch in all.
+constexpr int kFewPairs = 1024;
+template <typename T, int V>
+__global__ __launch_bounds__(kRowThreads) void dispatch_few_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k, PairDigits digit,
+                                                                   int32_t* __restrict__ offsets, int32_t* __restrict__ place, T* __restrict__ xs,
+                                                                   int64_t xs_stride) {
+    static_assert(kRowThreads == kSortThreads);
+    __shared__ SortLds lds;
+    __shared__ int32_t places[kFewPairs];
+    __shared__ int32_t used;
+    const bool first = blockIdx.x == 0 && blockIdx.y == 0;
+    if (threadIdx.x == 0) used = 0;
+    place_chunk(digit, 0, g.rows * k, digit.experts, nullptr, 1, 0, lds, first ? offsets : nullptr, [&](int64_t p, int at) {
+        places[p] = at;
+        if (at >= 0) atomicMax(&used, at + 1);
+        if (first) place[p] = at;
+    });
+    __syncthreads();
+    dispatch_rows<T, V>(g, x, x_stride, k, places, used, xs, xs_stride);
 }
 
 // out[t] = add[t] + sum of weight[t][j] * ys[place[t][j]], j ascending, one fused multiply-add each.
