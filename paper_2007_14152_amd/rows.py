@@ -7,11 +7,12 @@ any stride between them, their elements are adjacent; what the library refuses r
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
 from . import (SPDNN_BF16, SPDNN_EINVAL, SPDNN_F16, SPDNN_F32, SPDNN_I32, SPDNN_I64, SPDNN_SIGMOID, SPDNN_SOFTMAX, SpdnnError,
-               _check, _NO_SWITCH, lib)
+               _check, lib)
 
 _TYPES = {torch.float32: SPDNN_F32, torch.bfloat16: SPDNN_BF16, torch.float16: SPDNN_F16}
 _IDS = {torch.int32: SPDNN_I32, torch.int64: SPDNN_I64}
@@ -31,34 +32,52 @@ def _type(dtype, name):
 
 def _rows(t, name, device=None, shape=None):
     """(type, stride) of a matrix of rows."""
-    if t.dim() != 2 or not t.is_cuda:
-        _refuse("%s: a matrix in GPU memory, not %s on %s", name, tuple(t.shape), t.device)
+    size = t.shape
+    if len(size) != 2 or not t.is_cuda:
+        _refuse("%s: a matrix in GPU memory, not %s on %s", name, tuple(size), t.device)
     if device is not None and t.device != device:
         _refuse("%s is on %s, not on %s", name, t.device, device)
-    if shape is not None and tuple(t.shape) != shape:
-        _refuse("%s: %s, not %s", name, shape, tuple(t.shape))
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if shape is not None and size != shape:
+        _refuse("%s: %s, not %s", name, shape, tuple(size))
+    stride, step = t.stride()
+    if step != 1 and size[1] > 1:
         _refuse("%s: the elements of a row must be adjacent", name)
-    return _type(t.dtype, name), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        _type(t.dtype, name)
+    return code, stride if size[0] > 1 else max(stride, size[1])
 
 
 def _array(t, name, dtypes, device, shape):
     """Address of a contiguous array, 0 for None."""
     if t is None:
         return 0
-    if t.dtype not in dtypes or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype not in dtypes or t.device != device or t.shape != shape or not t.is_contiguous():
         _refuse("%s: a contiguous %s of %s on %s, not %s of %s on %s", name, shape, dtypes[0], device, tuple(t.shape), t.dtype, t.device)
     return t.data_ptr()
 
 
-def _on(device):
-    return _NO_SWITCH if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+_F32 = (torch.float32,)
+_I32 = (torch.int32,)
+_BYTES = (torch.bool, torch.uint8)
+
+# The raw handle of a device's current stream.  (torch.cuda.current_stream makes an object around it first, which takes 1.9 us;
+# the smallest call there is takes 4.5.)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+def _on_device(f):
+    """f with the device of its first argument made current, if it is not."""
+    @functools.wraps(f)
+    def call(t, *args, **kwargs):
+        if t.is_cuda and t.device.index != torch.cuda.current_device():
+            with torch.cuda.device(t.device):
+                return f(t, *args, **kwargs)
+        return f(t, *args, **kwargs)
+    return call
 
 
+@_on_device
 def embed(table, ids, scale=1.0, dtype=None):
     """scale * table[ids], rows of zeros for ids outside the table (padding): [*ids.shape, width] of dtype (the table's).
 
@@ -71,13 +90,13 @@ def embed(table, ids, scale=1.0, dtype=None):
     if ids.dtype not in _IDS or ids.device != dev:
         _refuse("ids: int32 or int64 on %s, not %s on %s", dev, ids.dtype, ids.device)
     ids = ids.contiguous()
-    with _on(dev):
-        out = torch.empty((*ids.shape, width), dtype=dtype, device=dev)
-        _check(lib().spdnn_embed(table.data_ptr(), ttype, vocab, width, tstride, ids.data_ptr(), _IDS[ids.dtype], ids.numel(),
-                                 scale, out.data_ptr(), otype, width, _stream(dev)))
+    out = torch.empty((*ids.shape, width), dtype=dtype, device=dev)
+    _check(lib().spdnn_embed(table.data_ptr(), ttype, vocab, width, tstride, ids.data_ptr(), _IDS[ids.dtype], ids.numel(),
+                             scale, out.data_ptr(), otype, width, _stream(dev.index)))
     return out
 
 
+@_on_device
 def embed_grad(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
     """Gradient of embed's table, [vocab, width]: scale * the sum of dout's rows of each id.
 
@@ -93,16 +112,15 @@ def embed_grad(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
         _refuse("ids: %d of int32 or int64 on %s, not %d of %s on %s", n, dev, ids.numel(), ids.dtype, ids.device)
     ids = ids.contiguous()
     add = out is not None
-    with _on(dev):
-        if not add:
-            _type(dtype, "dtype")
-            out = torch.empty((vocab, width), dtype=dtype, device=dev)
-        otype, ostride = _rows(out, "out", dev, (vocab, width))
-        need = ctypes.c_size_t()
-        _check(lib().spdnn_embed_grad_bytes(vocab, width, n, ctypes.byref(need)))
-        work = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        _check(lib().spdnn_embed_grad(dout.data_ptr(), itype, dstride, ids.data_ptr(), _IDS[ids.dtype], n, vocab, width, scale,
-                                      add, out.data_ptr(), otype, ostride, work.data_ptr(), need.value, _stream(dev)))
+    if not add:
+        _type(dtype, "dtype")
+        out = torch.empty((vocab, width), dtype=dtype, device=dev)
+    otype, ostride = _rows(out, "out", dev, (vocab, width))
+    need = ctypes.c_size_t()
+    _check(lib().spdnn_embed_grad_bytes(vocab, width, n, ctypes.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    _check(lib().spdnn_embed_grad(dout.data_ptr(), itype, dstride, ids.data_ptr(), _IDS[ids.dtype], n, vocab, width, scale,
+                                  add, out.data_ptr(), otype, ostride, work.data_ptr(), need.value, _stream(dev.index)))
     return out
 
 
@@ -112,6 +130,7 @@ def _score(score):
     return _SCORES[score]
 
 
+@_on_device
 def route(logits, k, bias=None, keep=None, score="softmax", normalise=True, scale=1.0):
     """(chosen int32 [rows, k], weight float32 [rows, k]): the k experts of each row with the largest logits (plus bias,
     which only the choice sees), and their weights; -1 and 0 where a row has no expert left.
@@ -120,16 +139,16 @@ def route(logits, k, bias=None, keep=None, score="softmax", normalise=True, scal
     ltype, stride = _rows(logits, "logits")
     rows, experts = logits.shape
     dev = logits.device
-    bp = _array(bias, "bias", (torch.float32,), dev, (experts,))
-    kp = _array(keep, "keep", (torch.bool, torch.uint8), dev, (rows,))
-    with _on(dev):
-        chosen = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
-        weight = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
-        _check(lib().spdnn_route(logits.data_ptr(), ltype, stride, rows, experts, k, bp, kp, _score(score), normalise, scale,
-                                 chosen.data_ptr(), weight.data_ptr(), _stream(dev)))
+    bp = _array(bias, "bias", _F32, dev, (experts,))
+    kp = _array(keep, "keep", _BYTES, dev, (rows,))
+    chosen = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
+    weight = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
+    _check(lib().spdnn_route(logits.data_ptr(), ltype, stride, rows, experts, k, bp, kp, _score(score), normalise, scale,
+                             chosen.data_ptr(), weight.data_ptr(), _stream(dev.index)))
     return chosen, weight
 
 
+@_on_device
 def route_grad(dweight, logits, chosen, bias=None, score="softmax", normalise=True, scale=1.0):
     """Gradient of route's weights with respect to the logits, of the logits' type; chosen, bias, score, normalise and scale
     as they were there."""
@@ -139,16 +158,16 @@ def route_grad(dweight, logits, chosen, bias=None, score="softmax", normalise=Tr
     if chosen.dim() != 2:
         _refuse("chosen: a matrix, not %s", tuple(chosen.shape))
     k = chosen.shape[1]
-    bp = _array(bias, "bias", (torch.float32,), dev, (experts,))
-    cp = _array(chosen, "chosen", (torch.int32,), dev, (rows, k))
-    wp = _array(dweight, "dweight", (torch.float32,), dev, (rows, k))
-    with _on(dev):
-        out = torch.empty((rows, experts), dtype=logits.dtype, device=dev)
-        _check(lib().spdnn_route_grad(wp, logits.data_ptr(), ltype, stride, cp, rows, experts, k, bp, _score(score), normalise,
-                                      scale, out.data_ptr(), experts, _stream(dev)))
+    bp = _array(bias, "bias", _F32, dev, (experts,))
+    cp = _array(chosen, "chosen", _I32, dev, (rows, k))
+    wp = _array(dweight, "dweight", _F32, dev, (rows, k))
+    out = torch.empty((rows, experts), dtype=logits.dtype, device=dev)
+    _check(lib().spdnn_route_grad(wp, logits.data_ptr(), ltype, stride, cp, rows, experts, k, bp, _score(score), normalise,
+                                  scale, out.data_ptr(), experts, _stream(dev.index)))
     return out
 
 
+@_on_device
 def dispatch(x, chosen, experts):
     """(xs [rows * k, width], offsets int32 [experts + 1], place int32 [rows, k]): x's rows sorted by expert, once for each
     expert they go to.  Expert e has the rows offsets[e] .. offsets[e + 1] of xs; row t's copy for its slot j is row
@@ -159,19 +178,19 @@ def dispatch(x, chosen, experts):
     if chosen.dim() != 2:
         _refuse("chosen: a matrix, not %s", tuple(chosen.shape))
     k = chosen.shape[1]
-    cp = _array(chosen, "chosen", (torch.int32,), dev, (rows, k))
-    with _on(dev):
-        need = ctypes.c_size_t()
-        _check(lib().spdnn_dispatch_bytes(rows, k, experts, ctypes.byref(need)))
-        xs = torch.empty((rows * k, width), dtype=x.dtype, device=dev)
-        offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev)
-        place = torch.empty((rows, k), dtype=torch.int32, device=dev)
-        work = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        _check(lib().spdnn_dispatch(cp, rows, k, experts, x.data_ptr(), xtype, width, xstride, xs.data_ptr(), width,
-                                    offsets.data_ptr(), place.data_ptr(), work.data_ptr(), need.value, _stream(dev)))
+    cp = _array(chosen, "chosen", _I32, dev, (rows, k))
+    need = ctypes.c_size_t()
+    _check(lib().spdnn_dispatch_bytes(rows, k, experts, ctypes.byref(need)))
+    xs = torch.empty((rows * k, width), dtype=x.dtype, device=dev)
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev)
+    place = torch.empty((rows, k), dtype=torch.int32, device=dev)
+    work = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    _check(lib().spdnn_dispatch(cp, rows, k, experts, x.data_ptr(), xtype, width, xstride, xs.data_ptr(), width,
+                                offsets.data_ptr(), place.data_ptr(), work.data_ptr(), need.value, _stream(dev.index)))
     return xs, offsets, place
 
 
+@_on_device
 def _back(ys, place, weight, add):
     ytype, ystride = _rows(ys, "ys")
     dev = ys.device
@@ -181,18 +200,17 @@ def _back(ys, place, weight, add):
     width = ys.shape[1]
     if ys.shape[0] != rows * k:
         _refuse("ys: %d rows for %d x %d places", ys.shape[0], rows, k)
-    pp = _array(place, "place", (torch.int32,), dev, (rows, k))
-    wp = _array(weight, "weight", (torch.float32,), dev, (rows, k))
+    pp = _array(place, "place", _I32, dev, (rows, k))
+    wp = _array(weight, "weight", _F32, dev, (rows, k))
     ap, astride = 0, width
     if add is not None:
         atype, astride = _rows(add, "add", dev, (rows, width))
         if atype != ytype:
             _refuse("add: %s, not %s", ys.dtype, add.dtype)
         ap = add.data_ptr()
-    with _on(dev):
-        out = torch.empty((rows, width), dtype=ys.dtype, device=dev)
-        _check(lib().spdnn_combine(ys.data_ptr(), ytype, width, ystride, pp, wp, rows, k, ap, astride, out.data_ptr(), width,
-                                   _stream(dev)))
+    out = torch.empty((rows, width), dtype=ys.dtype, device=dev)
+    _check(lib().spdnn_combine(ys.data_ptr(), ytype, width, ystride, pp, wp, rows, k, ap, astride, out.data_ptr(), width,
+                               _stream(dev.index)))
     return out
 
 
@@ -209,6 +227,7 @@ def dispatch_grad(dxs, place):
     return _back(dxs, place, None, None)
 
 
+@_on_device
 def combine_grad(dout, ys, place, weight, offsets):
     """(dys, dweight): gradients of combine with respect to ys and weight (that of add is dout).  offsets as dispatch gave
     them: rows of dys without a pair are zero."""
@@ -223,17 +242,16 @@ def combine_grad(dout, ys, place, weight, offsets):
     gtype, gstride = _rows(dout, "dout", dev, (rows, width))
     if gtype != ytype:
         _refuse("dout: %s, not %s", ys.dtype, dout.dtype)
-    pp = _array(place, "place", (torch.int32,), dev, (rows, k))
+    pp = _array(place, "place", _I32, dev, (rows, k))
     if weight is None:
         _refuse("weight is None")
-    wp = _array(weight, "weight", (torch.float32,), dev, (rows, k))
+    wp = _array(weight, "weight", _F32, dev, (rows, k))
     if offsets.dim() != 1 or offsets.shape[0] < 2:
         _refuse("offsets: one per expert and the end, not %s", tuple(offsets.shape))
-    op = _array(offsets, "offsets", (torch.int32,), dev, tuple(offsets.shape))
-    with _on(dev):
-        dys = torch.empty((rows * k, width), dtype=ys.dtype, device=dev)
-        dweight = torch.empty((rows, k), dtype=torch.float32, device=dev)
-        _check(lib().spdnn_combine_grad(dout.data_ptr(), ytype, width, gstride, ys.data_ptr(), ystride, pp, wp,
-                                        op + 4 * (offsets.shape[0] - 1), rows, k, dys.data_ptr(), width, dweight.data_ptr(),
-                                        _stream(dev)))
+    op = _array(offsets, "offsets", _I32, dev, tuple(offsets.shape))
+    dys = torch.empty((rows * k, width), dtype=ys.dtype, device=dev)
+    dweight = torch.empty((rows, k), dtype=torch.float32, device=dev)
+    _check(lib().spdnn_combine_grad(dout.data_ptr(), ytype, width, gstride, ys.data_ptr(), ystride, pp, wp,
+                                    op + 4 * (offsets.shape[0] - 1), rows, k, dys.data_ptr(), width, dweight.data_ptr(),
+                                    _stream(dev.index)))
     return dys, dweight
