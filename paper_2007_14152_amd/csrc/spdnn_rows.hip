@@ -321,7 +321,20 @@ int spdnn_combine_grad(const void* dout, int32_t type, int32_t width, int64_t do
     if (rows == 0) return SPDNN_OK;
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
-        spdnn::combine_grad_kernel<T><<<groups(n), 64, 0, (hipStream_t)hip_stream>>>((const T*)dout, dout_stride, (const T*)ys, ys_stride, place, weight, count, rows, k, width, (T*)dys, dys_stride, dweight);
+        const bool past = (int64_t)n * width * (int64_t)sizeof(T) >= kPastBytes;
+        with_vec<16 / sizeof(T)>(width, [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            const int vecs = (width - 1) / V + 1;
+            const auto run = [&](auto j, auto l) {
+                constexpr int L = decltype(l)::value;
+                spdnn::combine_grad_kernel<T, V, decltype(j)::value, L><<<groups((rows - 1) / (spdnn::kRowThreads / L) + 1), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>((const T*)dout, dout_stride, (const T*)ys, ys_stride, place, weight, count, rows, k, width, (T*)dys, dys_stride, dweight, past);
+            };
+            with_places(k, [&](auto j) {
+                if (vecs <= 32) run(j, std::integral_constant<int, 16>{});
+                else if (rows >= 2048) run(j, std::integral_constant<int, 64>{});
+                else run(j, std::integral_constant<int, 256>{});
+            });
+        });
     });
     return launched();
 }

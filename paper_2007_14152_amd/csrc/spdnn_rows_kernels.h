@@ -555,26 +555,85 @@ __global__ __launch_bounds__(kRowThreads) void combine_kernel(Tiles g, const T* 
     });
 }
 
-// dys[place[t][j]] = weight[t][j] * dout[t], dweight[t][j] = <dout[t], ys[place[t][j]]>; a wave per pair.
-template <typename T>
-__global__ __launch_bounds__(64) void combine_grad_kernel(const T* __restrict__ dout, int64_t dout_stride, const T* __restrict__ ys, int64_t ys_stride,
-                                                          const int32_t* __restrict__ place, const float* __restrict__ weight,
-                                                          const int32_t* __restrict__ count, int rows, int k, int width, T* __restrict__ dys,
-                                                          int64_t dys_stride, float* __restrict__ dweight) {
+// dys[place[t][j]] = weight[t][j] * dout[t], dweight[t][j] = <dout[t], ys[place[t][j]]>, zeros in those of the positions
+// t * k .. t * k + k - 1 that no pair has.  L lanes take a row, J of its slots at a time: dout is read once for all of them, and
+// a slot's row of ys comes in while its row of dys goes out.  A lane adds up its vectors in order, then the lanes' sums are
+// added pairwise.
+constexpr int kCombineGradVecs = 2;
+template <typename T, int V, int J, int L>
+__global__ __launch_bounds__(kRowThreads) void combine_grad_kernel(const T* __restrict__ dout, int64_t dout_stride, const T* __restrict__ ys, int64_t ys_stride,
+                                                                   const int32_t* __restrict__ place, const float* __restrict__ weight,
+                                                                   const int32_t* __restrict__ count, int rows, int k, int width, T* __restrict__ dys,
+                                                                   int64_t dys_stride, float* __restrict__ dweight, bool past) {
+    constexpr int U = kCombineGradVecs, kTeams = kRowThreads / L;
+    __shared__ float sums[kRowThreads / 64][J];
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int vecs = (width - 1) / V + 1;
     const int64_t n = (int64_t)rows * k;
-    for (int64_t p = blockIdx.x; p < n; p += gridDim.x) {
-        const int at = place[p];
-        float dot = 0.0f;
-        if (at >= 0 && at < n)
-            for (int d = threadIdx.x; d < width; d += 64) {
-                const float g = (float)dout[p / k * dout_stride + d];
-                dys[at * dys_stride + d] = rounded<T>(weight[p] * g);
-                dot = fmaf(g, (float)ys[at * ys_stride + d], dot);
+    const int used = *count;
+    for (int64_t t0 = (int64_t)blockIdx.x * kTeams; t0 < rows; t0 += (int64_t)gridDim.x * kTeams) {
+        const int64_t t = min(t0 + team, (int64_t)rows - 1);  // teams beyond the rows repeat the last one
+        for (int j0 = 0; j0 < k; j0 += J) {
+            int at[J];
+            float w[J], dot[J];
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int64_t p = t * k + min(j0 + j, k - 1);
+                at[j] = place[p];
+                w[j] = weight[p];
+                dot[j] = 0.0f;
             }
-        dot = wave_sum(dot);
-        if (threadIdx.x == 0) dweight[p] = dot;
-        if (p >= *count)
-            for (int d = threadIdx.x; d < width; d += 64) dys[p * dys_stride + d] = (T)0.0f;
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (j0 + j >= k || at[j] >= n) at[j] = -1;
+            for (int v0 = lane; v0 < vecs; v0 += U * L) {
+                int col[U], again[U];  // the vector's elements that count start at `again`: the others were in one before
+                Pack<T, V> g[U], y[U][J];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int vec = v0 + u * L;
+                    col[u] = min(vec * V, width - V);
+                    again[u] = vec < vecs ? vec * V - col[u] : V;
+                    g[u] = load_vec<V>(dout + t * dout_stride + col[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        if (at[j] >= 0) y[u][j] = load_vec<V>(ys + (int64_t)at[j] * ys_stride + col[u]);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        float d[V];
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            d[i] = w[j] * (float)g[u][i];
+                            const float x = fmaf((float)g[u][i], (float)y[u][j][i], dot[j]);
+                            dot[j] = i >= again[u] && at[j] >= 0 ? x : dot[j];
+                        }
+                        if (at[j] >= 0) store_vec<V, T>(dys + (int64_t)at[j] * dys_stride + col[u], rounded_vec<T, V>(d), past);
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int m = min(L, 64) / 2; m; m >>= 1) dot[j] += __shfl_xor(dot[j], m);
+            if constexpr (L > 64) {
+                static_assert(L == kRowThreads);
+                __syncthreads();
+                if (threadIdx.x % 64 == 0)
+                    for (int j = 0; j < J; ++j) sums[threadIdx.x / 64][j] = dot[j];
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < J; ++j) dot[j] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (lane == 0 && j0 + j < k) dweight[t * k + j0 + j] = dot[j];
+        }
+        for (int64_t p = max(t * k, (int64_t)used); p < (t + 1) * k; ++p)
+            for (int v = lane; v < vecs; v += L) store_vec<V, T>(dys + p * dys_stride + min(v * V, width - V), Pack<T, V>{}, past);
     }
 }
 
