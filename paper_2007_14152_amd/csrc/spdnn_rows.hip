@@ -122,6 +122,34 @@ Chunks chunks_of(int64_t n) {
     return {size, (int32_t)std::max<int64_t>(1, (n + size - 1) / size)};
 }
 
+// Work memory of the gradient of a table, and how many bits of the ids are sorted at a time.
+struct GradWork {
+    size_t keys[2], tokens[2], table, parts, bytes;
+    int passes, bits;
+    GradWork(int32_t vocab, int32_t width, int32_t n) : keys{}, tokens{}, table(0), parts(0), bytes(0), passes(0), bits(0) {
+        if (n <= spdnn::kFewIds) return;
+        int all = 0;  // bits of 0 .. vocab
+        while ((int64_t)vocab >> all) ++all;
+        passes = (all + 9) / 10;
+        bits = (all + passes - 1) / passes;
+        const auto take = [&](size_t size) {
+            const size_t at = bytes;
+            bytes += (size + kAlign - 1) / kAlign * kAlign;
+            return at;
+        };
+        for (int i = 0; i < 2; ++i) {
+            keys[i] = take(sizeof(uint32_t) * (size_t)n);
+            tokens[i] = take(sizeof(int32_t) * (size_t)n);
+        }
+        table = take(sizeof(int32_t) * ((size_t)1 << bits) * chunks_of(n).count);
+        parts = take(sizeof(float) * 2 * (size_t)width * ((size_t)(n - 1) / spdnn::kPiece + 1));
+    }
+};
+static_assert(spdnn::kMostBins >= 1 << 10 && spdnn::kMostBins >= 256);
+constexpr int64_t kClearBytes = 128 << 10;  // of a table that a workgroup clears at a time
+constexpr int kMostRowsEach = 256;          // rows of a table that a workgroup has with few ids
+constexpr int64_t kFewGroups = 2048;        // workgroups with few ids, if they have no more rows than that
+
 // f(V) with the elements of a vector: V, or 1 where a row has less.
 template <int V, typename F>
 void with_vec(int32_t width, F f) {
@@ -175,7 +203,7 @@ int spdnn_embed(const void* table, int32_t table_type, int32_t vocab, int32_t wi
 int spdnn_embed_grad_bytes(int32_t vocab, int32_t width, int32_t n, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
     if (vocab < 1 || width < 1 || n < 0) return fail(SPDNN_EINVAL, "need vocab >= 1, width >= 1, n >= 0");
-    *bytes = 0;
+    *bytes = GradWork(vocab, width, n).bytes;
     return SPDNN_OK;
 }
 
@@ -190,13 +218,81 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
     CHECK(check_array("ids", ids, n, ids_type == SPDNN_I32 ? 4 : 8));
     CHECK(check_work(work, work_bytes, need));
     const hipStream_t s = (hipStream_t)hip_stream;
+    if (n == 0 && accumulate) return SPDNN_OK;
+    const bool past = !accumulate && (int64_t)vocab * width * size_of(dtable_type) >= kPastBytes;
+    const int64_t row_bytes = (int64_t)width * size_of(dtable_type);
+    if (n <= spdnn::kFewIds) {
+        with_type(dout_type, [&](auto tt) {
+            with_type(dtable_type, [&](auto to) {
+                with_ids(ids_type, [&](auto ti) {
+                    using T = decltype(tt);
+                    using S = decltype(to);
+                    using I = decltype(ti);
+                    with_vec<16 / std::max(sizeof(T), sizeof(S))>(width, [&](auto v) {
+                        constexpr int V = decltype(v)::value;
+                        const int vecs = (width - 1) / V + 1;
+                        // a wave's width of columns each, so that many share the rows of a frequent id; eight workgroups per CU
+                        const int y = std::min((vecs - 1) / 64 + 1, 1024);
+                        const int per = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)vocab * y / kFewGroups, kMostRowsEach));
+                        const int64_t x = std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
+                        spdnn::embed_grad_few_kernel<T, S, I, V><<<dim3((unsigned)x, (unsigned)y), spdnn::kSortThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, per, (vecs - 1) / y + 1, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
+                    });
+                });
+            });
+        });
+        return launched();
+    }
+    // the ids sorted, a few of their bits at a time
+    const GradWork w(vocab, width, n);
+    char* const base = (char*)work;
+    const Chunks c = chunks_of(n);
+    int32_t* const table = (int32_t*)(base + w.table);
+    const uint32_t* keys = nullptr;
+    const int32_t* tokens = nullptr;
+    for (int pass = 0; pass < w.passes; ++pass) {
+        uint32_t* const to_keys = (uint32_t*)(base + w.keys[pass & 1]);
+        int32_t* const to_tokens = (int32_t*)(base + w.tokens[pass & 1]);
+        const int shift = pass * w.bits, mask = (1 << w.bits) - 1;
+        const auto sort = [&](auto in) {
+            spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, mask + 1, table);
+            spdnn::key_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, table, c.count, to_keys, to_tokens);
+        };
+        if (pass == 0)
+            with_ids(ids_type, [&](auto ti) {
+                using I = decltype(ti);
+                sort(spdnn::IdItems<I>{(const I*)ids, (uint32_t)vocab, shift, mask});
+            });
+        else
+            sort(spdnn::KeyItems{keys, tokens, shift, mask});
+        keys = to_keys;
+        tokens = to_tokens;
+    }
+    const spdnn::GradOrder order{keys, tokens, n, (uint32_t)vocab};
+    float* const parts = (float*)(base + w.parts);
+    const int64_t pieces = (n - 1) / spdnn::kPiece + 1;
     with_type(dout_type, [&](auto tt) {
         with_type(dtable_type, [&](auto to) {
-            with_ids(ids_type, [&](auto ti) {
-                using T = decltype(tt);
-                using S = decltype(to);
-                using I = decltype(ti);
-                spdnn::embed_grad_kernel<T, S, I><<<groups(vocab), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, scale, accumulate, (S*)dtable, dtable_stride);
+            using T = decltype(tt);
+            using S = decltype(to);
+            with_vec<16 / std::max(sizeof(T), sizeof(S))>(width, [&](auto v) {
+                constexpr int V = decltype(v)::value;
+                const int vecs = (width - 1) / V + 1;
+                const auto run = [&](auto l) {
+                    constexpr int L = decltype(l)::value;
+                    const int adders = (int)std::min<int64_t>((pieces - 1) / (spdnn::kRowThreads / L) + 1, kMostGroups);
+                    const int per = (int)std::min<int64_t>(std::max<int64_t>(kClearBytes / row_bytes, 1), spdnn::kRowThreads);
+                    const int clear = accumulate ? 0 : (int)std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
+                    const dim3 grid(adders + clear, std::min((vecs - 1) / L + 1, 1024));
+                    spdnn::embed_grad_kernel<T, S, V, L><<<grid, spdnn::kRowThreads, 0, s>>>(order, (const T*)dout, dout_stride, width, scale, accumulate != 0, (S*)dtable, dtable_stride, parts, adders, per, past);
+                };
+                if (vecs <= 16) run(std::integral_constant<int, 16>{});
+                else if (vecs <= 64) run(std::integral_constant<int, 64>{});
+                else run(std::integral_constant<int, 256>{});
+            });
+            with_vec<spdnn::kJoinVec>(width, [&](auto v) {
+                constexpr int V = decltype(v)::value;
+                const dim3 grid((unsigned)std::min(pieces, kMostGroups), (unsigned)std::min((width - 1) / (64 * V) + 1, 1024));
+                spdnn::embed_grad_join_kernel<S, V><<<grid, spdnn::kRowThreads, 0, s>>>(order, width, scale, accumulate != 0, (S*)dtable, dtable_stride, parts);
             });
         });
     });
@@ -255,12 +351,12 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
     CHECK(check_array("offsets", offsets, 1, 4));
     CHECK(check_work(work, work_bytes, need));
     const hipStream_t s = (hipStream_t)hip_stream;
-    const spdnn::PairDigits digit{chosen, experts};
+    const spdnn::PairItems in{chosen, experts};
     const bool few = n > 0 && n <= spdnn::kFewPairs;
     if (!few) {
         const Chunks c = chunks_of(n);
-        spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, experts, (int32_t*)work);
-        spdnn::expert_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(digit, n, c.size, (const int32_t*)work, c.count, offsets, place);
+        spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, experts, (int32_t*)work);
+        spdnn::expert_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, (const int32_t*)work, c.count, offsets, place);
     }
     if (n > 0)
         with_type(type, [&](auto tt) {
@@ -269,7 +365,7 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
                 constexpr int V = decltype(v)::value;
                 const spdnn::Tiles g = tiles(rows, width, V, spdnn::kDispatchVecs, (int64_t)n * width * sizeof(T));
                 if (few)
-                    spdnn::dispatch_few_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, digit, offsets, place, (T*)xs, xs_stride);
+                    spdnn::dispatch_few_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, in, offsets, place, (T*)xs, xs_stride);
                 else
                     spdnn::dispatch_rows_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, place, offsets + experts, (T*)xs, xs_stride);
             });

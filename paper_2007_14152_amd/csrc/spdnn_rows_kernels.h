@@ -136,28 +136,6 @@ __global__ __launch_bounds__(kRowThreads) void embed_kernel(Tiles g, const T* __
     });
 }
 
-// dtable[v] = [dtable[v] +] scale * sum of the dout[t] with ids[t] == v; a workgroup per v looks through all ids.
-template <typename T, typename S, typename I>
-__global__ __launch_bounds__(kRowThreads) void embed_grad_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
-                                                                 int vocab, int width, float scale, int accumulate, S* __restrict__ dtable,
-                                                                 int64_t dtable_stride) {
-    for (int64_t v = blockIdx.x; v < vocab; v += gridDim.x) {
-        for (int d0 = 0; d0 < width; d0 += kRowThreads) {
-            const int d = d0 + threadIdx.x;
-            float sum = 0.0f;
-            bool any = false;
-            for (int t = 0; t < n; ++t) {
-                if (ids[t] != (I)v) continue;
-                any = true;
-                if (d < width) sum += (float)dout[t * dout_stride + d];
-            }
-            if (d >= width || (accumulate && !any)) continue;
-            S& to = dtable[v * dtable_stride + d];
-            to = rounded<S>(accumulate ? fmaf(scale, sum, (float)to) : scale * sum);
-        }
-    }
-}
-
 // --- choice of experts ------------------------------------------------------
 
 // A number whose order as an integer is the order of r, -0 beside +0; 0 for what is not greater than minus infinity.
@@ -315,14 +293,13 @@ constexpr int kMostBins = 1024;
 constexpr int kMostChunks = 128;  // more pairs than these hold make the chunks longer
 constexpr int kLeastChunk = 1024;
 
-// The experts of pairs: -1 without one.
-struct PairDigits {
+// What is sorted: `at` loads a pair, `digit` is its number d (-1: it has no place).
+struct PairItems {
+    using Item = int32_t;
     const int32_t* chosen;
     int experts;
-    __device__ int operator()(int64_t p) const {
-        const int e = chosen[p];
-        return e >= 0 && e < experts ? e : -1;
-    }
+    __device__ Item at(int64_t p) const { return chosen[p]; }
+    __device__ int digit(Item e) const { return e >= 0 && e < experts ? e : -1; }
 };
 
 struct SortLds {
@@ -330,61 +307,87 @@ struct SortLds {
     int32_t total[kMostBins];
     int32_t wave_sum[kSortWaves];
 };
+constexpr int kSortAhead = 4;  // pairs that a lane has under way
 
 template <typename D>
-__global__ __launch_bounds__(kSortThreads) void count_kernel(D digit, int64_t n, int64_t chunk, int bins, int32_t* __restrict__ table) {
+__global__ __launch_bounds__(kSortThreads) void count_kernel(D in, int64_t n, int64_t chunk, int bins, int32_t* __restrict__ table) {
     __shared__ int32_t count[kMostBins];
     for (int e = threadIdx.x; e < bins; e += kSortThreads) count[e] = 0;
     __syncthreads();
     const int64_t first = blockIdx.x * chunk, last = min(first + chunk, n);
-    for (int64_t p = first + threadIdx.x; p < last; p += kSortThreads) {
-        const int d = digit(p);
-        if (d >= 0) atomicAdd(&count[d], 1);
+    for (int64_t p0 = first + threadIdx.x; p0 < last; p0 += kSortAhead * kSortThreads) {
+        typename D::Item x[kSortAhead];
+#pragma unroll
+        for (int a = 0; a < kSortAhead; ++a) x[a] = in.at(min(p0 + a * kSortThreads, last - 1));
+#pragma unroll
+        for (int a = 0; a < kSortAhead; ++a) {
+            const int d = in.digit(x[a]);
+            if (d >= 0 && p0 + a * kSortThreads < last) atomicAdd(&count[d], 1);
+        }
     }
     __syncthreads();
     for (int e = threadIdx.x; e < bins; e += kSortThreads) table[(int64_t)blockIdx.x * bins + e] = count[e];
 }
 
-// to(pair, position) for every pair of chunk `me`, position -1 without a digit; offsets (may be NULL): first positions of the
-// bins, and the end.  table: the counts of `chunks` chunks, or NULL if there is only this one.
+// to(pair, item, position) for every pair of chunk `me`, position -1 without a digit; offsets (may be NULL): first positions of
+// the bins, and the end.  table: the counts of `chunks` chunks, or NULL if there is only this one.
 template <typename D, typename F>
-__device__ inline void place_chunk(D digit, int64_t first, int64_t last, int bins, const int32_t* __restrict__ table, int chunks, int me,
+__device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, const int32_t* __restrict__ table, int chunks, int me,
                                    SortLds& lds, int32_t* __restrict__ offsets, F to) {
+    constexpr int A = kSortAhead;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t part = ((last - first + kSortThreads - 1) / kSortThreads) * 64;
     const int64_t mine = min(first + wave * part, last), end = min(mine + part, last);
+    typename D::Item x[A];  // the wave's pairs, A * 64 at a time; where there are no more, they are loaded once
+    const auto load = [&](int64_t p0) {
+#pragma unroll
+        for (int a = 0; a < A; ++a) x[a] = in.at(min(p0 + a * 64 + lane, end - 1));
+    };
+    if (mine < end) load(mine);
     for (int e = threadIdx.x; e < bins; e += kSortThreads)
         for (int w = 0; w < kSortWaves; ++w) lds.start[w][e] = 0;
     __syncthreads();
-    for (int64_t p = mine + lane; p < end; p += 64) {
-        const int d = digit(p);
-        if (d >= 0) atomicAdd(&lds.start[wave][d], 1);
+    for (int64_t p0 = mine; p0 < end; p0 += A * 64) {
+        if (p0 != mine) load(p0);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            const int d = in.digit(x[a]);
+            if (d >= 0 && p0 + a * 64 + lane < end) atomicAdd(&lds.start[wave][d], 1);
+        }
     }
     __syncthreads();
     // bin e's pairs in all chunks, and in start[0][e] .. start[3][e] where each wave's first one goes, within the bin
     for (int e = threadIdx.x; e < bins; e += kSortThreads) {
         int before = 0, total = 0;
-        for (int c = 0; table && c < chunks; ++c) {
-            const int x = table[(int64_t)c * bins + e];
-            total += x;
-            before += c < me ? x : 0;
+        if (table) {
+            constexpr int B = 16;
+            for (int c0 = 0; c0 < chunks; c0 += B) {
+                int y[B];
+#pragma unroll
+                for (int c = 0; c < B; ++c) y[c] = table[(int64_t)min(c0 + c, chunks - 1) * bins + e];
+#pragma unroll
+                for (int c = 0; c < B; ++c) {
+                    total += c0 + c < chunks ? y[c] : 0;
+                    before += c0 + c < me ? y[c] : 0;
+                }
+            }
         }
         for (int w = 0; w < kSortWaves; ++w) {
-            const int x = lds.start[w][e];
+            const int y = lds.start[w][e];
             lds.start[w][e] = before;
-            before += x;
+            before += y;
         }
         lds.total[e] = table ? total : before;
     }
     __syncthreads();
     // a thread's bins next to each other: their sum, the sums before it, then each bin's first position
     constexpr int kEach = kMostBins / kSortThreads;
-    int x[kEach], sum = 0;
+    int many[kEach], sum = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int e = threadIdx.x * kEach + i;
-        x[i] = e < bins ? lds.total[e] : 0;
-        sum += x[i];
+        many[i] = e < bins ? lds.total[e] : 0;
+        sum += many[i];
     }
     int upto = sum;
     for (int m = 1; m < 64; m <<= 1) {
@@ -401,36 +404,316 @@ __device__ inline void place_chunk(D digit, int64_t first, int64_t last, int bin
         if (e < bins) {
             if (offsets) offsets[e] = base;
             for (int w = 0; w < kSortWaves; ++w) lds.start[w][e] += base;
-            base += x[i];
+            base += many[i];
             if (offsets && e == bins - 1) offsets[bins] = base;
         }
     }
     __syncthreads();
     const int bits = 32 - __clz(bins - 1 | 1);
     volatile int32_t* start = lds.start[wave];  // read and written by this wave alone, in the order written here
-    for (int64_t p0 = mine; p0 < end; p0 += 64) {
-        const int64_t p = p0 + lane;
-        const int d = p < end ? digit(p) : -1;
-        uint64_t same = __ballot(d >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot(d >> b & 1);
-            same &= d >> b & 1 ? set : ~set;
+    for (int64_t p0 = mine; p0 < end; p0 += A * 64) {
+        if (end - mine > A * 64) load(p0);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            const int64_t p = p0 + a * 64 + lane;
+            const int d = p < end ? in.digit(x[a]) : -1;
+            uint64_t same = __ballot(d >= 0);
+            for (int b = 0; b < bits; ++b) {
+                const uint64_t set = __ballot(d >> b & 1);
+                same &= d >> b & 1 ? set : ~set;
+            }
+            int at = -1;
+            if (d >= 0) {
+                at = start[d] + __popcll(same & ((1ull << lane) - 1));
+                if (lane == 63 - __clzll(same)) start[d] = at + 1;  // the last of its kind leaves where the next one goes
+            }
+            if (p < end) to(p, x[a], at);
         }
-        int at = -1;
-        if (d >= 0) {
-            at = start[d] + __popcll(same & ((1ull << lane) - 1));
-            if (lane == 63 - __clzll(same)) start[d] = at + 1;  // the last of its kind leaves where the next one goes
-        }
-        if (p < end) to(p, at);
     }
 }
 
-__global__ __launch_bounds__(kSortThreads) void expert_place_kernel(PairDigits digit, int64_t n, int64_t chunk, const int32_t* __restrict__ table,
+__global__ __launch_bounds__(kSortThreads) void expert_place_kernel(PairItems in, int64_t n, int64_t chunk, const int32_t* __restrict__ table,
                                                                     int chunks, int32_t* __restrict__ offsets, int32_t* __restrict__ place) {
     __shared__ SortLds lds;
     const int64_t first = blockIdx.x * chunk;
-    place_chunk(digit, first, min(first + chunk, n), digit.experts, table, chunks, blockIdx.x, lds, blockIdx.x == 0 ? offsets : nullptr,
-                [&](int64_t p, int at) { place[p] = at; });
+    place_chunk(in, first, min(first + chunk, n), in.experts, table, chunks, blockIdx.x, lds, blockIdx.x == 0 ? offsets : nullptr,
+                [&](int64_t p, int32_t, int at) { place[p] = at; });
+}
+
+// --- gradient of a table ----------------------------------------------------
+
+// Ids of tokens with the tokens they belong to, `vocab` for those outside the table, sorted by a digit of their bits at a time: from
+// the caller's ids, or from what an earlier digit has sorted.
+struct Token {
+    uint32_t key;
+    int32_t token;
+};
+template <typename I>
+struct IdItems {
+    using Item = Token;
+    const I* ids;
+    uint32_t vocab;
+    int shift, mask;
+    __device__ Item at(int64_t p) const {
+        const I id = ids[p];
+        return {id >= 0 && id < (I)vocab ? (uint32_t)id : vocab, (int32_t)p};
+    }
+    __device__ int digit(Item x) const { return (int)(x.key >> shift) & mask; }
+};
+struct KeyItems {
+    using Item = Token;
+    const uint32_t* keys;
+    const int32_t* tokens;
+    int shift, mask;
+    __device__ Item at(int64_t p) const { return {keys[p], tokens[p]}; }
+    __device__ int digit(Item x) const { return (int)(x.key >> shift) & mask; }
+};
+
+// Sorted by one more digit.
+template <typename D>
+__global__ __launch_bounds__(kSortThreads) void key_place_kernel(D in, int64_t n, int64_t chunk, const int32_t* __restrict__ table, int chunks,
+                                                                 uint32_t* __restrict__ keys, int32_t* __restrict__ tokens) {
+    __shared__ SortLds lds;
+    const int64_t first = blockIdx.x * chunk;
+    place_chunk(in, first, min(first + chunk, n), in.mask + 1, table, chunks, blockIdx.x, lds, nullptr, [&](int64_t, Token x, int at) {
+        keys[at] = x.key;
+        tokens[at] = x.token;
+    });
+}
+
+// V elements of a row of the gradient from the sums of dout; the first `again` of them are left to the vector before this one.
+template <typename S, int V>
+__device__ inline void put_grad(S* __restrict__ to, int again, const float (&sum)[V], float scale, bool accumulate, bool past) {
+    float x[V];
+    Pack<S, V> old = {};
+    if (accumulate) old = load_vec<V>(to);
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = fmaf(scale, sum[i], (float)old[i]);
+    const Pack<S, V> y = rounded_vec<S, V>(x);
+    if (again == 0) {
+        store_vec<V, S>(to, y, past);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= again) to[i] = y[i];
+    }
+}
+
+// The sum of dout's rows tokens[first] .. tokens[last - 1], columns from col on, in that order, kAhead of them under way.
+constexpr int kAhead = 8;
+template <int V, typename T, typename F>
+__device__ inline void add_rows(const T* __restrict__ dout, int64_t dout_stride, int col, int first, int last, F token, float (&sum)[V]) {
+    for (int i0 = first; i0 < last; i0 += kAhead) {
+        Pack<T, V> x[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) x[a] = load_vec<V>(dout + (int64_t)token(min(i0 + a, last - 1)) * dout_stride + col);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] = i0 + a < last ? sum[i] + (float)x[a][i] : sum[i];
+    }
+}
+
+// The ids that fall into rows v0 .. v0 + rows - 1 of the table.
+template <typename I>
+struct RowItems {
+    using Item = int32_t;  // the row from v0 on, -1 outside
+    const I* ids;
+    I v0;
+    int rows;
+    __device__ Item at(int64_t p) const {
+        const I id = ids[p];
+        return id >= v0 && id < v0 + rows ? (int)(id - v0) : -1;
+    }
+    __device__ int digit(Item r) const { return r; }
+};
+
+// Few ids, one launch: a workgroup has `per` rows of the table (at most kMostBins) and `slab` of their vectors, sorts the ids that
+// fall there and adds up or clears a row after the other.
+constexpr int kFewIds = 1024;
+template <typename T, typename S, typename I, int V>
+__global__ __launch_bounds__(kSortThreads) void embed_grad_few_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
+                                                                      int vocab, int width, int per, int slab, float scale, bool accumulate,
+                                                                      S* __restrict__ dtable, int64_t dtable_stride, bool past) {
+    __shared__ SortLds lds;
+    __shared__ int32_t tokens[kFewIds], offsets[kMostBins + 1];
+    const int vecs = (width - 1) / V + 1, vec0 = blockIdx.y * slab, here = min(slab, vecs - vec0);
+    for (int64_t v0 = (int64_t)blockIdx.x * per; v0 < vocab; v0 += (int64_t)gridDim.x * per) {
+        const int rows = (int)min((int64_t)per, vocab - v0);
+        __syncthreads();  // the table's rows before these are done with what is sorted
+        place_chunk(RowItems<I>{ids, (I)v0, rows}, 0, n, rows, nullptr, 1, 0, lds, offsets, [&](int64_t p, int32_t, int at) {
+            if (at >= 0) tokens[at] = (int32_t)p;
+        });
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * here; i += kSortThreads) {
+            const int r = i / here, vec = vec0 + i - r * here, col = min(vec * V, width - V);
+            const int first = offsets[r], last = offsets[r + 1];
+            if (accumulate && first == last) continue;
+            float sum[V] = {};
+            add_rows<V>(dout, dout_stride, col, first, last, [&](int a) { return tokens[a]; }, sum);
+            put_grad<S, V>(dtable + (v0 + r) * dtable_stride + col, vec * V - col, sum, first < last ? scale : 0.0f, accumulate, past);
+        }
+    }
+}
+
+// Many ids, sorted: the order is cut into pieces of kPiece places, and a team of L lanes adds up a piece, L * V columns of it.
+// Where an id's places lie in one piece, its row is done.  Otherwise the piece's part of the sum goes to the work memory, and
+// embed_grad_join_kernel adds the parts up: long runs of a frequent id are shared out, and no atomics decide an order.
+// parts: two rows of `width` floats per piece: for the id that comes in from the piece before, and for the one that goes on.
+constexpr int kPiece = 32;
+struct GradOrder {
+    const uint32_t* keys;
+    const int32_t* tokens;
+    int32_t n;
+    uint32_t vocab;
+    // the first place whose key is not less than v
+    __device__ int lower(uint32_t v) const {
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int mid = lo + (hi - lo) / 2;
+            if (keys[mid] < v) lo = mid + 1;
+            else hi = mid;
+        }
+        return lo;
+    }
+};
+
+template <typename T, typename S, int V, int L>
+__device__ inline void add_pieces(const GradOrder& o, const T* __restrict__ dout, int64_t dout_stride, int width, float scale, bool accumulate,
+                                  S* __restrict__ dtable, int64_t dtable_stride, float* __restrict__ parts, int group, int groups) {
+    constexpr int kTeams = kRowThreads / L;
+    __shared__ uint32_t keys[kTeams][kPiece + 2];  // from the place before the piece to the one behind it; vocab where there is none
+    __shared__ int32_t tokens[kTeams][kPiece];
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int vecs = (width - 1) / V + 1;
+    const int pieces = (o.n - 1) / kPiece + 1;
+    for (int64_t piece0 = (int64_t)group * kTeams; piece0 < pieces; piece0 += (int64_t)groups * kTeams) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kTeams * (kPiece + 2); i += kRowThreads) {
+            const int in = i % (kPiece + 2);
+            const int64_t at = (piece0 + i / (kPiece + 2)) * kPiece + in - 1;
+            keys[i / (kPiece + 2)][in] = at >= 0 && at < o.n ? o.keys[at] : o.vocab;
+            if (in >= 1 && in <= kPiece) tokens[i / (kPiece + 2)][in - 1] = at < o.n ? o.tokens[at] : 0;
+        }
+        __syncthreads();
+        const uint32_t* key = keys[team] + 1;
+        int many = 0;  // of the piece's places have an id: the others are the last of all
+        for (int a = 0; a < kPiece; ++a) many += key[a] < o.vocab;
+        const int64_t piece = piece0 + team;
+        for (int vec = blockIdx.y * L + lane; vec < vecs && many > 0; vec += gridDim.y * L) {
+            const int col = min(vec * V, width - V), again = vec * V - col;
+            float sum[V] = {};
+            bool in = key[-1] == key[0];  // the run at hand began in the piece before
+            for (int a0 = 0; a0 < many; a0 += kAhead) {
+                Pack<T, V> x[kAhead];
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) x[a] = load_vec<V>(dout + (int64_t)tokens[team][min(a0 + a, many - 1)] * dout_stride + col);
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) {
+                    if (a0 + a >= many) break;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[i] += (float)x[a][i];
+                    const uint32_t v = key[a0 + a];
+                    const bool on = v == key[a0 + a + 1];
+                    if (on && a0 + a + 1 < kPiece) continue;
+                    if (!in && !on) {
+                        put_grad<S, V>(dtable + (int64_t)v * dtable_stride + col, again, sum, scale, accumulate, false);
+                    } else {
+                        float* to = parts + (piece * 2 + (in ? 0 : 1)) * width + col;
+                        store_vec<V, float>(to, rounded_vec<float, V>(sum), false);
+                    }
+                    in = false;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+                }
+            }
+        }
+    }
+}
+
+// Zeros in rows of ids that do not occur.
+template <typename S, int V>
+__device__ inline void clear_rows(const GradOrder& o, int width, int per, S* __restrict__ dtable, int64_t dtable_stride, bool past, int group, int groups) {
+    __shared__ bool there[kRowThreads];
+    const int vecs = (width - 1) / V + 1;
+    for (int64_t v0 = (int64_t)group * per; v0 < o.vocab; v0 += (int64_t)groups * per) {
+        const int rows = (int)min((int64_t)per, (int64_t)o.vocab - v0);
+        __syncthreads();
+        if ((int)threadIdx.x < rows) {
+            const int at = o.lower((uint32_t)v0 + threadIdx.x);
+            there[threadIdx.x] = at < o.n && o.keys[at] == (uint32_t)v0 + threadIdx.x;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * vecs; i += kRowThreads) {
+            const int r = i / vecs, vec = i - r * vecs;
+            if (!there[r]) store_vec<V, S>(dtable + (v0 + r) * dtable_stride + min(vec * V, width - V), Pack<S, V>{}, past);
+        }
+    }
+}
+
+// The first `adders` workgroups add pieces, the others (none if accumulate) clear rows, `per` at a time.
+template <typename T, typename S, int V, int L>
+__global__ __launch_bounds__(kRowThreads) void embed_grad_kernel(GradOrder o, const T* __restrict__ dout, int64_t dout_stride, int width, float scale,
+                                                                 bool accumulate, S* __restrict__ dtable, int64_t dtable_stride,
+                                                                 float* __restrict__ parts, int adders, int per, bool past) {
+    if ((int)blockIdx.x < adders)
+        add_pieces<T, S, V, L>(o, dout, dout_stride, width, scale, accumulate, dtable, dtable_stride, parts, blockIdx.x, adders);
+    else if (blockIdx.y == 0)
+        clear_rows<S, V>(o, width, per, dtable, dtable_stride, past, blockIdx.x - adders, gridDim.x - adders);
+}
+
+// The rows of ids whose places lie in more than one piece: a workgroup per piece and 64 vectors of columns, which has work if such a
+// run begins there.  Its waves take a quarter of the run's parts each, the quarters are added in order.
+constexpr int kJoinVec = 4;
+template <typename S, int V>
+__global__ __launch_bounds__(kRowThreads) void embed_grad_join_kernel(GradOrder o, int width, float scale, bool accumulate, S* __restrict__ dtable,
+                                                                      int64_t dtable_stride, const float* __restrict__ parts) {
+    constexpr int kWaves = kRowThreads / 64;
+    __shared__ float sums[kWaves][64][V];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int vecs = (width - 1) / V + 1;
+    const int pieces = (o.n - 1) / kPiece + 1;
+    for (int64_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const int64_t first = piece * kPiece, end = min(first + kPiece, (int64_t)o.n);
+        const uint32_t v = o.keys[end - 1], next = o.keys[min(end, (int64_t)o.n - 1)], head = o.keys[first], before = o.keys[max(first - 1, (int64_t)0)];
+        if (end == o.n || next != v || v >= o.vocab || (head == v && first > 0 && before == v)) continue;
+        int64_t last = piece + 1;  // the run's last piece: the first one that does not end with v and go on so
+        for (;; last += 64) {
+            const int64_t e = min((last + lane + 1) * kPiece, (int64_t)o.n);
+            const uint64_t stops = __ballot(e == o.n || o.keys[e - 1] != v || o.keys[e] != v);
+            if (stops) {
+                last += __ffsll((unsigned long long)stops) - 1;
+                break;
+            }
+        }
+        const int many = (int)(last - piece) + 1, each = (many + kWaves - 1) / kWaves;
+        for (int v0 = blockIdx.y * 64; v0 < vecs; v0 += gridDim.y * 64) {
+            const int vec = min(v0 + lane, vecs - 1), col = min(vec * V, width - V);
+            float sum[V] = {};
+            const int from = min(wave * each, many), to = min(from + each, many);
+            for (int i0 = from; i0 < to; i0 += kAhead) {
+                Pack<float, V> x[kAhead];
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) {
+                    const int i = min(i0 + a, to - 1);
+                    x[a] = load_vec<V>(parts + ((piece + i) * 2 + (i == 0 ? 1 : 0)) * width + col);
+                }
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[i] = i0 + a < to ? sum[i] + x[a][i] : sum[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) sums[wave][lane][i] = sum[i];
+            __syncthreads();
+            if (wave == 0 && v0 + lane < vecs) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] = (sum[i] + sums[1][lane][i]) + (sums[2][lane][i] + sums[3][lane][i]);
+                put_grad<S, V>(dtable + (int64_t)v * dtable_stride + col, vec * V - col, sum, scale, accumulate, false);
+            }
+        }
+    }
 }
 
 // J of a row's places at a time, -1 where there is none: all of them before the first load or store that needs one, for a wait
@@ -484,7 +767,7 @@ __global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(Tiles g, con
 // Few pairs: every workgroup sorts all of them for itself and moves its tile of rows, one launch in all.
 constexpr int kFewPairs = 1024;
 template <typename T, int V>
-__global__ __launch_bounds__(kRowThreads) void dispatch_few_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k, PairDigits digit,
+__global__ __launch_bounds__(kRowThreads) void dispatch_few_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k, PairItems in,
                                                                    int32_t* __restrict__ offsets, int32_t* __restrict__ place, T* __restrict__ xs,
                                                                    int64_t xs_stride) {
     static_assert(kRowThreads == kSortThreads);
@@ -493,7 +776,7 @@ __global__ __launch_bounds__(kRowThreads) void dispatch_few_kernel(Tiles g, cons
     __shared__ int32_t used;
     const bool first = blockIdx.x == 0 && blockIdx.y == 0;
     if (threadIdx.x == 0) used = 0;
-    place_chunk(digit, 0, g.rows * k, digit.experts, nullptr, 1, 0, lds, first ? offsets : nullptr, [&](int64_t p, int at) {
+    place_chunk(in, 0, g.rows * k, in.experts, nullptr, 1, 0, lds, first ? offsets : nullptr, [&](int64_t p, int32_t, int at) {
         places[p] = at;
         if (at >= 0) atomicMax(&used, at + 1);
         if (first) place[p] = at;
