@@ -165,6 +165,25 @@ void with_places(int32_t k, F f) {
     else f(std::integral_constant<int, 4>{});
 }
 
+constexpr int32_t kFewRows = 1024;
+
+// f(K), k rounded up to a power of two.
+template <typename F>
+void with_chosen(int32_t k, F f) {
+    if (k == 1) f(std::integral_constant<int, 1>{});
+    else if (k == 2) f(std::integral_constant<int, 2>{});
+    else if (k <= 4) f(std::integral_constant<int, 4>{});
+    else if (k <= 8) f(std::integral_constant<int, 8>{});
+    else f(std::integral_constant<int, 16>{});
+}
+
+// f(G) with the lanes that take a row of logits: G0, or a wave where there are few rows.
+template <int G0, typename F>
+void with_team(int32_t rows, F f) {
+    if (rows > kFewRows) f(std::integral_constant<int, G0>{});
+    else f(std::integral_constant<int, 64>{});
+}
+
 int launched() {
     HIP_TRY(hipGetLastError());
     return SPDNN_OK;
@@ -309,7 +328,13 @@ int spdnn_route(const void* logits, int32_t type, int64_t stride, int32_t rows, 
     if (rows == 0) return SPDNN_OK;
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
-        spdnn::route_kernel<T><<<groups(rows), 64, 0, (hipStream_t)hip_stream>>>((const T*)logits, stride, rows, experts, k, bias, keep, score, normalise, scale, chosen, weight);
+        with_chosen(k, [&](auto kk) {
+            constexpr int K = decltype(kk)::value;
+            with_team<(K > 8 ? K : 8)>(rows, [&](auto gg) {
+                constexpr int G = decltype(gg)::value;
+                spdnn::route_kernel<T, K, G><<<groups((rows - 1) / (spdnn::kRowThreads / G) + 1), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>((const T*)logits, stride, rows, experts, k, bias, keep, score, normalise, scale, chosen, weight);
+            });
+        });
     });
     return launched();
 }
@@ -325,7 +350,10 @@ int spdnn_route_grad(const float* dweight, const void* logits, int32_t type, int
     if (rows == 0) return SPDNN_OK;
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
-        spdnn::route_grad_kernel<T><<<groups(rows), 64, 0, (hipStream_t)hip_stream>>>(dweight, (const T*)logits, stride, chosen, rows, experts, k, bias, score, normalise, scale, (T*)dlogits, dstride);
+        with_team<SPDNN_MAX_CHOSEN>(rows, [&](auto gg) {
+            constexpr int G = decltype(gg)::value;
+            spdnn::route_grad_kernel<T, G><<<groups((rows - 1) / (spdnn::kRowThreads / G) + 1), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>(dweight, (const T*)logits, stride, chosen, rows, experts, k, bias, score, normalise, scale, (T*)dlogits, dstride);
+        });
     });
     return launched();
 }

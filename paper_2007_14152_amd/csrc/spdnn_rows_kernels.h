@@ -138,146 +138,270 @@ __global__ __launch_bounds__(kRowThreads) void embed_kernel(Tiles g, const T* __
 
 // --- choice of experts ------------------------------------------------------
 
-// A number whose order as an integer is the order of r, -0 beside +0; 0 for what is not greater than minus infinity.
-__device__ inline uint32_t rank_of(float r) {
-    if (!(r > -INFINITY)) return 0;
-    const uint32_t b = __float_as_uint(r + 0.0f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+// x of another lane, in steps that together reach all G lanes of a team: 1, 2 (the lane's number with that bit turned), 4 and 8
+// (mirrored within 8 and 16 lanes: another four, another eight), 16 and 32.
+template <int STEP>
+__device__ inline int other(int x) {
+    if constexpr (STEP == 1) return __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true);
+    else if constexpr (STEP == 2) return __builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true);
+    else if constexpr (STEP == 4) return __builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true);
+    else if constexpr (STEP == 8) return __builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true);
+    else return __shfl_xor(x, STEP);
+}
+template <int STEP>
+__device__ inline float other(float x) {
+    return __int_as_float(other<STEP>(__float_as_int(x)));
+}
+template <int STEP>
+__device__ inline double other(double x) {
+    return __hiloint2double(other<STEP>(__double2hiint(x)), other<STEP>(__double2loint(x)));
+}
+// f(x, y) over a team's lanes, the same in all of them.
+template <int G, int STEP = 1, typename T, typename F>
+__device__ inline T team_reduce(T x, F f) {
+    if constexpr (STEP < G) return team_reduce<G, 2 * STEP>(f(x, other<STEP>(x)), f);
+    else return x;
+}
+template <int G>
+__device__ inline float team_sum(float x) {
+    return team_reduce<G>(x, [](float a, float b) { return a + b; });
+}
+template <int G>
+__device__ inline float team_max(float x) {
+    return team_reduce<G>(x, [](float a, float b) { return fmaxf(a, b); });
 }
 
-__device__ inline float wave_sum(float x) {
-    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
-    return x;
+// A logit (with bias) and its column as one number whose order is that of the choice: the larger logit first, then the lower
+// column.  It is the logit in 64 bits, of which a 32-bit float leaves the last 29 free: the column goes there, turned round
+// where a larger last part makes a larger number.  +inf becomes a finite number beyond all floats, -0 becomes 0, and what is
+// not open is the smallest number.
+constexpr uint32_t kColumnBits = 0x3ff;
+static_assert(SPDNN_MAX_EXPERTS <= kColumnBits + 1);
+__device__ inline double closed() { return -1.7976931348623157e308; }
+__device__ inline double rank_of(float r, int col) {
+    double d = (double)(r + 0.0f);
+    if (r == INFINITY) d = 0x1p1000;
+    const uint32_t last = (uint32_t)col ^ (d >= 0.0 ? kColumnBits : 0u);
+    d = __hiloint2double(__double2hiint(d), __double2loint(d) | (int)last);
+    return r > -INFINITY ? d : closed();
 }
-__device__ inline float wave_max(float x) {
-    for (int m = 32; m; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
-    return x;
+__device__ inline int column_of(double d) {  // -1: none
+    if (d == closed()) return -1;
+    return (int)(((uint32_t)__double2loint(d) & kColumnBits) ^ (__double2hiint(d) >= 0 ? kColumnBits : 0u));
+}
+
+// Networks of compare-exchanges: K numbers in descending order, K a power of two.
+__device__ inline void order_two(double& a, double& b) {
+    const double x = fmax(a, b), y = fmin(a, b);
+    a = x;
+    b = y;
+}
+template <int K>
+__device__ inline void order_bitonic(double (&a)[K]) {  // a rises, then falls, or the other way round
+#pragma unroll
+    for (int m = K / 2; m; m /= 2)
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (!(i & m)) order_two(a[i], a[i | m]);
+}
+template <int K>
+__device__ inline void order_all(double (&a)[K]) {
+#pragma unroll
+    for (int n = 2; n <= K; n *= 2)
+#pragma unroll
+        for (int m = n / 2; m; m /= 2)
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                if (i & m) continue;
+                if (i & n) order_two(a[i | m], a[i]);
+                else order_two(a[i], a[i | m]);
+            }
+}
+// The first K of a and b, both in order.
+template <int K>
+__device__ inline void keep_first(double (&a)[K], const double (&b)[K]) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) a[i] = fmax(a[i], b[K - 1 - i]);
+    order_bitonic(a);
+}
+template <int G, int K, int STEP = 1>
+__device__ inline void keep_first_of_team(double (&a)[K]) {
+    if constexpr (STEP < G) {
+        double b[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) b[i] = other<STEP>(a[i]);
+        keep_first(a, b);
+        keep_first_of_team<G, K, 2 * STEP>(a);
+    }
 }
 
 __device__ inline float log_sigmoid(float x) { return fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); }
-
 __device__ inline float sigmoid(float x) {  // no overflow on the way: small values stay apart from zero
     const float e = expf(-fabsf(x)), r = 1.0f / (1.0f + e);
     return x >= 0.0f ? r : e * r;
 }
 
-// Weights of the chosen experts before the scale: lane j < k has the logit of slot j, valid says whether the slot has an expert.
-// Softmax over the open experts: top and total are the largest of their logits and the sum of exp(logit - top).
+// Weights of the chosen experts before the scale: lane j < k of a team has the logit of slot j, valid says whether the slot has
+// an expert.  Softmax over the open experts: top and total are the largest of their logits and the sum of exp(logit - top).
+template <int G>
 __device__ inline float slot_weight(float l, bool valid, int score, int normalise, float top, float total) {
     if (normalise) {
         const float x = score == SPDNN_SIGMOID ? log_sigmoid(l) : l;
-        const float m = wave_max(valid ? x : -INFINITY);
+        const float m = team_max<G>(valid ? x : -INFINITY);
         const float e = valid ? expf(x - m) : 0.0f;
-        const float sum = wave_sum(e);
+        const float sum = team_sum<G>(e);
         return valid ? e / sum : 0.0f;
     }
     if (!valid) return 0.0f;
     return score == SPDNN_SIGMOID ? sigmoid(l) : expf(l - top) / total;
 }
 
-constexpr int kLaneExperts = SPDNN_MAX_EXPERTS / 64;
+// V logits of a row from column col on, minus infinity beyond its end.
+template <int V, typename T>
+__device__ inline void load_logits(const T* __restrict__ row, int col, int experts, float (&l)[V]) {
+    if (col + V <= experts) {
+        const Pack<T, V> x = load_vec<V>(row + col);
+#pragma unroll
+        for (int i = 0; i < V; ++i) l[i] = (float)x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) l[i] = col + i < experts ? (float)row[col + i] : -INFINITY;
+    }
+}
+template <int V>
+__device__ inline void load_bias(const float* __restrict__ bias, int col, int experts, float (&b)[V]) {
+    if (bias) load_logits(bias, col, experts, b);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (!bias || col + i >= experts) b[i] = 0.0f;
+}
 
-// A wave per row; the lanes hold the row's logits, k rounds take the largest that is left.
-template <typename T>
-__global__ __launch_bounds__(64) void route_kernel(const T* __restrict__ logits, int64_t stride, int rows, int experts, int k,
-                                                   const float* __restrict__ bias, const uint8_t* __restrict__ keep, int score, int normalise,
-                                                   float scale, int32_t* __restrict__ chosen, float* __restrict__ weight) {
-    const int lane = threadIdx.x;
-    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x) {
-        uint32_t rank[kLaneExperts];
+// A team of G lanes takes a row, kLogits columns a lane at a time.  Every lane keeps the first K of its columns in order (K: k
+// rounded up), the lanes' lists are merged pairwise, and lane j weighs slot j.  No round per expert, no branch on values.
+constexpr int kLogits = 8;
+template <typename T, int K, int G>
+__global__ __launch_bounds__(kRowThreads) void route_kernel(const T* __restrict__ logits, int64_t stride, int rows, int experts, int k,
+                                                            const float* __restrict__ bias, const uint8_t* __restrict__ keep, int score, int normalise,
+                                                            float scale, int32_t* __restrict__ chosen, float* __restrict__ weight) {
+    static_assert(K <= G);
+    constexpr int V = K > kLogits ? K : kLogits, kTeams = kRowThreads / G;
+    const int lane = threadIdx.x % G, team = threadIdx.x / G;
+    const bool all = score == SPDNN_SOFTMAX && !normalise;  // the weights need all open experts
+    for (int64_t t0 = (int64_t)blockIdx.x * kTeams; t0 < rows; t0 += (int64_t)gridDim.x * kTeams) {
+        const int64_t t = min(t0 + team, (int64_t)rows - 1);  // teams beyond the rows repeat the last one
+        const T* row = logits + t * stride;
+        const int columns = !keep || keep[t] ? experts : 0;
+        double first[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) first[i] = closed();
         float top = -INFINITY, total = 0.0f;
-        const bool kept = !keep || keep[t];
-        for (int i = 0; i < kLaneExperts; ++i) {
-            const int e = i * 64 + lane;
-            rank[i] = 0;
-            if (!kept || e >= experts) continue;
-            const float l = (float)logits[t * stride + e];
-            rank[i] = rank_of(bias ? l + bias[e] : l);
-            if (rank[i]) top = fmaxf(top, l);
-        }
-        if (score == SPDNN_SOFTMAX && !normalise) {
-            top = wave_max(top);
-            for (int i = 0; i < kLaneExperts; ++i)
-                if (rank[i]) total += expf((float)logits[t * stride + i * 64 + lane] - top);
-            total = wave_sum(total);
-        }
-        int mine = -1;  // lane j: the expert of slot j
-        for (int j = 0; j < k; ++j) {
-            uint64_t best = 0;
-            for (int i = 0; i < kLaneExperts; ++i) {
-                const uint64_t c = (uint64_t)rank[i] << 32 | (uint32_t)~(i * 64 + lane);
-                if (rank[i] && c > best) best = c;
+        for (int col = lane * V; col < columns; col += G * V) {
+            float l[V], b[V];
+            load_logits<V>(row, col, experts, l);
+            load_bias<V>(bias, col, experts, b);
+#pragma unroll
+            for (int c = 0; c < V; c += K) {
+                double some[K];
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    const float r = l[c + i] + b[c + i];
+                    some[i] = rank_of(r, col + c + i);
+                    if (r > -INFINITY) top = fmaxf(top, l[c + i]);
+                }
+                order_all(some);
+                keep_first(first, some);
             }
-            for (int m = 32; m; m >>= 1) {
-                const uint64_t o = __shfl_xor((unsigned long long)best, m);
-                best = o > best ? o : best;
-            }
-            if (!best) break;
-            const int e = (int)~(uint32_t)best;
-            if (lane == j) mine = e;
-            for (int i = 0; i < kLaneExperts; ++i)
-                if (i * 64 + lane == e) rank[i] = 0;
         }
-        const float l = mine >= 0 ? (float)logits[t * stride + mine] : 0.0f;
-        const float w = slot_weight(l, mine >= 0, score, normalise, top, total);
+        keep_first_of_team<G>(first);
+        if (all) {
+            top = team_max<G>(top);
+            for (int col = lane * V; col < columns; col += G * V) {
+                float l[V], b[V];
+                load_logits<V>(row, col, experts, l);
+                load_bias<V>(bias, col, experts, b);
+#pragma unroll
+                for (int i = 0; i < V; ++i) total += l[i] + b[i] > -INFINITY ? expf(l[i] - top) : 0.0f;
+            }
+            total = team_sum<G>(total);
+        }
+        double mine = closed();
+#pragma unroll
+        for (int i = 0; i < K; ++i) mine = lane == i && i < k ? first[i] : mine;
+        const int e = column_of(mine);
+        const float l = e >= 0 ? (float)row[e] : 0.0f;
+        const float w = slot_weight<G>(l, e >= 0, score, normalise, top, total);
         if (lane < k) {
-            chosen[t * k + lane] = mine;
+            chosen[t * k + lane] = e;
             weight[t * k + lane] = scale * w;
         }
     }
 }
 
-// A wave per row.
-template <typename T>
-__global__ __launch_bounds__(64) void route_grad_kernel(const float* __restrict__ dweight, const T* __restrict__ logits, int64_t stride,
-                                                        const int32_t* __restrict__ chosen, int rows, int experts, int k,
-                                                        const float* __restrict__ bias, int score, int normalise, float scale,
-                                                        T* __restrict__ dlogits, int64_t dstride) {
-    const int lane = threadIdx.x;
-    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x) {
-        int mine = lane < k ? chosen[t * k + lane] : -1;
-        const bool valid = mine >= 0 && mine < experts;
-        const float l = valid ? (float)logits[t * stride + mine] : 0.0f;
+// A team of G lanes takes a row: the slots' weights and their gradient, then all of the row but for the chosen experts, then those.
+constexpr int kGradLogits = 4;
+template <typename T, int G>
+__global__ __launch_bounds__(kRowThreads) void route_grad_kernel(const float* __restrict__ dweight, const T* __restrict__ logits, int64_t stride,
+                                                                 const int32_t* __restrict__ chosen, int rows, int experts, int k,
+                                                                 const float* __restrict__ bias, int score, int normalise, float scale,
+                                                                 T* __restrict__ dlogits, int64_t dstride) {
+    static_assert(G >= SPDNN_MAX_CHOSEN);
+    constexpr int V = kGradLogits, kTeams = kRowThreads / G;
+    const int lane = threadIdx.x % G, team = threadIdx.x / G;
+    const bool all = score == SPDNN_SOFTMAX && !normalise;
+    for (int64_t t0 = (int64_t)blockIdx.x * kTeams; t0 < rows; t0 += (int64_t)gridDim.x * kTeams) {
+        const int64_t t = min(t0 + team, (int64_t)rows - 1);
+        const T* row = logits + t * stride;
+        T* to = dlogits + t * dstride;
+        const int e = lane < k ? chosen[t * k + lane] : -1;
+        const bool valid = e >= 0 && e < experts;
+        const float l = valid ? (float)row[e] : 0.0f;
         const float g = valid ? scale * dweight[t * k + lane] : 0.0f;
-        const bool dense = score == SPDNN_SOFTMAX && !normalise;
-        const bool any = __ballot(valid) != 0;
+        const bool any = team_max<G>(valid ? 1.0f : 0.0f) > 0.0f;
         float top = -INFINITY, total = 0.0f;
-        if (dense && any) {
-            for (int e = lane; e < experts; e += 64) {
-                const float x = (float)logits[t * stride + e];
-                if ((bias ? x + bias[e] : x) > -INFINITY) top = fmaxf(top, x);
+        if (all && any) {
+            for (int col = lane * V; col < experts; col += G * V) {
+                float x[V], b[V];
+                load_logits<V>(row, col, experts, x);
+                load_bias<V>(bias, col, experts, b);
+#pragma unroll
+                for (int i = 0; i < V; ++i) top = x[i] + b[i] > -INFINITY ? fmaxf(top, x[i]) : top;
             }
-            top = wave_max(top);
-            for (int e = lane; e < experts; e += 64) {
-                const float x = (float)logits[t * stride + e];
-                if ((bias ? x + bias[e] : x) > -INFINITY) total += expf(x - top);
+            top = team_max<G>(top);
+            for (int col = lane * V; col < experts; col += G * V) {
+                float x[V], b[V];
+                load_logits<V>(row, col, experts, x);
+                load_bias<V>(bias, col, experts, b);
+#pragma unroll
+                for (int i = 0; i < V; ++i) total += x[i] + b[i] > -INFINITY ? expf(x[i] - top) : 0.0f;
             }
-            total = wave_sum(total);
+            total = team_sum<G>(total);
         }
-        const float w = slot_weight(l, valid, score, normalise, top, total);
-        const float mean = wave_sum(g * w);
-        float d = 0.0f;  // of the slot's logit, but for the dense form's part that every logit has
-        if (valid) {
-            if (dense) d = g;
-            else if (normalise) d = w * (g - mean) * (score == SPDNN_SIGMOID ? sigmoid(-l) : 1.0f);
-            else d = g * w * sigmoid(-l);
-        }
-        for (int e0 = 0; e0 < experts; e0 += 64) {
-            const int e = e0 + lane;
-            float at = 0.0f;
-            for (int j = 0; j < k; ++j) {
-                const int to = __shfl(valid ? mine : -1, j);
-                const float dj = __shfl(d, j);
-                if (to == e) at = dj;
+        const float w = slot_weight<G>(l, valid, score, normalise, top, total);
+        const float mean = team_sum<G>(g * w);
+        float d;  // of the slot's logit
+        if (normalise) d = w * (g - mean) * (score == SPDNN_SIGMOID ? sigmoid(-l) : 1.0f);
+        else d = score == SPDNN_SIGMOID ? g * w * sigmoid(-l) : w * (g - mean);
+        for (int col = lane * V; col < experts; col += G * V) {
+            float x[V] = {};
+            if (all && any) {
+                float b[V];
+                load_logits<V>(row, col, experts, x);
+                load_bias<V>(bias, col, experts, b);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] = x[i] + b[i] > -INFINITY ? expf(x[i] - top) / total * -mean : 0.0f;
             }
-            if (e >= experts) continue;
-            if (dense) {
-                const float x = (float)logits[t * stride + e];
-                const bool open = any && (bias ? x + bias[e] : x) > -INFINITY;
-                at = open ? expf(x - top) / total * (at - mean) : 0.0f;
+            if (col + V <= experts) {
+                store_vec<V, T>(to + col, rounded_vec<T, V>(x), false);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (col + i < experts) to[col + i] = rounded<T>(x[i]);
             }
-            dlogits[t * dstride + e] = rounded<T>(at);
         }
+        // The wave's stores to one address keep their order, whichever lanes they come from.
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (valid) to[e] = rounded<T>(d);
     }
 }
 
