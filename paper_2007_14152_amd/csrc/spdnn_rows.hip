@@ -113,13 +113,13 @@ void with_ids(int32_t type, F f) {
 
 // How n pairs are cut for the sort.
 struct Chunks {
-    int64_t size;
+    int log_size;
     int32_t count;  // 1 at least
 };
 Chunks chunks_of(int64_t n) {
-    const int64_t each = (n + spdnn::kMostChunks - 1) / spdnn::kMostChunks;
-    const int64_t size = std::max<int64_t>(spdnn::kLeastChunk, (each + spdnn::kSortThreads - 1) / spdnn::kSortThreads * spdnn::kSortThreads);
-    return {size, (int32_t)std::max<int64_t>(1, (n + size - 1) / size)};
+    int log = 0;
+    while ((int64_t)1 << log < spdnn::kLeastChunk || (int64_t)spdnn::kMostChunks << log < n) ++log;
+    return {log, (int32_t)std::max<int64_t>(1, ((n - 1) >> log) + 1)};
 }
 
 // Work memory of the gradient of a table, and how many bits of the ids are sorted at a time.
@@ -147,6 +147,8 @@ struct GradWork {
 };
 static_assert(spdnn::kMostBins >= 1 << 10 && spdnn::kMostBins >= 256);
 constexpr int64_t kClearBytes = 128 << 10;  // of a table that a workgroup clears at a time
+constexpr int64_t kCountClears = 24 << 20, kPlaceClears = 40 << 20;  // ... that a launch of the sort clears beside
+constexpr int kSpareGroups = 768;           // workgroups for that
 constexpr int kMostRowsEach = 256;          // rows of a table that a workgroup has with few ids
 constexpr int64_t kFewGroups = 2048;        // workgroups with few ids, if they have no more rows than that
 
@@ -254,7 +256,7 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
                         const int y = std::min((vecs - 1) / 64 + 1, 1024);
                         const int per = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)vocab * y / kFewGroups, kMostRowsEach));
                         const int64_t x = std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
-                        spdnn::embed_grad_few_kernel<T, S, I, V><<<dim3((unsigned)x, (unsigned)y), spdnn::kSortThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, per, (vecs - 1) / y + 1, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
+                        spdnn::embed_grad_few_kernel<T, S, I, V><<<dim3((unsigned)x, (unsigned)y), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, per, (vecs - 1) / y + 1, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
                     });
                 });
             });
@@ -265,24 +267,38 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
     const GradWork w(vocab, width, n);
     char* const base = (char*)work;
     const Chunks c = chunks_of(n);
-    int32_t* const table = (int32_t*)(base + w.table);
+    const int bins = 1 << w.bits;
+    int32_t* const table = c.count > 1 ? (int32_t*)(base + w.table) : nullptr;
     const uint32_t* keys = nullptr;
     const int32_t* tokens = nullptr;
+    // The sort's launches leave most of the chip idle: meanwhile the last rows of the table are cleared, whether their ids occur
+    // or not.  (The last ones because ids are mostly numbered by frequency: rows that are written again cost twice.)
+    spdnn::Clear rows{(char*)dtable, dtable_stride * size_of(dtable_type), (int32_t)std::min<int64_t>(row_bytes, INT32_MAX), vocab, vocab, past};
+    const auto spare = [&](int64_t bytes) -> int {  // workgroups that clear so much, and the rows for it
+        rows.last = rows.first;
+        if (accumulate || row_bytes < 16 || row_bytes > INT32_MAX) return 0;
+        rows.first = std::max<int64_t>(0, rows.last - bytes / row_bytes);
+        return rows.first < rows.last ? kSpareGroups : 0;
+    };
     for (int pass = 0; pass < w.passes; ++pass) {
         uint32_t* const to_keys = (uint32_t*)(base + w.keys[pass & 1]);
         int32_t* const to_tokens = (int32_t*)(base + w.tokens[pass & 1]);
-        const int shift = pass * w.bits, mask = (1 << w.bits) - 1;
+        const int shift = pass * w.bits;
         const auto sort = [&](auto in) {
-            spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, mask + 1, table);
-            spdnn::key_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, table, c.count, to_keys, to_tokens);
+            if (table) {
+                const int more = spare(kCountClears);
+                spdnn::count_kernel<<<c.count + more, spdnn::kSortThreads, 0, s>>>(in, n, c.log_size, c.count, bins, table, rows);
+            }
+            const int more = spare(kPlaceClears);
+            spdnn::key_place_kernel<<<c.count + more, spdnn::kSortThreads, 0, s>>>(in, n, c.log_size, c.count, table, to_keys, to_tokens, rows);
         };
         if (pass == 0)
             with_ids(ids_type, [&](auto ti) {
                 using I = decltype(ti);
-                sort(spdnn::IdItems<I>{(const I*)ids, (uint32_t)vocab, shift, mask});
+                sort(spdnn::IdItems<I>{(const I*)ids, (uint32_t)vocab, shift, bins - 1});
             });
         else
-            sort(spdnn::KeyItems{keys, tokens, shift, mask});
+            sort(spdnn::KeyItems{keys, tokens, shift, bins - 1});
         keys = to_keys;
         tokens = to_tokens;
     }
@@ -300,9 +316,9 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
                     constexpr int L = decltype(l)::value;
                     const int adders = (int)std::min<int64_t>((pieces - 1) / (spdnn::kRowThreads / L) + 1, kMostGroups);
                     const int per = (int)std::min<int64_t>(std::max<int64_t>(kClearBytes / row_bytes, 1), spdnn::kRowThreads);
-                    const int clear = accumulate ? 0 : (int)std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
+                    const int clear = accumulate ? 0 : (int)std::min<int64_t>((rows.first + per - 1) / per, kMostGroups);
                     const dim3 grid(adders + clear, std::min((vecs - 1) / L + 1, 1024));
-                    spdnn::embed_grad_kernel<T, S, V, L><<<grid, spdnn::kRowThreads, 0, s>>>(order, (const T*)dout, dout_stride, width, scale, accumulate != 0, (S*)dtable, dtable_stride, parts, adders, per, past);
+                    spdnn::embed_grad_kernel<T, S, V, L><<<grid, spdnn::kRowThreads, 0, s>>>(order, (const T*)dout, dout_stride, width, scale, accumulate != 0, (S*)dtable, dtable_stride, parts, adders, (uint32_t)rows.first, per, past);
                 };
                 if (vecs <= 16) run(std::integral_constant<int, 16>{});
                 else if (vecs <= 64) run(std::integral_constant<int, 64>{});
@@ -361,7 +377,8 @@ int spdnn_route_grad(const float* dweight, const void* logits, int32_t type, int
 int spdnn_dispatch_bytes(int32_t rows, int32_t k, int32_t experts, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
     CHECK(check_pairs(rows, k, experts));
-    *bytes = sizeof(int32_t) * experts * chunks_of((int64_t)rows * k).count;
+    const Chunks c = chunks_of((int64_t)rows * k);
+    *bytes = c.count > 1 ? sizeof(int32_t) * experts * c.count : 0;
     return SPDNN_OK;
 }
 
@@ -383,8 +400,9 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
     const bool few = n > 0 && n <= spdnn::kFewPairs;
     if (!few) {
         const Chunks c = chunks_of(n);
-        spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, experts, (int32_t*)work);
-        spdnn::expert_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.size, (const int32_t*)work, c.count, offsets, place);
+        int32_t* const table = c.count > 1 ? (int32_t*)work : nullptr;
+        if (table) spdnn::count_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.log_size, c.count, experts, table, spdnn::Clear{});
+        spdnn::expert_place_kernel<<<c.count, spdnn::kSortThreads, 0, s>>>(in, n, c.log_size, table, c.count, offsets, place);
     }
     if (n > 0)
         with_type(type, [&](auto tt) {

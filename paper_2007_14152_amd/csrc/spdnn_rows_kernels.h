@@ -411,11 +411,12 @@ __global__ __launch_bounds__(kRowThreads) void route_grad_kernel(const float* __
 // are cut into chunks, a workgroup per chunk counts (count_kernel), then every workgroup adds up the counts of all chunks for
 // itself, which is cheaper than a launch for it, and places its chunk's pairs (place_kernel).  A chunk is cut into a segment per
 // wave; a wave takes 64 pairs at a time, whose rank among equals comes from ballots, a bit of d at a time: no pair's position
-// depends on which wave was first.
-constexpr int kSortWaves = 4, kSortThreads = 64 * kSortWaves;
-constexpr int kMostBins = 1024;
+// depends on which wave was first.  One chunk needs no count.
+constexpr int kSortAhead = 4;  // pairs that a lane has under way
+constexpr int kSortWaves = 8, kSortThreads = 64 * kSortWaves;
+constexpr int kLeastChunk = kSortAhead * kSortThreads;
 constexpr int kMostChunks = 128;  // more pairs than these hold make the chunks longer
-constexpr int kLeastChunk = 1024;
+constexpr int kMostBins = 1024;
 
 // What is sorted: `at` loads a pair, `digit` is its number d (-1: it has no place).
 struct PairItems {
@@ -426,19 +427,45 @@ struct PairItems {
     __device__ int digit(Item e) const { return e >= 0 && e < experts ? e : -1; }
 };
 
+template <int WAVES>
 struct SortLds {
-    int32_t start[kSortWaves][kMostBins];
+    int32_t start[WAVES][kMostBins];
     int32_t total[kMostBins];
-    int32_t wave_sum[kSortWaves];
+    int32_t wave_sum[WAVES];
 };
-constexpr int kSortAhead = 4;  // pairs that a lane has under way
 
+// Rows first .. last - 1 of a matrix whose elements become zero, by workgroups that a launch has to spare.
+struct Clear {
+    char* base;
+    int64_t stride;  // bytes
+    int32_t bytes;   // of a row, 16 at least
+    int64_t first, last;
+    bool past;
+};
+__device__ inline void clear(const Clear& c, int group, int groups) {
+    constexpr int kRows = 16;
+    const int vecs = (c.bytes - 1) / 16 + 1;
+    for (int64_t r0 = c.first + (int64_t)group * kRows; r0 < c.last; r0 += (int64_t)groups * kRows) {
+        const int rows = (int)min((int64_t)kRows, c.last - r0);
+        for (int64_t i = threadIdx.x; i < (int64_t)rows * vecs; i += blockDim.x) {
+            const int64_t r = i / vecs;
+            const int at = min((int)(i - r * vecs) * 16, c.bytes - 16);
+            store_vec<8, uint16_t>(reinterpret_cast<uint16_t*>(c.base + (r0 + r) * c.stride + at), Pack<uint16_t, 8>{}, c.past);
+        }
+    }
+}
+
+// Workgroups beyond the chunks clear.
 template <typename D>
-__global__ __launch_bounds__(kSortThreads) void count_kernel(D in, int64_t n, int64_t chunk, int bins, int32_t* __restrict__ table) {
+__global__ __launch_bounds__(kSortThreads) void count_kernel(D in, int64_t n, int log_chunk, int chunks, int bins, int32_t* __restrict__ table, Clear c) {
     __shared__ int32_t count[kMostBins];
+    if ((int)blockIdx.x >= chunks) {
+        clear(c, blockIdx.x - chunks, gridDim.x - chunks);
+        return;
+    }
     for (int e = threadIdx.x; e < bins; e += kSortThreads) count[e] = 0;
     __syncthreads();
-    const int64_t first = blockIdx.x * chunk, last = min(first + chunk, n);
+    const int64_t first = (int64_t)blockIdx.x << log_chunk, last = min(first + (1ll << log_chunk), n);
     for (int64_t p0 = first + threadIdx.x; p0 < last; p0 += kSortAhead * kSortThreads) {
         typename D::Item x[kSortAhead];
 #pragma unroll
@@ -455,12 +482,12 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(D in, int64_t n, in
 
 // to(pair, item, position) for every pair of chunk `me`, position -1 without a digit; offsets (may be NULL): first positions of
 // the bins, and the end.  table: the counts of `chunks` chunks, or NULL if there is only this one.
-template <typename D, typename F>
+template <int WAVES, typename D, typename F>
 __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, const int32_t* __restrict__ table, int chunks, int me,
-                                   SortLds& lds, int32_t* __restrict__ offsets, F to) {
-    constexpr int A = kSortAhead;
+                                   SortLds<WAVES>& lds, int32_t* __restrict__ offsets, F to) {
+    constexpr int A = kSortAhead, kThreads = 64 * WAVES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t part = ((last - first + kSortThreads - 1) / kSortThreads) * 64;
+    const int64_t part = ((last - first + kThreads - 1) / kThreads) * 64;
     const int64_t mine = min(first + wave * part, last), end = min(mine + part, last);
     typename D::Item x[A];  // the wave's pairs, A * 64 at a time; where there are no more, they are loaded once
     const auto load = [&](int64_t p0) {
@@ -468,8 +495,8 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
         for (int a = 0; a < A; ++a) x[a] = in.at(min(p0 + a * 64 + lane, end - 1));
     };
     if (mine < end) load(mine);
-    for (int e = threadIdx.x; e < bins; e += kSortThreads)
-        for (int w = 0; w < kSortWaves; ++w) lds.start[w][e] = 0;
+    for (int e = threadIdx.x; e < bins; e += kThreads)
+        for (int w = 0; w < WAVES; ++w) lds.start[w][e] = 0;
     __syncthreads();
     for (int64_t p0 = mine; p0 < end; p0 += A * 64) {
         if (p0 != mine) load(p0);
@@ -481,7 +508,7 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
     }
     __syncthreads();
     // bin e's pairs in all chunks, and in start[0][e] .. start[3][e] where each wave's first one goes, within the bin
-    for (int e = threadIdx.x; e < bins; e += kSortThreads) {
+    for (int e = threadIdx.x; e < bins; e += kThreads) {
         int before = 0, total = 0;
         if (table) {
             constexpr int B = 16;
@@ -496,7 +523,7 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
                 }
             }
         }
-        for (int w = 0; w < kSortWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const int y = lds.start[w][e];
             lds.start[w][e] = before;
             before += y;
@@ -505,7 +532,7 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
     }
     __syncthreads();
     // a thread's bins next to each other: their sum, the sums before it, then each bin's first position
-    constexpr int kEach = kMostBins / kSortThreads;
+    constexpr int kEach = kMostBins / kThreads;
     int many[kEach], sum = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -527,7 +554,7 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
         const int e = threadIdx.x * kEach + i;
         if (e < bins) {
             if (offsets) offsets[e] = base;
-            for (int w = 0; w < kSortWaves; ++w) lds.start[w][e] += base;
+            for (int w = 0; w < WAVES; ++w) lds.start[w][e] += base;
             base += many[i];
             if (offsets && e == bins - 1) offsets[bins] = base;
         }
@@ -539,6 +566,7 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
         if (end - mine > A * 64) load(p0);
 #pragma unroll
         for (int a = 0; a < A; ++a) {
+            if (p0 + a * 64 >= end) break;
             const int64_t p = p0 + a * 64 + lane;
             const int d = p < end ? in.digit(x[a]) : -1;
             uint64_t same = __ballot(d >= 0);
@@ -556,11 +584,11 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
     }
 }
 
-__global__ __launch_bounds__(kSortThreads) void expert_place_kernel(PairItems in, int64_t n, int64_t chunk, const int32_t* __restrict__ table,
+__global__ __launch_bounds__(kSortThreads) void expert_place_kernel(PairItems in, int64_t n, int log_chunk, const int32_t* __restrict__ table,
                                                                     int chunks, int32_t* __restrict__ offsets, int32_t* __restrict__ place) {
-    __shared__ SortLds lds;
-    const int64_t first = blockIdx.x * chunk;
-    place_chunk(in, first, min(first + chunk, n), in.experts, table, chunks, blockIdx.x, lds, blockIdx.x == 0 ? offsets : nullptr,
+    __shared__ SortLds<kSortWaves> lds;
+    const int64_t first = (int64_t)blockIdx.x << log_chunk;
+    place_chunk(in, first, min(first + (1ll << log_chunk), n), in.experts, table, chunks, blockIdx.x, lds, blockIdx.x == 0 ? offsets : nullptr,
                 [&](int64_t p, int32_t, int at) { place[p] = at; });
 }
 
@@ -593,13 +621,17 @@ struct KeyItems {
     __device__ int digit(Item x) const { return (int)(x.key >> shift) & mask; }
 };
 
-// Sorted by one more digit.
+// Sorted by one more digit; workgroups beyond the chunks clear.
 template <typename D>
-__global__ __launch_bounds__(kSortThreads) void key_place_kernel(D in, int64_t n, int64_t chunk, const int32_t* __restrict__ table, int chunks,
-                                                                 uint32_t* __restrict__ keys, int32_t* __restrict__ tokens) {
-    __shared__ SortLds lds;
-    const int64_t first = blockIdx.x * chunk;
-    place_chunk(in, first, min(first + chunk, n), in.mask + 1, table, chunks, blockIdx.x, lds, nullptr, [&](int64_t, Token x, int at) {
+__global__ __launch_bounds__(kSortThreads) void key_place_kernel(D in, int64_t n, int log_chunk, int chunks, const int32_t* __restrict__ table,
+                                                                 uint32_t* __restrict__ keys, int32_t* __restrict__ tokens, Clear c) {
+    __shared__ SortLds<kSortWaves> lds;
+    if ((int)blockIdx.x >= chunks) {
+        clear(c, blockIdx.x - chunks, gridDim.x - chunks);
+        return;
+    }
+    const int64_t first = (int64_t)blockIdx.x << log_chunk;
+    place_chunk(in, first, min(first + (1ll << log_chunk), n), in.mask + 1, table, chunks, blockIdx.x, lds, nullptr, [&](int64_t, Token x, int at) {
         keys[at] = x.key;
         tokens[at] = x.token;
     });
@@ -656,10 +688,10 @@ struct RowItems {
 // fall there and adds up or clears a row after the other.
 constexpr int kFewIds = 1024;
 template <typename T, typename S, typename I, int V>
-__global__ __launch_bounds__(kSortThreads) void embed_grad_few_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
+__global__ __launch_bounds__(kRowThreads) void embed_grad_few_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
                                                                       int vocab, int width, int per, int slab, float scale, bool accumulate,
                                                                       S* __restrict__ dtable, int64_t dtable_stride, bool past) {
-    __shared__ SortLds lds;
+    __shared__ SortLds<kRowThreads / 64> lds;
     __shared__ int32_t tokens[kFewIds], offsets[kMostBins + 1];
     const int vecs = (width - 1) / V + 1, vec0 = blockIdx.y * slab, here = min(slab, vecs - vec0);
     for (int64_t v0 = (int64_t)blockIdx.x * per; v0 < vocab; v0 += (int64_t)gridDim.x * per) {
@@ -669,7 +701,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_grad_few_kernel(const T* _
             if (at >= 0) tokens[at] = (int32_t)p;
         });
         __syncthreads();
-        for (int i = threadIdx.x; i < rows * here; i += kSortThreads) {
+        for (int i = threadIdx.x; i < rows * here; i += kRowThreads) {
             const int r = i / here, vec = vec0 + i - r * here, col = min(vec * V, width - V);
             const int first = offsets[r], last = offsets[r + 1];
             if (accumulate && first == last) continue;
@@ -755,13 +787,13 @@ __device__ inline void add_pieces(const GradOrder& o, const T* __restrict__ dout
     }
 }
 
-// Zeros in rows of ids that do not occur.
+// Zeros in the first `end` rows, in those of ids that do not occur.
 template <typename S, int V>
-__device__ inline void clear_rows(const GradOrder& o, int width, int per, S* __restrict__ dtable, int64_t dtable_stride, bool past, int group, int groups) {
+__device__ inline void clear_rows(const GradOrder& o, uint32_t end, int width, int per, S* __restrict__ dtable, int64_t dtable_stride, bool past, int group, int groups) {
     __shared__ bool there[kRowThreads];
     const int vecs = (width - 1) / V + 1;
-    for (int64_t v0 = (int64_t)group * per; v0 < o.vocab; v0 += (int64_t)groups * per) {
-        const int rows = (int)min((int64_t)per, (int64_t)o.vocab - v0);
+    for (int64_t v0 = (int64_t)group * per; v0 < end; v0 += (int64_t)groups * per) {
+        const int rows = (int)min((int64_t)per, (int64_t)end - v0);
         __syncthreads();
         if ((int)threadIdx.x < rows) {
             const int at = o.lower((uint32_t)v0 + threadIdx.x);
@@ -775,15 +807,16 @@ __device__ inline void clear_rows(const GradOrder& o, int width, int per, S* __r
     }
 }
 
-// The first `adders` workgroups add pieces, the others (none if accumulate) clear rows, `per` at a time.
+// The first `adders` workgroups add pieces, the others (none if accumulate) clear those of the first `end` rows that have no id,
+// `per` at a time.
 template <typename T, typename S, int V, int L>
 __global__ __launch_bounds__(kRowThreads) void embed_grad_kernel(GradOrder o, const T* __restrict__ dout, int64_t dout_stride, int width, float scale,
                                                                  bool accumulate, S* __restrict__ dtable, int64_t dtable_stride,
-                                                                 float* __restrict__ parts, int adders, int per, bool past) {
+                                                                 float* __restrict__ parts, int adders, uint32_t end, int per, bool past) {
     if ((int)blockIdx.x < adders)
         add_pieces<T, S, V, L>(o, dout, dout_stride, width, scale, accumulate, dtable, dtable_stride, parts, blockIdx.x, adders);
     else if (blockIdx.y == 0)
-        clear_rows<S, V>(o, width, per, dtable, dtable_stride, past, blockIdx.x - adders, gridDim.x - adders);
+        clear_rows<S, V>(o, end, width, per, dtable, dtable_stride, past, blockIdx.x - adders, gridDim.x - adders);
 }
 
 // The rows of ids whose places lie in more than one piece: a workgroup per piece and 64 vectors of columns, which has work if such a
@@ -894,8 +927,7 @@ template <typename T, int V>
 __global__ __launch_bounds__(kRowThreads) void dispatch_few_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k, PairItems in,
                                                                    int32_t* __restrict__ offsets, int32_t* __restrict__ place, T* __restrict__ xs,
                                                                    int64_t xs_stride) {
-    static_assert(kRowThreads == kSortThreads);
-    __shared__ SortLds lds;
+    __shared__ SortLds<kRowThreads / 64> lds;
     __shared__ int32_t places[kFewPairs];
     __shared__ int32_t used;
     const bool first = blockIdx.x == 0 && blockIdx.y == 0;

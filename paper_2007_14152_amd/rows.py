@@ -118,9 +118,9 @@ def embed_grad(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
     otype, ostride = _rows(out, "out", dev, (vocab, width))
     need = ctypes.c_size_t()
     _check(lib().spdnn_embed_grad_bytes(vocab, width, n, ctypes.byref(need)))
-    work = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    _check(lib().spdnn_embed_grad(dout.data_ptr(), itype, dstride, ids.data_ptr(), _IDS[ids.dtype], n, vocab, width, scale,
-                                  add, out.data_ptr(), otype, ostride, work.data_ptr(), need.value, _stream(dev.index)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    _check(lib().spdnn_embed_grad(dout.data_ptr(), itype, dstride, ids.data_ptr(), _IDS[ids.dtype], n, vocab, width, scale, add,
+                                  out.data_ptr(), otype, ostride, work.data_ptr() if need.value else 0, need.value, _stream(dev.index)))
     return out
 
 
@@ -184,9 +184,9 @@ def dispatch(x, chosen, experts):
     xs = torch.empty((rows * k, width), dtype=x.dtype, device=dev)
     offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev)
     place = torch.empty((rows, k), dtype=torch.int32, device=dev)
-    work = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    _check(lib().spdnn_dispatch(cp, rows, k, experts, x.data_ptr(), xtype, width, xstride, xs.data_ptr(), width,
-                                offsets.data_ptr(), place.data_ptr(), work.data_ptr(), need.value, _stream(dev.index)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    _check(lib().spdnn_dispatch(cp, rows, k, experts, x.data_ptr(), xtype, width, xstride, xs.data_ptr(), width, offsets.data_ptr(),
+                                place.data_ptr(), work.data_ptr() if need.value else 0, need.value, _stream(dev.index)))
     return xs, offsets, place
 
 
