@@ -145,12 +145,11 @@ struct GradWork {
         parts = take(sizeof(float) * 2 * (size_t)width * ((size_t)(n - 1) / spdnn::kPiece + 1));
     }
 };
-static_assert(spdnn::kMostBins >= 1 << 10 && spdnn::kMostBins >= 256);
+static_assert(spdnn::kMostBins >= 1 << 10);
 constexpr int64_t kClearBytes = 128 << 10;  // of a table that a workgroup clears at a time
 constexpr int64_t kCountClears = 24 << 20, kPlaceClears = 40 << 20;  // ... that a launch of the sort clears beside
 constexpr int kSpareGroups = 768;           // workgroups for that
-constexpr int kMostRowsEach = 256;          // rows of a table that a workgroup has with few ids
-constexpr int64_t kFewGroups = 2048;        // workgroups with few ids, if they have no more rows than that
+constexpr int64_t kFewGroups = 4096;        // workgroups that add with few ids
 
 // f(V) with the elements of a vector: V, or 1 where a row has less.
 template <int V, typename F>
@@ -252,11 +251,11 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
                     with_vec<16 / std::max(sizeof(T), sizeof(S))>(width, [&](auto v) {
                         constexpr int V = decltype(v)::value;
                         const int vecs = (width - 1) / V + 1;
-                        // a wave's width of columns each, so that many share the rows of a frequent id; eight workgroups per CU
-                        const int y = std::min((vecs - 1) / 64 + 1, 1024);
-                        const int per = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)vocab * y / kFewGroups, kMostRowsEach));
-                        const int64_t x = std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
-                        spdnn::embed_grad_few_kernel<T, S, I, V><<<dim3((unsigned)x, (unsigned)y), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, per, (vecs - 1) / y + 1, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
+                        const int per = (int)std::min<int64_t>(std::max<int64_t>(kClearBytes / row_bytes, 1), spdnn::kMostRowsToClear);
+                        const int64_t clear = accumulate ? 0 : std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
+                        // as many workgroups for a token's columns as make kFewGroups in all
+                        const int y = (int)std::max<int64_t>(1, std::min<int64_t>((vecs - 1) / 64 + 1, kFewGroups / std::max(n, 1)));
+                        spdnn::embed_grad_few_kernel<T, S, I, V><<<dim3((unsigned)(n + clear), (unsigned)y), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, n, per, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
                     });
                 });
             });
@@ -326,7 +325,7 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
             });
             with_vec<spdnn::kJoinVec>(width, [&](auto v) {
                 constexpr int V = decltype(v)::value;
-                const dim3 grid((unsigned)std::min(pieces, kMostGroups), (unsigned)std::min((width - 1) / (64 * V) + 1, 1024));
+                const dim3 grid((unsigned)std::min(pieces, kMostGroups), (unsigned)std::min((width - 1) / (64 * V) + 1, 64));
                 spdnn::embed_grad_join_kernel<S, V><<<grid, spdnn::kRowThreads, 0, s>>>(order, width, scale, accumulate != 0, (S*)dtable, dtable_stride, parts);
             });
         });

@@ -427,10 +427,10 @@ struct PairItems {
     __device__ int digit(Item e) const { return e >= 0 && e < experts ? e : -1; }
 };
 
-template <int WAVES>
+template <int WAVES, int BINS = kMostBins>
 struct SortLds {
-    int32_t start[WAVES][kMostBins];
-    int32_t total[kMostBins];
+    int32_t start[WAVES][BINS];
+    int32_t total[BINS];
     int32_t wave_sum[WAVES];
 };
 
@@ -482,9 +482,9 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(D in, int64_t n, in
 
 // to(pair, item, position) for every pair of chunk `me`, position -1 without a digit; offsets (may be NULL): first positions of
 // the bins, and the end.  table: the counts of `chunks` chunks, or NULL if there is only this one.
-template <int WAVES, typename D, typename F>
+template <int WAVES, int BINS, typename D, typename F>
 __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, const int32_t* __restrict__ table, int chunks, int me,
-                                   SortLds<WAVES>& lds, int32_t* __restrict__ offsets, F to) {
+                                   SortLds<WAVES, BINS>& lds, int32_t* __restrict__ offsets, F to) {
     constexpr int A = kSortAhead, kThreads = 64 * WAVES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t part = ((last - first + kThreads - 1) / kThreads) * 64;
@@ -532,7 +532,8 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
     }
     __syncthreads();
     // a thread's bins next to each other: their sum, the sums before it, then each bin's first position
-    constexpr int kEach = kMostBins / kThreads;
+    constexpr int kEach = BINS / kThreads;
+    static_assert(BINS % kThreads == 0);
     int many[kEach], sum = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -670,44 +671,77 @@ __device__ inline void add_rows(const T* __restrict__ dout, int64_t dout_stride,
     }
 }
 
-// The ids that fall into rows v0 .. v0 + rows - 1 of the table.
-template <typename I>
-struct RowItems {
-    using Item = int32_t;  // the row from v0 on, -1 outside
-    const I* ids;
-    I v0;
-    int rows;
-    __device__ Item at(int64_t p) const {
-        const I id = ids[p];
-        return id >= v0 && id < v0 + rows ? (int)(id - v0) : -1;
-    }
-    __device__ int digit(Item r) const { return r; }
-};
-
-// Few ids, one launch: a workgroup has `per` rows of the table (at most kMostBins) and `slab` of their vectors, sorts the ids that
-// fall there and adds up or clears a row after the other.
-constexpr int kFewIds = 1024;
+// Few ids, one launch and no sort.  The first `adders` workgroups (of blockIdx.x) have a token each: the one that is the first
+// with its id finds the others in order and adds their rows, a quarter of them per wave, 64 vectors of columns at a time (shared
+// out over blockIdx.y).  The others (none if accumulate) clear `per` rows each, but for those that an id has.
+constexpr int kFewIds = 1024, kMostRowsToClear = 1024;
 template <typename T, typename S, typename I, int V>
 __global__ __launch_bounds__(kRowThreads) void embed_grad_few_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
-                                                                      int vocab, int width, int per, int slab, float scale, bool accumulate,
-                                                                      S* __restrict__ dtable, int64_t dtable_stride, bool past) {
-    __shared__ SortLds<kRowThreads / 64> lds;
-    __shared__ int32_t tokens[kFewIds], offsets[kMostBins + 1];
-    const int vecs = (width - 1) / V + 1, vec0 = blockIdx.y * slab, here = min(slab, vecs - vec0);
-    for (int64_t v0 = (int64_t)blockIdx.x * per; v0 < vocab; v0 += (int64_t)gridDim.x * per) {
-        const int rows = (int)min((int64_t)per, vocab - v0);
-        __syncthreads();  // the table's rows before these are done with what is sorted
-        place_chunk(RowItems<I>{ids, (I)v0, rows}, 0, n, rows, nullptr, 1, 0, lds, offsets, [&](int64_t p, int32_t, int at) {
-            if (at >= 0) tokens[at] = (int32_t)p;
-        });
-        __syncthreads();
-        for (int i = threadIdx.x; i < rows * here; i += kRowThreads) {
-            const int r = i / here, vec = vec0 + i - r * here, col = min(vec * V, width - V);
-            const int first = offsets[r], last = offsets[r + 1];
-            if (accumulate && first == last) continue;
-            float sum[V] = {};
-            add_rows<V>(dout, dout_stride, col, first, last, [&](int a) { return tokens[a]; }, sum);
-            put_grad<S, V>(dtable + (v0 + r) * dtable_stride + col, vec * V - col, sum, first < last ? scale : 0.0f, accumulate, past);
+                                                                     int vocab, int width, int adders, int per, float scale, bool accumulate,
+                                                                     S* __restrict__ dtable, int64_t dtable_stride, bool past) {
+    constexpr int kWaves = kRowThreads / 64, kRounds = kFewIds / kRowThreads;
+    __shared__ uint64_t with_id[kRounds * kWaves];
+    __shared__ int32_t tokens[kFewIds];
+    __shared__ float sums[kWaves][64][V];
+    __shared__ bool there[kMostRowsToClear];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int vecs = (width - 1) / V + 1;
+    I id[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) id[r] = n > 0 ? ids[min(r * kRowThreads + (int)threadIdx.x, n - 1)] : (I)-1;
+    if ((int)blockIdx.x >= adders) {
+        if (blockIdx.y) return;
+        for (int64_t v0 = (int64_t)(blockIdx.x - adders) * per; v0 < vocab; v0 += (int64_t)(gridDim.x - adders) * per) {
+            const int rows = (int)min((int64_t)per, vocab - v0);
+            __syncthreads();
+            for (int r = threadIdx.x; r < rows; r += kRowThreads) there[r] = false;
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r)
+                if (id[r] >= (I)v0 && id[r] < (I)(v0 + rows)) there[(int)(id[r] - (I)v0)] = true;
+            __syncthreads();
+            for (int64_t i = threadIdx.x; i < (int64_t)rows * vecs; i += kRowThreads) {
+                const int r = (int)(i / vecs), vec = (int)(i - (int64_t)r * vecs);
+                if (!there[r]) store_vec<V, S>(dtable + (v0 + r) * dtable_stride + min(vec * V, width - V), Pack<S, V>{}, past);
+            }
+        }
+        return;
+    }
+    const int t = blockIdx.x;
+    const I v = ids[t];
+    if (v < 0 || v >= (I)vocab) return;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const uint64_t mine = __ballot(id[r] == v && r * kRowThreads + (int)threadIdx.x < n);
+        if (lane == 0) with_id[r * kWaves + wave] = mine;
+    }
+    __syncthreads();
+    int many = 0, first = -1;
+#pragma unroll
+    for (int i = 0; i < kRounds * kWaves; ++i) {
+        const uint64_t some = with_id[i];
+        if (first < 0 && some) first = i * 64 + __ffsll((unsigned long long)some) - 1;
+        if (i % kWaves == wave && (some >> lane & 1)) tokens[many + __popcll(some & ((1ull << lane) - 1))] = i * 64 + lane;
+        many += __popcll(some);
+    }
+    if (first != t) return;
+    __syncthreads();
+    const int each = (many + kWaves - 1) / kWaves, from = min(wave * each, many), to = min(from + each, many);
+    for (int v0 = blockIdx.y * 64; v0 < vecs; v0 += gridDim.y * 64) {
+        const int vec = min(v0 + lane, vecs - 1), col = min(vec * V, width - V);
+        float sum[V] = {};
+        add_rows<V>(dout, dout_stride, col, from, to, [&](int a) { return tokens[a]; }, sum);
+        if (many > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) sums[wave][lane][i] = sum[i];
+            __syncthreads();
+        }
+        if (wave == 0 && v0 + lane < vecs) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (many > 1) sum[i] = (sum[i] + sums[1][lane][i]) + (sums[2][lane][i] + sums[3][lane][i]);
+            put_grad<S, V>(dtable + (int64_t)v * dtable_stride + col, vec * V - col, sum, scale, accumulate, past);
         }
     }
 }
@@ -819,9 +853,25 @@ __global__ __launch_bounds__(kRowThreads) void embed_grad_kernel(GradOrder o, co
         clear_rows<S, V>(o, end, width, per, dtable, dtable_stride, past, blockIdx.x - adders, gridDim.x - adders);
 }
 
-// The rows of ids whose places lie in more than one piece: a workgroup per piece and 64 vectors of columns, which has work if such a
-// run begins there.  Its waves take a quarter of the run's parts each, the quarters are added in order.
+// The rows of ids whose places lie in more than one piece: workgroups per piece, which have work if such a run begins there.  A run
+// of at most kAhead parts is added by the first of them, every lane for its columns.  Of a longer one each workgroup has 64
+// vectors of columns at a time, each wave adds a quarter of the parts, and the quarters are added in order.
 constexpr int kJoinVec = 4;
+template <int V>
+__device__ inline void add_parts(const float* __restrict__ parts, int64_t piece, int width, int col, int from, int to, float (&sum)[V]) {
+    for (int i0 = from; i0 < to; i0 += kAhead) {
+        Pack<float, V> x[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int i = min(i0 + a, to - 1);
+            x[a] = load_vec<V>(parts + ((piece + i) * 2 + (i == 0 ? 1 : 0)) * width + col);
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] = i0 + a < to ? sum[i] + x[a][i] : sum[i];
+    }
+}
 template <typename S, int V>
 __global__ __launch_bounds__(kRowThreads) void embed_grad_join_kernel(GradOrder o, int width, float scale, bool accumulate, S* __restrict__ dtable,
                                                                       int64_t dtable_stride, const float* __restrict__ parts) {
@@ -831,9 +881,10 @@ __global__ __launch_bounds__(kRowThreads) void embed_grad_join_kernel(GradOrder 
     const int vecs = (width - 1) / V + 1;
     const int pieces = (o.n - 1) / kPiece + 1;
     for (int64_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
-        const int64_t first = piece * kPiece, end = min(first + kPiece, (int64_t)o.n);
+        const int64_t first = piece * kPiece, end = min(first + kPiece, (int64_t)o.n), far = first + kAhead * kPiece;
         const uint32_t v = o.keys[end - 1], next = o.keys[min(end, (int64_t)o.n - 1)], head = o.keys[first], before = o.keys[max(first - 1, (int64_t)0)];
-        if (end == o.n || next != v || v >= o.vocab || (head == v && first > 0 && before == v)) continue;
+        const bool long_run = far < o.n && o.keys[far] == v;  // more than kAhead parts
+        if (end == o.n || next != v || v >= o.vocab || (head == v && first > 0 && before == v) || (!long_run && blockIdx.y)) continue;
         int64_t last = piece + 1;  // the run's last piece: the first one that does not end with v and go on so
         for (;; last += 64) {
             const int64_t e = min((last + lane + 1) * kPiece, (int64_t)o.n);
@@ -844,22 +895,21 @@ __global__ __launch_bounds__(kRowThreads) void embed_grad_join_kernel(GradOrder 
             }
         }
         const int many = (int)(last - piece) + 1, each = (many + kWaves - 1) / kWaves;
+        S* const row = dtable + (int64_t)v * dtable_stride;
+        if (!long_run) {
+            for (int vec = threadIdx.x; vec < vecs; vec += kRowThreads) {
+                const int col = min(vec * V, width - V);
+                float sum[V] = {};
+                add_parts<V>(parts, piece, width, col, 0, many, sum);
+                put_grad<S, V>(row + col, vec * V - col, sum, scale, accumulate, false);
+            }
+            continue;
+        }
         for (int v0 = blockIdx.y * 64; v0 < vecs; v0 += gridDim.y * 64) {
             const int vec = min(v0 + lane, vecs - 1), col = min(vec * V, width - V);
             float sum[V] = {};
-            const int from = min(wave * each, many), to = min(from + each, many);
-            for (int i0 = from; i0 < to; i0 += kAhead) {
-                Pack<float, V> x[kAhead];
-#pragma unroll
-                for (int a = 0; a < kAhead; ++a) {
-                    const int i = min(i0 + a, to - 1);
-                    x[a] = load_vec<V>(parts + ((piece + i) * 2 + (i == 0 ? 1 : 0)) * width + col);
-                }
-#pragma unroll
-                for (int a = 0; a < kAhead; ++a)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) sum[i] = i0 + a < to ? sum[i] + x[a][i] : sum[i];
-            }
+            const int from = min(wave * each, many);
+            add_parts<V>(parts, piece, width, col, from, min(from + each, many), sum);
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < V; ++i) sums[wave][lane][i] = sum[i];
@@ -867,7 +917,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_grad_join_kernel(GradOrder 
             if (wave == 0 && v0 + lane < vecs) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[i] = (sum[i] + sums[1][lane][i]) + (sums[2][lane][i] + sums[3][lane][i]);
-                put_grad<S, V>(dtable + (int64_t)v * dtable_stride + col, vec * V - col, sum, scale, accumulate, false);
+                put_grad<S, V>(row + col, vec * V - col, sum, scale, accumulate, false);
             }
         }
     }
