@@ -174,16 +174,14 @@ __device__ inline float team_max(float x) {
 // A logit (with bias) and its column as one number whose order is that of the choice: the larger logit first, then the lower
 // column.  It is the logit in 64 bits, of which a 32-bit float leaves the last 29 free: the column goes there, turned round
 // where a larger last part makes a larger number.  +inf becomes a finite number beyond all floats, -0 becomes 0, and what is
-// not open is the smallest number.
+// not open (-inf, a NaN) the smallest number of all, whose last bits are set already.
 constexpr uint32_t kColumnBits = 0x3ff;
 static_assert(SPDNN_MAX_EXPERTS <= kColumnBits + 1);
 __device__ inline double closed() { return -1.7976931348623157e308; }
 __device__ inline double rank_of(float r, int col) {
-    double d = (double)(r + 0.0f);
-    if (r == INFINITY) d = 0x1p1000;
-    const uint32_t last = (uint32_t)col ^ (d >= 0.0 ? kColumnBits : 0u);
-    d = __hiloint2double(__double2hiint(d), __double2loint(d) | (int)last);
-    return r > -INFINITY ? d : closed();
+    const double d = fmin(fmax((double)(r + 0.0f), closed()), 0x1p1000);
+    const int hi = __double2hiint(d);
+    return __hiloint2double(hi, __double2loint(d) | (int)((uint32_t)col ^ kColumnBits ^ ((uint32_t)(hi >> 31) & kColumnBits)));
 }
 __device__ inline int column_of(double d) {  // -1: none
     if (d == closed()) return -1;
@@ -205,17 +203,16 @@ __device__ inline void order_bitonic(double (&a)[K]) {  // a rises, then falls, 
             if (!(i & m)) order_two(a[i], a[i | m]);
 }
 template <int K>
-__device__ inline void order_all(double (&a)[K]) {
+__device__ inline void order_all(double (&a)[K]) {  // odd-even merges: 19 exchanges for 8 numbers, where bitonic ones take 24
 #pragma unroll
-    for (int n = 2; n <= K; n *= 2)
+    for (int n = 1; n < K; n *= 2)
 #pragma unroll
-        for (int m = n / 2; m; m /= 2)
+        for (int m = n; m; m /= 2)
 #pragma unroll
-            for (int i = 0; i < K; ++i) {
-                if (i & m) continue;
-                if (i & n) order_two(a[i | m], a[i]);
-                else order_two(a[i], a[i | m]);
-            }
+            for (int i = m % n; i + m < K; i += 2 * m)
+#pragma unroll
+                for (int j = 0; j < m; ++j)
+                    if (i + j + m < K && (i + j) / (2 * n) == (i + j + m) / (2 * n)) order_two(a[i + j], a[i + j + m]);
 }
 // The first K of a and b, both in order.
 template <int K>
@@ -268,12 +265,41 @@ __device__ inline void load_logits(const T* __restrict__ row, int col, int exper
         for (int i = 0; i < V; ++i) l[i] = col + i < experts ? (float)row[col + i] : -INFINITY;
     }
 }
+// What the choice goes by: logits l of columns from col on, with their bias.
 template <int V>
-__device__ inline void load_bias(const float* __restrict__ bias, int col, int experts, float (&b)[V]) {
-    if (bias) load_logits(bias, col, experts, b);
+__device__ inline void add_bias(const float* __restrict__ bias, int col, int experts, const float (&l)[V], float (&r)[V]) {
+    if (bias) {
+        float b[V];
+        load_logits<V>(bias, col, experts, b);
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (!bias || col + i >= experts) b[i] = 0.0f;
+        for (int i = 0; i < V; ++i) r[i] = l[i] + b[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = l[i];
+    }
+}
+
+// The largest open logit of a team's row, and the sum of exp(logit - the largest) over the open ones.
+template <int V, int G, typename T>
+__device__ inline void softmax_sums(const T* __restrict__ row, const float* __restrict__ bias, int lane, int columns, float& top, float& total) {
+    top = -INFINITY;
+    total = 0.0f;
+    for (int col = lane * V; col < columns; col += G * V) {
+        float l[V], r[V];
+        load_logits<V>(row, col, columns, l);
+        add_bias<V>(bias, col, columns, l, r);
+#pragma unroll
+        for (int i = 0; i < V; ++i) top = r[i] > -INFINITY ? fmaxf(top, l[i]) : top;
+    }
+    top = team_max<G>(top);
+    for (int col = lane * V; col < columns; col += G * V) {
+        float l[V], r[V];
+        load_logits<V>(row, col, columns, l);
+        add_bias<V>(bias, col, columns, l, r);
+#pragma unroll
+        for (int i = 0; i < V; ++i) total += r[i] > -INFINITY ? expf(l[i] - top) : 0.0f;
+    }
+    total = team_sum<G>(total);
 }
 
 // A team of G lanes takes a row, kLogits columns a lane at a time.  Every lane keeps the first K of its columns in order (K: k
@@ -292,38 +318,27 @@ __global__ __launch_bounds__(kRowThreads) void route_kernel(const T* __restrict_
         const T* row = logits + t * stride;
         const int columns = !keep || keep[t] ? experts : 0;
         double first[K];
-#pragma unroll
-        for (int i = 0; i < K; ++i) first[i] = closed();
-        float top = -INFINITY, total = 0.0f;
-        for (int col = lane * V; col < columns; col += G * V) {
-            float l[V], b[V];
-            load_logits<V>(row, col, experts, l);
-            load_bias<V>(bias, col, experts, b);
+        for (int col = lane * V, turn = 0; turn == 0 || col < columns; col += G * V, ++turn) {
+            float l[V], r[V];
+            load_logits<V>(row, col, columns, l);
+            add_bias<V>(bias, col, columns, l, r);
 #pragma unroll
             for (int c = 0; c < V; c += K) {
                 double some[K];
 #pragma unroll
-                for (int i = 0; i < K; ++i) {
-                    const float r = l[c + i] + b[c + i];
-                    some[i] = rank_of(r, col + c + i);
-                    if (r > -INFINITY) top = fmaxf(top, l[c + i]);
-                }
+                for (int i = 0; i < K; ++i) some[i] = rank_of(r[c + i], col + c + i);
                 order_all(some);
-                keep_first(first, some);
+                if (turn == 0 && c == 0) {
+#pragma unroll
+                    for (int i = 0; i < K; ++i) first[i] = some[i];
+                } else {
+                    keep_first(first, some);
+                }
             }
         }
         keep_first_of_team<G>(first);
-        if (all) {
-            top = team_max<G>(top);
-            for (int col = lane * V; col < columns; col += G * V) {
-                float l[V], b[V];
-                load_logits<V>(row, col, experts, l);
-                load_bias<V>(bias, col, experts, b);
-#pragma unroll
-                for (int i = 0; i < V; ++i) total += l[i] + b[i] > -INFINITY ? expf(l[i] - top) : 0.0f;
-            }
-            total = team_sum<G>(total);
-        }
+        float top = 0.0f, total = 0.0f;
+        if (all) softmax_sums<V, G>(row, bias, lane, columns, top, total);
         double mine = closed();
 #pragma unroll
         for (int i = 0; i < K; ++i) mine = lane == i && i < k ? first[i] : mine;
@@ -357,25 +372,8 @@ __global__ __launch_bounds__(kRowThreads) void route_grad_kernel(const float* __
         const float l = valid ? (float)row[e] : 0.0f;
         const float g = valid ? scale * dweight[t * k + lane] : 0.0f;
         const bool any = team_max<G>(valid ? 1.0f : 0.0f) > 0.0f;
-        float top = -INFINITY, total = 0.0f;
-        if (all && any) {
-            for (int col = lane * V; col < experts; col += G * V) {
-                float x[V], b[V];
-                load_logits<V>(row, col, experts, x);
-                load_bias<V>(bias, col, experts, b);
-#pragma unroll
-                for (int i = 0; i < V; ++i) top = x[i] + b[i] > -INFINITY ? fmaxf(top, x[i]) : top;
-            }
-            top = team_max<G>(top);
-            for (int col = lane * V; col < experts; col += G * V) {
-                float x[V], b[V];
-                load_logits<V>(row, col, experts, x);
-                load_bias<V>(bias, col, experts, b);
-#pragma unroll
-                for (int i = 0; i < V; ++i) total += x[i] + b[i] > -INFINITY ? expf(x[i] - top) : 0.0f;
-            }
-            total = team_sum<G>(total);
-        }
+        float top = 0.0f, total = 0.0f;
+        if (all && any) softmax_sums<V, G>(row, bias, lane, experts, top, total);
         const float w = slot_weight<G>(l, valid, score, normalise, top, total);
         const float mean = team_sum<G>(g * w);
         float d;  // of the slot's logit
@@ -384,11 +382,11 @@ __global__ __launch_bounds__(kRowThreads) void route_grad_kernel(const float* __
         for (int col = lane * V; col < experts; col += G * V) {
             float x[V] = {};
             if (all && any) {
-                float b[V];
+                float r[V];
                 load_logits<V>(row, col, experts, x);
-                load_bias<V>(bias, col, experts, b);
+                add_bias<V>(bias, col, experts, x, r);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = x[i] + b[i] > -INFINITY ? expf(x[i] - top) / total * -mean : 0.0f;
+                for (int i = 0; i < V; ++i) x[i] = r[i] > -INFINITY ? expf(x[i] - top) / total * -mean : 0.0f;
             }
             if (col + V <= experts) {
                 store_vec<V, T>(to + col, rounded_vec<T, V>(x), false);
