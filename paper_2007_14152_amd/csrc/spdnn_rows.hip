@@ -365,10 +365,12 @@ int spdnn_route_grad(const float* dweight, const void* logits, int32_t type, int
     if (rows == 0) return SPDNN_OK;
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
-        with_team<SPDNN_MAX_CHOSEN>(rows, [&](auto gg) {
+        const auto run = [&](auto gg) {
             constexpr int G = decltype(gg)::value;
             spdnn::route_grad_kernel<T, G><<<groups((rows - 1) / (spdnn::kRowThreads / G) + 1), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>(dweight, (const T*)logits, stride, chosen, rows, experts, k, bias, score, normalise, scale, (T*)dlogits, dstride);
-        });
+        };
+        if (k <= 8) with_team<8>(rows, run);  // a lane per slot
+        else with_team<16>(rows, run);
     });
     return launched();
 }

@@ -279,6 +279,10 @@ __device__ inline void add_bias(const float* __restrict__ bias, int col, int exp
     }
 }
 
+// exp(x) for x <= 0 in two instructions: x log2(e) is rounded at the size of x, as the logit it came from was, and what is below
+// 2^-126 becomes zero.
+__device__ inline float exp_fast(float x) { return __expf(x); }
+
 // The largest open logit of a team's row, and the sum of exp(logit - the largest) over the open ones.
 template <int V, int G, typename T>
 __device__ inline void softmax_sums(const T* __restrict__ row, const float* __restrict__ bias, int lane, int columns, float& top, float& total) {
@@ -297,7 +301,7 @@ __device__ inline void softmax_sums(const T* __restrict__ row, const float* __re
         load_logits<V>(row, col, columns, l);
         add_bias<V>(bias, col, columns, l, r);
 #pragma unroll
-        for (int i = 0; i < V; ++i) total += r[i] > -INFINITY ? expf(l[i] - top) : 0.0f;
+        for (int i = 0; i < V; ++i) total += r[i] > -INFINITY ? exp_fast(l[i] - top) : 0.0f;
     }
     total = team_sum<G>(total);
 }
@@ -352,48 +356,68 @@ __global__ __launch_bounds__(kRowThreads) void route_kernel(const T* __restrict_
     }
 }
 
-// A team of G lanes takes a row: the slots' weights and their gradient, then all of the row but for the chosen experts, then those.
-constexpr int kGradLogits = 4;
+// A team of G lanes takes a row: the slots' weights and their gradient, then all of the row but for the chosen experts, then
+// those.  Softmax over the open experts needs all of the row; a row of at most G * kLogits logits is read once and stays in
+// registers as exp(logit - top).
 template <typename T, int G>
 __global__ __launch_bounds__(kRowThreads) void route_grad_kernel(const float* __restrict__ dweight, const T* __restrict__ logits, int64_t stride,
                                                                  const int32_t* __restrict__ chosen, int rows, int experts, int k,
                                                                  const float* __restrict__ bias, int score, int normalise, float scale,
                                                                  T* __restrict__ dlogits, int64_t dstride) {
-    static_assert(G >= SPDNN_MAX_CHOSEN);
-    constexpr int V = kGradLogits, kTeams = kRowThreads / G;
+    constexpr int V = kLogits, kTeams = kRowThreads / G;
     const int lane = threadIdx.x % G, team = threadIdx.x / G;
-    const bool all = score == SPDNN_SOFTMAX && !normalise;
+    const bool all = score == SPDNN_SOFTMAX && !normalise, one = experts <= G * V;
     for (int64_t t0 = (int64_t)blockIdx.x * kTeams; t0 < rows; t0 += (int64_t)gridDim.x * kTeams) {
         const int64_t t = min(t0 + team, (int64_t)rows - 1);
         const T* row = logits + t * stride;
         T* to = dlogits + t * dstride;
+        float x[V];
+        if (all && one) load_logits<V>(row, lane * V, experts, x);
         const int e = lane < k ? chosen[t * k + lane] : -1;
         const bool valid = e >= 0 && e < experts;
-        const float l = valid ? (float)row[e] : 0.0f;
         const float g = valid ? scale * dweight[t * k + lane] : 0.0f;
+        const float l = valid ? (float)row[e] : 0.0f;
         const bool any = team_max<G>(valid ? 1.0f : 0.0f) > 0.0f;
         float top = 0.0f, total = 0.0f;
-        if (all && any) softmax_sums<V, G>(row, bias, lane, experts, top, total);
+        if (all && one) {
+            float r[V];
+            add_bias<V>(bias, lane * V, experts, x, r);
+            top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = r[i] > -INFINITY ? fmaxf(top, x[i]) : top;
+            top = team_max<G>(top);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                x[i] = r[i] > -INFINITY ? exp_fast(x[i] - top) : 0.0f;
+                total += x[i];
+            }
+            total = team_sum<G>(total);
+        } else if (all) {
+            softmax_sums<V, G>(row, bias, lane, experts, top, total);
+        }
         const float w = slot_weight<G>(l, valid, score, normalise, top, total);
-        const float mean = team_sum<G>(g * w);
+        const float mean = team_sum<G>(g * w), back = any ? -mean / total : 0.0f;
         float d;  // of the slot's logit
         if (normalise) d = w * (g - mean) * (score == SPDNN_SIGMOID ? sigmoid(-l) : 1.0f);
         else d = score == SPDNN_SIGMOID ? g * w * sigmoid(-l) : w * (g - mean);
         for (int col = lane * V; col < experts; col += G * V) {
-            float x[V] = {};
-            if (all && any) {
+            float y[V] = {};
+            if (all && one) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = any ? x[i] * back : 0.0f;
+            } else if (all) {
                 float r[V];
                 load_logits<V>(row, col, experts, x);
                 add_bias<V>(bias, col, experts, x, r);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = r[i] > -INFINITY ? expf(x[i] - top) / total * -mean : 0.0f;
+                for (int i = 0; i < V; ++i) y[i] = any && r[i] > -INFINITY ? exp_fast(x[i] - top) * back : 0.0f;
             }
             if (col + V <= experts) {
-                store_vec<V, T>(to + col, rounded_vec<T, V>(x), false);
+                store_vec<V, T>(to + col, rounded_vec<T, V>(y), false);
             } else {
 #pragma unroll
                 for (int i = 0; i < V; ++i)
-                    if (col + i < experts) to[col + i] = rounded<T>(x[i]);
+                    if (col + i < experts) to[col + i] = rounded<T>(y[i]);
             }
         }
         // The wave's stores to one address keep their order, whichever lanes they come from.

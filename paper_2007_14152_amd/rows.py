@@ -61,42 +61,39 @@ _F32 = (torch.float32,)
 _I32 = (torch.int32,)
 _BYTES = (torch.bool, torch.uint8)
 
-# The raw handle of a device's current stream.  (torch.cuda.current_stream makes an object around it first, which takes 1.9 us;
-# the smallest call there is takes 4.5.)
+# The number of the current device, and the raw handle of a device's current stream.  (torch.cuda.current_stream makes an object
+# around it first, which takes 1.9 us; the smallest call there is takes 4.5.)
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _on_device(f):
-    """f with the device of its first argument made current, if it is not."""
-    @functools.wraps(f)
-    def call(t, *args, **kwargs):
-        if t.is_cuda and t.device.index != torch.cuda.current_device():
-            with torch.cuda.device(t.device):
-                return f(t, *args, **kwargs)
-        return f(t, *args, **kwargs)
-    return call
+@functools.lru_cache(maxsize=64)
+def _work_bytes(name, *sizes):
+    need = ctypes.c_size_t()
+    _check(getattr(lib(), name)(*sizes, ctypes.byref(need)))
+    return need.value
 
 
-@_on_device
 def embed(table, ids, scale=1.0, dtype=None):
     """scale * table[ids], rows of zeros for ids outside the table (padding): [*ids.shape, width] of dtype (the table's).
 
     table: float32, bfloat16 or float16 [vocab, width]; ids: int32 or int64 of any shape."""
     ttype, tstride = _rows(table, "table")
     vocab, width = table.shape
-    dtype = dtype or table.dtype
-    otype = _type(dtype, "dtype")
+    otype = ttype if dtype is None else _type(dtype, "dtype")
     dev = table.device
+    if dev.index != _current():
+        with torch.cuda.device(dev):
+            return embed(table, ids, scale, dtype)
     if ids.dtype not in _IDS or ids.device != dev:
         _refuse("ids: int32 or int64 on %s, not %s on %s", dev, ids.dtype, ids.device)
     ids = ids.contiguous()
-    out = torch.empty((*ids.shape, width), dtype=dtype, device=dev)
+    out = table.new_empty((*ids.shape, width), dtype=dtype)
     _check(lib().spdnn_embed(table.data_ptr(), ttype, vocab, width, tstride, ids.data_ptr(), _IDS[ids.dtype], ids.numel(),
                              scale, out.data_ptr(), otype, width, _stream(dev.index)))
     return out
 
 
-@_on_device
 def embed_grad(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
     """Gradient of embed's table, [vocab, width]: scale * the sum of dout's rows of each id.
 
@@ -108,19 +105,21 @@ def embed_grad(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
     itype, dstride = _rows(dout, "dout")
     n, width = dout.shape
     dev = dout.device
+    if dev.index != _current():
+        with torch.cuda.device(dev):
+            return embed_grad(dout, ids, vocab, scale, dtype, out)
     if ids.dtype not in _IDS or ids.device != dev or ids.numel() != n:
         _refuse("ids: %d of int32 or int64 on %s, not %d of %s on %s", n, dev, ids.numel(), ids.dtype, ids.device)
     ids = ids.contiguous()
     add = out is not None
+    need = _work_bytes("spdnn_embed_grad_bytes", vocab, width, n)
     if not add:
         _type(dtype, "dtype")
-        out = torch.empty((vocab, width), dtype=dtype, device=dev)
+        out = dout.new_empty((vocab, width), dtype=dtype)
     otype, ostride = _rows(out, "out", dev, (vocab, width))
-    need = ctypes.c_size_t()
-    _check(lib().spdnn_embed_grad_bytes(vocab, width, n, ctypes.byref(need)))
-    work = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    work = dout.new_empty(need, dtype=torch.uint8) if need else None
     _check(lib().spdnn_embed_grad(dout.data_ptr(), itype, dstride, ids.data_ptr(), _IDS[ids.dtype], n, vocab, width, scale, add,
-                                  out.data_ptr(), otype, ostride, work.data_ptr() if need.value else 0, need.value, _stream(dev.index)))
+                                  out.data_ptr(), otype, ostride, work.data_ptr() if need else 0, need, _stream(dev.index)))
     return out
 
 
@@ -130,7 +129,6 @@ def _score(score):
     return _SCORES[score]
 
 
-@_on_device
 def route(logits, k, bias=None, keep=None, score="softmax", normalise=True, scale=1.0):
     """(chosen int32 [rows, k], weight float32 [rows, k]): the k experts of each row with the largest logits (plus bias,
     which only the choice sees), and their weights; -1 and 0 where a row has no expert left.
@@ -139,35 +137,39 @@ def route(logits, k, bias=None, keep=None, score="softmax", normalise=True, scal
     ltype, stride = _rows(logits, "logits")
     rows, experts = logits.shape
     dev = logits.device
+    if dev.index != _current():
+        with torch.cuda.device(dev):
+            return route(logits, k, bias, keep, score, normalise, scale)
     bp = _array(bias, "bias", _F32, dev, (experts,))
     kp = _array(keep, "keep", _BYTES, dev, (rows,))
-    chosen = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
-    weight = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
+    chosen = logits.new_empty((rows, max(k, 0)), dtype=torch.int32)
+    weight = logits.new_empty((rows, max(k, 0)), dtype=torch.float32)
     _check(lib().spdnn_route(logits.data_ptr(), ltype, stride, rows, experts, k, bp, kp, _score(score), normalise, scale,
                              chosen.data_ptr(), weight.data_ptr(), _stream(dev.index)))
     return chosen, weight
 
 
-@_on_device
 def route_grad(dweight, logits, chosen, bias=None, score="softmax", normalise=True, scale=1.0):
     """Gradient of route's weights with respect to the logits, of the logits' type; chosen, bias, score, normalise and scale
     as they were there."""
     ltype, stride = _rows(logits, "logits")
     rows, experts = logits.shape
     dev = logits.device
+    if dev.index != _current():
+        with torch.cuda.device(dev):
+            return route_grad(dweight, logits, chosen, bias, score, normalise, scale)
     if chosen.dim() != 2:
         _refuse("chosen: a matrix, not %s", tuple(chosen.shape))
     k = chosen.shape[1]
     bp = _array(bias, "bias", _F32, dev, (experts,))
     cp = _array(chosen, "chosen", _I32, dev, (rows, k))
     wp = _array(dweight, "dweight", _F32, dev, (rows, k))
-    out = torch.empty((rows, experts), dtype=logits.dtype, device=dev)
+    out = logits.new_empty((rows, experts))
     _check(lib().spdnn_route_grad(wp, logits.data_ptr(), ltype, stride, cp, rows, experts, k, bp, _score(score), normalise,
                                   scale, out.data_ptr(), experts, _stream(dev.index)))
     return out
 
 
-@_on_device
 def dispatch(x, chosen, experts):
     """(xs [rows * k, width], offsets int32 [experts + 1], place int32 [rows, k]): x's rows sorted by expert, once for each
     expert they go to.  Expert e has the rows offsets[e] .. offsets[e + 1] of xs; row t's copy for its slot j is row
@@ -175,25 +177,29 @@ def dispatch(x, chosen, experts):
     xtype, xstride = _rows(x, "x")
     rows, width = x.shape
     dev = x.device
+    if dev.index != _current():
+        with torch.cuda.device(dev):
+            return dispatch(x, chosen, experts)
     if chosen.dim() != 2:
         _refuse("chosen: a matrix, not %s", tuple(chosen.shape))
     k = chosen.shape[1]
     cp = _array(chosen, "chosen", _I32, dev, (rows, k))
-    need = ctypes.c_size_t()
-    _check(lib().spdnn_dispatch_bytes(rows, k, experts, ctypes.byref(need)))
-    xs = torch.empty((rows * k, width), dtype=x.dtype, device=dev)
-    offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev)
-    place = torch.empty((rows, k), dtype=torch.int32, device=dev)
-    work = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    need = _work_bytes("spdnn_dispatch_bytes", rows, k, experts)
+    xs = x.new_empty((rows * k, width))
+    offsets = chosen.new_empty(experts + 1)
+    place = chosen.new_empty((rows, k))
+    work = x.new_empty(need, dtype=torch.uint8) if need else None
     _check(lib().spdnn_dispatch(cp, rows, k, experts, x.data_ptr(), xtype, width, xstride, xs.data_ptr(), width, offsets.data_ptr(),
-                                place.data_ptr(), work.data_ptr() if need.value else 0, need.value, _stream(dev.index)))
+                                place.data_ptr(), work.data_ptr() if need else 0, need, _stream(dev.index)))
     return xs, offsets, place
 
 
-@_on_device
 def _back(ys, place, weight, add):
     ytype, ystride = _rows(ys, "ys")
     dev = ys.device
+    if dev.index != _current():
+        with torch.cuda.device(dev):
+            return _back(ys, place, weight, add)
     if place.dim() != 2:
         _refuse("place: a matrix, not %s", tuple(place.shape))
     rows, k = place.shape
@@ -208,7 +214,7 @@ def _back(ys, place, weight, add):
         if atype != ytype:
             _refuse("add: %s, not %s", ys.dtype, add.dtype)
         ap = add.data_ptr()
-    out = torch.empty((rows, width), dtype=ys.dtype, device=dev)
+    out = ys.new_empty((rows, width))
     _check(lib().spdnn_combine(ys.data_ptr(), ytype, width, ystride, pp, wp, rows, k, ap, astride, out.data_ptr(), width,
                                _stream(dev.index)))
     return out
@@ -227,12 +233,14 @@ def dispatch_grad(dxs, place):
     return _back(dxs, place, None, None)
 
 
-@_on_device
 def combine_grad(dout, ys, place, weight, offsets):
     """(dys, dweight): gradients of combine with respect to ys and weight (that of add is dout).  offsets as dispatch gave
     them: rows of dys without a pair are zero."""
     ytype, ystride = _rows(ys, "ys")
     dev = ys.device
+    if dev.index != _current():
+        with torch.cuda.device(dev):
+            return combine_grad(dout, ys, place, weight, offsets)
     if place.dim() != 2:
         _refuse("place: a matrix, not %s", tuple(place.shape))
     rows, k = place.shape
@@ -249,8 +257,8 @@ def combine_grad(dout, ys, place, weight, offsets):
     if offsets.dim() != 1 or offsets.shape[0] < 2:
         _refuse("offsets: one per expert and the end, not %s", tuple(offsets.shape))
     op = _array(offsets, "offsets", _I32, dev, tuple(offsets.shape))
-    dys = torch.empty((rows * k, width), dtype=ys.dtype, device=dev)
-    dweight = torch.empty((rows, k), dtype=torch.float32, device=dev)
+    dys = ys.new_empty((rows * k, width))
+    dweight = weight.new_empty((rows, k))
     _check(lib().spdnn_combine_grad(dout.data_ptr(), ytype, width, gstride, ys.data_ptr(), ystride, pp, wp,
                                     op + 4 * (offsets.shape[0] - 1), rows, k, dys.data_ptr(), width, dweight.data_ptr(),
                                     _stream(dev.index)))
