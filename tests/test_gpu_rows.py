@@ -161,6 +161,37 @@ def test_embed_grad_ids_that_gather(sp, which, n):
     assert np.array_equal(ref.f64(got), want)
 
 
+@pytest.mark.parametrize("n,vocab,width", [(300000, 1 << 20, 3), (270000, 1000, 8), (2049, (1 << 21) + 5, 1), (1024, 3, 70000),
+                                           (1025, 3, 70000), (70000, 40, 12)])
+def test_embed_grad_large(sp, n, vocab, width):
+    """More chunks than one workgroup adds up at once, three digits, rows longer than a tile, runs of thousands.  Whole numbers:
+    every sum is exact."""
+    g = torch.Generator().manual_seed(n)
+    dout = torch.randint(-4, 5, (n, width), generator=g).float()
+    ids = torch.randint(-1, vocab, (n,), generator=g)
+    ids[: n // 3] = vocab // 2
+    want = torch.zeros(vocab + 1, width, dtype=torch.float64).index_add_(0, torch.where(ids < 0, vocab, ids), dout.double())
+    got = sp.embed_grad(dout.to(DEV), ids.to(DEV), vocab)
+    assert torch.equal(got.cpu().double(), want[:vocab])
+
+
+@pytest.mark.parametrize("rows,k,experts,width", [(140000, 2, 1024, 2), (60000, 5, 7, 4), (1, 16, 16, 40000), (64, 16, 64, 9000), (65, 16, 64, 9000)])
+def test_dispatch_and_combine_large(sp, rows, k, experts, width):
+    """Chunks longer than the least, rows longer than a tile, both sides of the single launch's limit."""
+    chosen = pairs(rows, rows, k, experts)
+    x = torch.randint(-9, 10, (rows, width), generator=torch.Generator().manual_seed(1)).float().to(DEV)
+    xs, offsets, place = sp.dispatch(x, chosen, experts)
+    want_place, want_offsets = ref.sort_pairs(chosen.cpu().numpy(), experts)
+    assert np.array_equal(place.cpu().numpy(), want_place) and np.array_equal(offsets.cpu().numpy(), want_offsets)
+    used = int(want_offsets[-1])
+    assert not xs[used:].any()
+    there = (place >= 0).sum(1, keepdim=True)
+    assert torch.equal(sp.dispatch_grad(xs, place), x * there)  # whole numbers: exact
+    dys, dweight = sp.combine_grad(x, xs, place, torch.full((rows, k), 2.0, device=DEV), offsets)
+    assert torch.equal(dys, 2 * xs)
+    assert torch.equal(dweight, torch.where(place >= 0, (x * x).sum(1, keepdim=True), 0.0))
+
+
 def test_embed_grad_leaves_masked_rows_out(sp):
     """What stands in rows of padding does not matter, and an id's infinity stays with it."""
     dout = normal(1, (300, 20), F32)
