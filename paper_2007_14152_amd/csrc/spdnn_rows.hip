@@ -79,6 +79,7 @@ spdnn::Tiles tiles(int64_t rows, int32_t width, int v, int unroll, int64_t out_b
     g.vecs = (width - 1) / v + 1;
     g.slab = std::min(g.vecs, spdnn::kTileVecs);
     g.past = out_bytes >= kPastBytes;
+    g.past_in = false;
     g.per = 1;
     double best = 0;
     const int64_t turn = unroll * spdnn::kRowThreads;
@@ -435,7 +436,8 @@ int spdnn_combine(const void* ys, int32_t type, int32_t width, int64_t ys_stride
         using T = decltype(tt);
         with_vec<16 / sizeof(T)>(width, [&](auto v) {
             constexpr int V = decltype(v)::value;
-            const spdnn::Tiles g = tiles(rows, width, V, spdnn::kCombineVecs, (int64_t)rows * width * sizeof(T));
+            spdnn::Tiles g = tiles(rows, width, V, spdnn::kCombineVecs, (int64_t)rows * width * sizeof(T));
+            g.past_in = (int64_t)n * width * (int64_t)sizeof(T) >= kPastBytes;
             const auto run = [&](auto j, auto weighted) {
                 spdnn::combine_kernel<T, V, decltype(j)::value, decltype(weighted)::value><<<groups(g), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>(g, (const T*)ys, ys_stride, place, weight, k, (const T*)add, add_stride, (T*)out, out_stride);
             };

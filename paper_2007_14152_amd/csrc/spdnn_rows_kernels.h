@@ -36,6 +36,7 @@ struct Tiles {
     int32_t slab;    // vectors of a row in a tile
     uint32_t magic;  // ceil(2^32 / slab): quotients by slab > 1 for what is less than 2^16
     bool past;       // stores that leave nothing in the caches
+    bool past_in;    // and loads (of the input that is as large as all that)
 };
 constexpr int kTileVecs = 4096;  // at most, of a tile
 
@@ -48,8 +49,20 @@ __device__ inline Pack<T, V> load_vec(const T* p) {
     if constexpr (V == 1) return Pack<T, V>(*p);
     else return *reinterpret_cast<const Pack<T, V>*>(p);
 }
-// past: the same for all lanes.  The empty asm on both sides of that branch keeps the compiler from making one store of the two,
+// past: the same for all lanes.  The empty asm on both sides of that branch keeps the compiler from making one access of the two,
 // an ordinary one.
+template <int V, typename T>
+__device__ inline Pack<T, V> load_vec(const T* p, bool past) {
+    Pack<T, V> x;
+    if (past) {
+        asm volatile("");
+        x = __builtin_nontemporal_load(reinterpret_cast<const Pack<T, V>*>(p));
+        asm volatile("");
+    } else {
+        x = *reinterpret_cast<const Pack<T, V>*>(p);
+    }
+    return x;
+}
 template <int V, typename T>
 __device__ inline void store_vec(T* p, Pack<T, V> x, bool past) {
     if (past) {
@@ -1038,7 +1051,7 @@ __global__ __launch_bounds__(kRowThreads) void combine_kernel(Tiles g, const T* 
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int j = 0; j < J; ++j)
-                    if (from[u][j] >= 0) y[u][j] = load_vec<V>(ys + (int64_t)from[u][j] * ys_stride + at[u].col);
+                    if (from[u][j] >= 0) y[u][j] = load_vec<V, T>(ys + (int64_t)from[u][j] * ys_stride + at[u].col, g.past_in);
             if (add && j0 == 0) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) r[u] = load_vec<V>(add + at[u].row * add_stride + at[u].col);
@@ -1111,7 +1124,7 @@ __global__ __launch_bounds__(kRowThreads) void combine_grad_kernel(const T* __re
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int j = 0; j < J; ++j)
-                        if (at[j] >= 0) y[u][j] = load_vec<V>(ys + (int64_t)at[j] * ys_stride + col[u]);
+                        if (at[j] >= 0) y[u][j] = load_vec<V, T>(ys + (int64_t)at[j] * ys_stride + col[u], past);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
