@@ -167,8 +167,6 @@ void with_places(int32_t k, F f) {
     else f(std::integral_constant<int, 4>{});
 }
 
-constexpr int32_t kFewRows = 1024;
-
 // f(K), k rounded up to a power of two.
 template <typename F>
 void with_chosen(int32_t k, F f) {
@@ -179,12 +177,22 @@ void with_chosen(int32_t k, F f) {
     else f(std::integral_constant<int, 16>{});
 }
 
-// f(G) with the lanes that take a row of logits: G0, or a wave where there are few rows.
+// f(G) with the lanes that take a row of logits, at least G0: so many that a lane has kLogits of them, but a wave at most.  (The
+// gradient through a softmax over 256 logits, which then reads its row once: 16384 rows 10.7 us with 8 lanes, 9.0 with 32.)
 template <int G0, typename F>
-void with_team(int32_t rows, F f) {
-    if (rows > kFewRows) f(std::integral_constant<int, G0>{});
+void with_team(int32_t experts, F f) {
+    if constexpr (G0 <= 8) {
+        if (experts <= 8 * spdnn::kLogits) return f(std::integral_constant<int, 8>{});
+    }
+    if (experts <= 16 * spdnn::kLogits) f(std::integral_constant<int, 16>{});
+    else if (experts <= 32 * spdnn::kLogits) f(std::integral_constant<int, 32>{});
     else f(std::integral_constant<int, 64>{});
 }
+
+// Up to so many rows the lanes of a route_kernel team are as many as the logits ask for; above, as few as the slots allow, for what
+// the lanes do together (merge lists) costs a wave the same whether it has one row or eight.  256 logits, 8 experts, 8 lanes and 32:
+// 64 rows 4.2 and 3.4 us, 2048 rows 4.4 and 3.6, 4096 rows 4.5 and 4.3, 16384 rows 5.9 and 9.3.
+constexpr int32_t kFewRows = 4096;
 
 int launched() {
     HIP_TRY(hipGetLastError());
@@ -346,10 +354,13 @@ int spdnn_route(const void* logits, int32_t type, int64_t stride, int32_t rows, 
         using T = decltype(tt);
         with_chosen(k, [&](auto kk) {
             constexpr int K = decltype(kk)::value;
-            with_team<(K > 8 ? K : 8)>(rows, [&](auto gg) {
+            constexpr int G0 = K > 8 ? K : 8;
+            const auto run = [&](auto gg) {
                 constexpr int G = decltype(gg)::value;
                 spdnn::route_kernel<T, K, G><<<groups((rows - 1) / (spdnn::kRowThreads / G) + 1), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>((const T*)logits, stride, rows, experts, k, bias, keep, score, normalise, scale, chosen, weight);
-            });
+            };
+            if (rows > kFewRows) run(std::integral_constant<int, G0>{});
+            else with_team<G0>(experts, run);
         });
     });
     return launched();
@@ -370,8 +381,8 @@ int spdnn_route_grad(const float* dweight, const void* logits, int32_t type, int
             constexpr int G = decltype(gg)::value;
             spdnn::route_grad_kernel<T, G><<<groups((rows - 1) / (spdnn::kRowThreads / G) + 1), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>(dweight, (const T*)logits, stride, chosen, rows, experts, k, bias, score, normalise, scale, (T*)dlogits, dstride);
         };
-        if (k <= 8) with_team<8>(rows, run);  // a lane per slot
-        else with_team<16>(rows, run);
+        if (k <= 8) with_team<8>(experts, run);  // a lane per slot
+        else with_team<16>(experts, run);
     });
     return launched();
 }
@@ -475,8 +486,10 @@ int spdnn_combine_grad(const void* dout, int32_t type, int32_t width, int64_t do
                 spdnn::combine_grad_kernel<T, V, decltype(j)::value, L><<<groups((rows - 1) / (spdnn::kRowThreads / L) + 1), spdnn::kRowThreads, 0, (hipStream_t)hip_stream>>>((const T*)dout, dout_stride, (const T*)ys, ys_stride, place, weight, count, rows, k, width, (T*)dys, dys_stride, dweight, past);
             };
             with_places(k, [&](auto j) {
-                if (vecs <= 32) run(j, std::integral_constant<int, 16>{});
-                else if (rows >= 2048) run(j, std::integral_constant<int, 64>{});
+                // bf16, 4 experts, with 16, 64 and 256 lanes: 20000 rows of 512 30.1, 32.9 and 72 us; 4000 of 1024 15.4, 13.4 and
+                // 21.3; 4000 of 2048 28.0, 24.6 and 28.3; 8000 of 4096 115, 117 and 103; 512 of 4096 31.5, 11.2 and 8.3
+                if (vecs <= 64) run(j, std::integral_constant<int, 16>{});
+                else if (vecs <= 256) run(j, std::integral_constant<int, 64>{});
                 else run(j, std::integral_constant<int, 256>{});
             });
         });

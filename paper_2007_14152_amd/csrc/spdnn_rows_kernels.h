@@ -467,6 +467,7 @@ struct SortLds {
     int32_t start[WAVES][BINS];
     int32_t total[BINS];
     int32_t wave_sum[WAVES];
+    int32_t end;  // behind the last position
 };
 
 // Rows first .. last - 1 of a matrix whose elements become zero, by workgroups that a launch has to spare.
@@ -592,7 +593,10 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
             if (offsets) offsets[e] = base;
             for (int w = 0; w < WAVES; ++w) lds.start[w][e] += base;
             base += many[i];
-            if (offsets && e == bins - 1) offsets[bins] = base;
+            if (e == bins - 1) {
+                lds.end = base;
+                if (offsets) offsets[bins] = base;
+            }
         }
     }
     __syncthreads();
@@ -1014,16 +1018,13 @@ __global__ __launch_bounds__(kRowThreads) void dispatch_few_kernel(Tiles g, cons
                                                                    int64_t xs_stride) {
     __shared__ SortLds<kRowThreads / 64> lds;
     __shared__ int32_t places[kFewPairs];
-    __shared__ int32_t used;
     const bool first = blockIdx.x == 0 && blockIdx.y == 0;
-    if (threadIdx.x == 0) used = 0;
     place_chunk(in, 0, g.rows * k, in.experts, nullptr, 1, 0, lds, first ? offsets : nullptr, [&](int64_t p, int32_t, int at) {
         places[p] = at;
-        if (at >= 0) atomicMax(&used, at + 1);
         if (first) place[p] = at;
     });
     __syncthreads();
-    dispatch_rows<T, V>(g, x, x_stride, k, places, used, xs, xs_stride);
+    dispatch_rows<T, V>(g, x, x_stride, k, places, lds.end, xs, xs_stride);
 }
 
 // out[t] = add[t] + sum of weight[t][j] * ys[place[t][j]], j ascending, one fused multiply-add each.
