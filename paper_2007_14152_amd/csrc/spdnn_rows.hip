@@ -65,13 +65,15 @@ int check_work(const void* work, size_t bytes, size_t need) {
 
 dim3 groups(int64_t n) { return dim3((unsigned)std::max<int64_t>(1, std::min(n, kMostGroups))); }
 
-// Outputs of this many bytes go past the caches, for whoever reads them next does not find them there (256 MB at the most) anyway.
-// Rows of 4096 bf16 by id, alone and with a kernel behind that reads them, through -> past: 400 MB 128 -> 117 and 266 -> 256 us,
-// 200 MB 70 -> 62 and 141 -> 137, 128 MB 42 -> 41 and 83 -> 87, 16 MB 10.4 -> 11.8 and 15.9 -> 17.5.
+// Outputs of this many bytes go past the caches, for whoever reads them next does not find them there (256 MB at the most) anyway,
+// and so do inputs that are read once.  Rows of 4096 bf16 by id, alone and with a kernel behind that reads them, through -> past:
+// 400 MB 128 -> 117 and 266 -> 256 us, 200 MB 70 -> 62 and 141 -> 137, 128 MB 42 -> 41 and 83 -> 87, 16 MB 10.4 -> 11.8 and
+// 15.9 -> 17.5.  combine of 4 such rows each, its input through -> past: 512 MB 128 -> 112 us, 256 MB 64 -> 60, 128 MB 28.5 -> 35.6.
 constexpr int64_t kPastBytes = 160 << 20;
 
-// Tiles of rows x width elements in vectors of v, out_bytes of output in all: as many rows to a tile as fill its workgroup's turns best, but not so many
-// that less than two workgroups per CU are left.
+// Tiles of rows x width elements in vectors of v, `unroll` a lane at a time, out_bytes of output in all: as many rows to a tile as
+// fill its workgroup's turns best, but not so many that less than two workgroups per CU are left.
+constexpr int64_t kTilesAtLeast = 512;
 spdnn::Tiles tiles(int64_t rows, int32_t width, int v, int unroll, int64_t out_bytes) {
     spdnn::Tiles g;
     g.rows = rows;
@@ -81,16 +83,17 @@ spdnn::Tiles tiles(int64_t rows, int32_t width, int v, int unroll, int64_t out_b
     g.past = out_bytes >= kPastBytes;
     g.past_in = false;
     g.per = 1;
+    const int64_t turn = unroll * spdnn::kRowThreads;  // vectors that a workgroup takes at a time
     double best = 0;
-    const int64_t turn = unroll * spdnn::kRowThreads;
-    for (int64_t per = 1; per * g.slab <= spdnn::kTileVecs && (per == 1 || rows / per >= 512); ++per) {
-        const int64_t turns = (per * g.slab + turn - 1) / turn;
-        const double full = (double)(per * g.slab) / (double)(turns * turn);
+    const auto consider = [&](int64_t per) {
+        const double full = (double)(per * g.slab) / (double)((per * g.slab + turn - 1) / turn * turn);
         if (full > best + 0.02) {
             best = full;
             g.per = (int32_t)per;
         }
-    }
+    };
+    consider(1);
+    for (int64_t vecs = turn; vecs <= spdnn::kTileVecs; vecs += turn) consider(std::max<int64_t>(1, std::min(vecs / g.slab, rows / kTilesAtLeast)));
     g.magic = (uint32_t)(((1ull << 32) + g.slab - 1) / g.slab);
     return g;
 }
