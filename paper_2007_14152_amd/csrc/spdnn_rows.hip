@@ -425,7 +425,8 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
             using T = decltype(tt);
             with_vec<16 / sizeof(T)>(width, [&](auto v) {
                 constexpr int V = decltype(v)::value;
-                const spdnn::Tiles g = tiles(rows, width, V, spdnn::kDispatchVecs, (int64_t)n * width * sizeof(T));
+                spdnn::Tiles g = tiles(rows, width, V, spdnn::kDispatchVecs, (int64_t)n * width * sizeof(T));
+                g.past_in = (int64_t)rows * width * (int64_t)sizeof(T) >= kPastBytes;
                 if (few)
                     spdnn::dispatch_few_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, in, offsets, place, (T*)xs, xs_stride);
                 else

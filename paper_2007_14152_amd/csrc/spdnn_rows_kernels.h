@@ -1000,7 +1000,7 @@ __device__ inline void dispatch_rows(const Tiles& g, const T* __restrict__ x, in
     each_vec<V, U>(g, [&](const At (&at)[U]) {
         Pack<T, V> v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = load_vec<V>(x + at[u].row * x_stride + at[u].col);
+        for (int u = 0; u < U; ++u) v[u] = load_vec<V, T>(x + at[u].row * x_stride + at[u].col, g.past_in);
         for (int j0 = 0; j0 < k; j0 += J) {
             int to[U][J];
             load_places<J, U>(place, at, j0, k, g.rows * k, to);
