@@ -267,7 +267,7 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
                         const int64_t clear = accumulate ? 0 : std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
                         // as many workgroups for a token's columns as make kFewGroups in all
                         const int y = (int)std::max<int64_t>(1, std::min<int64_t>((vecs - 1) / 64 + 1, kFewGroups / std::max(n, 1)));
-                        spdnn::embed_grad_few_kernel<T, S, I, V><<<dim3((unsigned)(n + clear), (unsigned)y), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, n, per, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
+                        spdnn::embed_grad_short_kernel<T, S, I, V><<<dim3((unsigned)(n + clear), (unsigned)y), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, n, per, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
                     });
                 });
             });
@@ -428,7 +428,7 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
                 spdnn::Tiles g = tiles(rows, width, V, spdnn::kDispatchVecs, (int64_t)n * width * sizeof(T));
                 g.past_in = (int64_t)rows * width * (int64_t)sizeof(T) >= kPastBytes;
                 if (few)
-                    spdnn::dispatch_few_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, in, offsets, place, (T*)xs, xs_stride);
+                    spdnn::dispatch_short_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, in, offsets, place, (T*)xs, xs_stride);
                 else
                     spdnn::dispatch_rows_kernel<T, V><<<groups(g), spdnn::kRowThreads, 0, s>>>(g, (const T*)x, x_stride, k, place, offsets + experts, (T*)xs, xs_stride);
             });

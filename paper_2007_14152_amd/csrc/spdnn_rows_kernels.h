@@ -725,7 +725,7 @@ __device__ inline void add_rows(const T* __restrict__ dout, int64_t dout_stride,
 // them into 1000 rows of 1024 12 us, where the sort takes 19, but 4096 49 us, where it takes 26.
 constexpr int kFewIds = 1024, kMostRowsToClear = 1024;
 template <typename T, typename S, typename I, int V>
-__global__ __launch_bounds__(kRowThreads) void embed_grad_few_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
+__global__ __launch_bounds__(kRowThreads) void embed_grad_short_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
                                                                      int vocab, int width, int adders, int per, float scale, bool accumulate,
                                                                      S* __restrict__ dtable, int64_t dtable_stride, bool past) {
     constexpr int kWaves = kRowThreads / 64, kRounds = kFewIds / kRowThreads;
@@ -1028,7 +1028,7 @@ __global__ __launch_bounds__(kRowThreads) void dispatch_rows_kernel(Tiles g, con
 // experts, beside two launches (place, move): 32 rows 5.8 and 7.7 us, 128 rows 8.2 and 9.0; 1000 rows, 2 of 8: 10.6 and 8.1.
 constexpr int kFewPairs = 1024;
 template <typename T, int V>
-__global__ __launch_bounds__(kRowThreads) void dispatch_few_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k, PairItems in,
+__global__ __launch_bounds__(kRowThreads) void dispatch_short_kernel(Tiles g, const T* __restrict__ x, int64_t x_stride, int k, PairItems in,
                                                                    int32_t* __restrict__ offsets, int32_t* __restrict__ place, T* __restrict__ xs,
                                                                    int64_t xs_stride) {
     __shared__ SortLds<kRowThreads / 64> lds;
