@@ -5,6 +5,7 @@ import os
 import re
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -49,14 +50,22 @@ def _resource_usage(text):
 
 def build(verbose: bool = False, extra=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + ["-Rpass-analysis=kernel-resource-usage"] + list(extra) + SOURCES + ["-o", LIB]
-    if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
-    usage = _resource_usage(res.stderr)
-    if res.returncode != 0:
-        sys.stderr.write("\n".join(l for l in res.stderr.splitlines() if "kernel-resource-usage" not in l) + "\n")
-        raise subprocess.CalledProcessError(res.returncode, cmd)
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"] + list(extra)
+    objects = [os.path.splitext(src)[0] + ".o" for src in SOURCES]
+    cmds = [[hipcc] + flags + ["-Rpass-analysis=kernel-resource-usage", "-c", src, "-o", obj] for src, obj in zip(SOURCES, objects)]
+    with ThreadPoolExecutor(len(cmds)) as side_by_side:
+        runs = list(side_by_side.map(lambda cmd: subprocess.run(cmd, stderr=subprocess.PIPE, text=True), cmds))
+    usage = {}
+    for cmd, res in zip(cmds, runs):
+        if verbose:
+            print(" ".join(cmd))
+        if res.returncode != 0:
+            sys.stderr.write("\n".join(l for l in res.stderr.splitlines() if "kernel-resource-usage" not in l) + "\n")
+            raise subprocess.CalledProcessError(res.returncode, cmd)
+        usage.update(_resource_usage(res.stderr))
+    subprocess.run([hipcc] + HIPCC_FLAGS + objects + ["-o", LIB], check=True, stderr=subprocess.DEVNULL if not verbose else None)
+    for obj in objects:
+        os.remove(obj)
     # Kernels that issue their global loads as inline instructions keep the loaded values in registers
     # the compiler believes to be ready; a spill between load and wait would save stale data.
     for kernel in NO_SCRATCH_KERNELS:
