@@ -306,7 +306,7 @@ int spdnn_layer_passes(spdnn_t h, int32_t l, int32_t* passes);
  *
  * Rows are row-major with a stride in elements of their own (outputs: stride >= width; inputs: any stride >= 0, so that a
  * row may stand for many) and any alignment that the element type has.
- * Outputs must not overlap inputs.  Sizes may be 0 where a comment does not say more. */
+ * Outputs must not overlap inputs.  1 <= width <= 2^30; other sizes may be 0 where a comment does not say more. */
 enum { SPDNN_F32 = 0, SPDNN_BF16 = 1, SPDNN_F16 = 2 }; /* types of rows */
 enum { SPDNN_I32 = 0, SPDNN_I64 = 1 };                 /* types of token ids */
 enum { SPDNN_SOFTMAX = 0, SPDNN_SIGMOID = 1 };         /* how logits become weights */

@@ -16,6 +16,7 @@ using spdnn::fail;
 
 constexpr size_t kAlign = 256;
 constexpr int64_t kMostPairs = 1 << 30;   // rows * k
+constexpr int32_t kMostWidth = 1 << 30;   // columns: a vector beyond a row's end must not pass 32 bits
 constexpr int64_t kMostGroups = 1 << 20;  // workgroups of a launch; more rows take turns
 
 int size_of(int32_t type) { return type == SPDNN_F32 ? 4 : type == SPDNN_BF16 || type == SPDNN_F16 ? 2 : 0; }
@@ -43,6 +44,10 @@ int check_array(const char* what, const void* p, int64_t n, int size) {
         if (rc_ != SPDNN_OK) return rc_;   \
     } while (0)
 
+int check_width(int32_t width) {
+    if (width < 1 || width > kMostWidth) return fail(SPDNN_EINVAL, "need 1 <= width <= %d", kMostWidth);
+    return SPDNN_OK;
+}
 int check_pairs(int32_t rows, int32_t k, int32_t experts) {
     if (rows < 0) return fail(SPDNN_EINVAL, "rows < 0");
     if (k < 1 || k > SPDNN_MAX_CHOSEN) return fail(SPDNN_EINVAL, "need 1 <= k <= %d", SPDNN_MAX_CHOSEN);
@@ -208,7 +213,8 @@ extern "C" {
 
 int spdnn_embed(const void* table, int32_t table_type, int32_t vocab, int32_t width, int64_t table_stride, const void* ids,
                 int32_t ids_type, int32_t n, float scale, void* out, int32_t out_type, int64_t out_stride, void* hip_stream) {
-    if (vocab < 1 || width < 1 || n < 0) return fail(SPDNN_EINVAL, "need vocab >= 1, width >= 1, n >= 0");
+    if (vocab < 1 || n < 0) return fail(SPDNN_EINVAL, "need vocab >= 1, n >= 0");
+    CHECK(check_width(width));
     if (ids_type != SPDNN_I32 && ids_type != SPDNN_I64) return fail(SPDNN_EINVAL, "ids_type must be SPDNN_I32 or SPDNN_I64");
     CHECK(check_rows("table", table, table_type, vocab, width, table_stride, kRead));
     CHECK(check_rows("out", out, out_type, n, width, out_stride, kWritten));
@@ -234,7 +240,8 @@ int spdnn_embed(const void* table, int32_t table_type, int32_t vocab, int32_t wi
 
 int spdnn_embed_grad_bytes(int32_t vocab, int32_t width, int32_t n, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
-    if (vocab < 1 || width < 1 || n < 0) return fail(SPDNN_EINVAL, "need vocab >= 1, width >= 1, n >= 0");
+    if (vocab < 1 || n < 0) return fail(SPDNN_EINVAL, "need vocab >= 1, n >= 0");
+    CHECK(check_width(width));
     *bytes = GradWork(vocab, width, n).bytes;
     return SPDNN_OK;
 }
@@ -403,7 +410,7 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
                    size_t work_bytes, void* hip_stream) {
     size_t need = 0;
     CHECK(spdnn_dispatch_bytes(rows, k, experts, &need));
-    if (width < 1) return fail(SPDNN_EINVAL, "need width >= 1");
+    CHECK(check_width(width));
     const int n = rows * k;
     CHECK(check_rows("x", x, type, rows, width, x_stride, kRead));
     CHECK(check_rows("xs", xs, type, n, width, xs_stride, kWritten));
@@ -439,7 +446,7 @@ int spdnn_dispatch(const int32_t* chosen, int32_t rows, int32_t k, int32_t exper
 int spdnn_combine(const void* ys, int32_t type, int32_t width, int64_t ys_stride, const int32_t* place, const float* weight,
                   int32_t rows, int32_t k, const void* add, int64_t add_stride, void* out, int64_t out_stride, void* hip_stream) {
     CHECK(check_pairs(rows, k, 1));
-    if (width < 1) return fail(SPDNN_EINVAL, "need width >= 1");
+    CHECK(check_width(width));
     const int n = rows * k;
     CHECK(check_rows("ys", ys, type, n, width, ys_stride, kRead));
     CHECK(check_rows("out", out, type, rows, width, out_stride, kWritten));
@@ -469,7 +476,7 @@ int spdnn_combine_grad(const void* dout, int32_t type, int32_t width, int64_t do
                        const int32_t* place, const float* weight, const int32_t* count, int32_t rows, int32_t k, void* dys,
                        int64_t dys_stride, float* dweight, void* hip_stream) {
     CHECK(check_pairs(rows, k, 1));
-    if (width < 1) return fail(SPDNN_EINVAL, "need width >= 1");
+    CHECK(check_width(width));
     const int n = rows * k;
     CHECK(check_rows("dout", dout, type, rows, width, dout_stride, kRead));
     CHECK(check_rows("ys", ys, type, n, width, ys_stride, kRead));

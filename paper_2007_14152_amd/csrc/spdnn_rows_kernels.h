@@ -549,7 +549,7 @@ __device__ inline void place_chunk(D in, int64_t first, int64_t last, int bins, 
         }
     }
     __syncthreads();
-    // bin e's pairs in all chunks, and in start[0][e] .. start[3][e] where each wave's first one goes, within the bin
+    // bin e's pairs in all chunks, and in start[w][e] where wave w's first one goes, within the bin
     for (int e = threadIdx.x; e < bins; e += kThreads) {
         int before = 0, total = 0;
         if (table) {

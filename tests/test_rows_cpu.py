@@ -53,6 +53,12 @@ REFUSED = [
 ]
 
 
+W = (1 << 30) + 1  # a row too long
+REFUSED += [("spdnn_embed", [dict(width=W, table_stride=W, out_stride=W)]), ("spdnn_embed_grad", [dict(width=W, dout_stride=W, dtable_stride=W)]),
+            ("spdnn_dispatch", [dict(width=W, x_stride=W, xs_stride=W)]), ("spdnn_combine", [dict(width=W, ys_stride=W, out_stride=W)]),
+            ("spdnn_combine_grad", [dict(width=W, dout_stride=W, ys_stride=W, dys_stride=W)])]
+
+
 @pytest.mark.parametrize("name,changes", [(n, c) for n, cs in REFUSED for c in cs], ids=lambda v: str(v))
 def test_refused_before_touching_the_gpu(name, changes):
     assert call(name, **changes) == sp.SPDNN_EINVAL
@@ -62,7 +68,7 @@ def test_refused_before_touching_the_gpu(name, changes):
 def test_work_memory():
     size = ctypes.c_size_t()
     for name, args in [("spdnn_embed_grad_bytes", (50000, 1024, 1)), ("spdnn_embed_grad_bytes", (1, 1, 0)),
-                       ("spdnn_embed_grad_bytes", (2 ** 31 - 1, 65536, 2 ** 31 - 1)), ("spdnn_dispatch_bytes", (0, 1, 1)),
+                       ("spdnn_embed_grad_bytes", (2 ** 31 - 1, 1 << 30, 2 ** 31 - 1)), ("spdnn_dispatch_bytes", (0, 1, 1)),
                        ("spdnn_dispatch_bytes", (1 << 26, 16, 1024))]:
         assert getattr(sp.lib(), name)(*args, ctypes.byref(size)) == sp.SPDNN_OK
         assert getattr(sp.lib(), name)(*args, None) == sp.SPDNN_EINVAL
