@@ -272,6 +272,15 @@ def test_route_takes_the_first_of_equals(sp, dtype):
         assert np.array_equal(sp.route(few, k)[0].cpu().numpy(), want)
 
 
+def test_route_without_rows(sp):
+    none = torch.empty(0, 12, device=DEV)
+    chosen, weight = sp.route(none, 3)
+    assert chosen.shape == (0, 3) and weight.shape == (0, 3)
+    assert sp.route_grad(weight, none, chosen).shape == (0, 12)
+    dys, dweight = sp.combine_grad(none, none, chosen[:, :1], weight[:, :1], torch.zeros(5, dtype=torch.int32, device=DEV))
+    assert dys.shape == (0, 12) and dweight.shape == (0, 1)
+
+
 @pytest.mark.parametrize("score,normalise", SCORES)
 def test_route_rows_that_masks_leave_empty(sp, score, normalise):
     inf, low = float("inf"), torch.finfo(F32).min
