@@ -273,8 +273,8 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
                         const int per = (int)std::min<int64_t>(std::max<int64_t>(kClearBytes / row_bytes, 1), spdnn::kMostRowsToClear);
                         const int64_t clear = accumulate ? 0 : std::min<int64_t>((vocab - 1) / per + 1, kMostGroups);
                         // as many workgroups for a token's columns as make kFewGroups in all
-                        const int y = (int)std::max<int64_t>(1, std::min<int64_t>((vecs - 1) / 64 + 1, kFewGroups / std::max(n, 1)));
-                        spdnn::embed_grad_short_kernel<T, S, I, V><<<dim3((unsigned)(n + clear), (unsigned)y), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, n, per, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
+                        const int slabs = (int)std::max<int64_t>(1, std::min<int64_t>((vecs - 1) / 64 + 1, kFewGroups / std::max(n, 1)));
+                        spdnn::embed_grad_short_kernel<T, S, I, V><<<dim3((unsigned)(n * slabs + clear)), spdnn::kRowThreads, 0, s>>>((const T*)dout, dout_stride, (const I*)ids, n, vocab, width, slabs, per, scale, accumulate != 0, (S*)dtable, dtable_stride, past);
                     });
                 });
             });
@@ -335,8 +335,9 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
                     const int adders = (int)std::min<int64_t>((pieces - 1) / (spdnn::kRowThreads / L) + 1, kMostGroups);
                     const int per = (int)std::min<int64_t>(std::max<int64_t>(kClearBytes / row_bytes, 1), spdnn::kRowThreads);
                     const int clear = accumulate ? 0 : (int)std::min<int64_t>((rows.first + per - 1) / per, kMostGroups);
-                    const dim3 grid(adders + clear, std::min((vecs - 1) / L + 1, 1024));
-                    spdnn::embed_grad_kernel<T, S, V, L><<<grid, spdnn::kRowThreads, 0, s>>>(order, (const T*)dout, dout_stride, width, scale, accumulate != 0, (S*)dtable, dtable_stride, parts, adders, (uint32_t)rows.first, per, past);
+                    const int slabs = (int)std::min<int64_t>((vecs - 1) / L + 1, std::max<int64_t>(1, kMostGroups / adders));
+                    const dim3 grid((unsigned)(adders * slabs + clear));
+                    spdnn::embed_grad_kernel<T, S, V, L><<<grid, spdnn::kRowThreads, 0, s>>>(order, (const T*)dout, dout_stride, width, scale, accumulate != 0, (S*)dtable, dtable_stride, parts, adders, slabs, (uint32_t)rows.first, per, past);
                 };
                 if (vecs <= 16) run(std::integral_constant<int, 16>{});
                 else if (vecs <= 64) run(std::integral_constant<int, 64>{});

@@ -718,29 +718,29 @@ __device__ inline void add_rows(const T* __restrict__ dout, int64_t dout_stride,
 
 // dtable[v] = [dtable[v] +] scale * sum of the dout[t] with ids[t] == v.
 //
-// Few ids, one launch and no sort.  The first `adders` workgroups (of blockIdx.x) have a token each: the one that is the first
-// with its id finds the others in order and adds their rows, a quarter of them per wave, 64 vectors of columns at a time (shared
-// out over blockIdx.y).  The others (none if accumulate) clear `per` rows each, but for those that an id has.  777 rows of 1500
-// floats into 10007 rows: 16.2 us, of which clearing 60 MB takes 11 (9.3 alone).  A workgroup's work grows with the ids: 1000 of
-// them into 1000 rows of 1024 12 us, where the sort takes 19, but 4096 49 us, where it takes 26.
+// Few ids, one launch and no sort.  n * slabs workgroups have a token each: the one that is the first with its id finds the others
+// in order and adds their rows, a quarter of them per wave, 64 vectors of columns at a time (shared out over the slabs).  Those
+// before them (none if accumulate) clear `per` rows each, but for rows that an id has.  777 rows of 1500 floats into 10007 rows:
+// 17.0 us, of which clearing 60 MB takes 11.5 (a fill 9.3); with those that clear behind or in turn 20.  A workgroup's work grows
+// with the ids: 1000 of them into 1000 rows of 1024 12 us, where the sort takes 19, but 4096 49 us, where it takes 26.
 constexpr int kFewIds = 1024, kMostRowsToClear = 1024;
 template <typename T, typename S, typename I, int V>
 __global__ __launch_bounds__(kRowThreads) void embed_grad_short_kernel(const T* __restrict__ dout, int64_t dout_stride, const I* __restrict__ ids, int n,
-                                                                     int vocab, int width, int adders, int per, float scale, bool accumulate,
+                                                                     int vocab, int width, int slabs, int per, float scale, bool accumulate,
                                                                      S* __restrict__ dtable, int64_t dtable_stride, bool past) {
     constexpr int kWaves = kRowThreads / 64, kRounds = kFewIds / kRowThreads;
     __shared__ uint64_t with_id[kRounds * kWaves];
     __shared__ int32_t tokens[kFewIds];
     __shared__ float sums[kWaves][64][V];
     __shared__ bool there[kMostRowsToClear];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, adders = n * slabs;
     const int vecs = (width - 1) / V + 1;
     I id[kRounds];
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) id[r] = n > 0 ? ids[min(r * kRowThreads + (int)threadIdx.x, n - 1)] : (I)-1;
-    if ((int)blockIdx.x >= adders) {
-        if (blockIdx.y) return;
-        for (int64_t v0 = (int64_t)(blockIdx.x - adders) * per; v0 < vocab; v0 += (int64_t)(gridDim.x - adders) * per) {
+    const int clearers = (int)gridDim.x - adders, number = (int)blockIdx.x - clearers;
+    if (number < 0) {
+        for (int64_t v0 = (int64_t)blockIdx.x * per; v0 < vocab; v0 += (int64_t)clearers * per) {
             const int rows = (int)min((int64_t)per, vocab - v0);
             __syncthreads();
             for (int r = threadIdx.x; r < rows; r += kRowThreads) there[r] = false;
@@ -756,7 +756,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_grad_short_kernel(const T* 
         }
         return;
     }
-    const int t = blockIdx.x;
+    const int t = number % n, slab = number / n;
     const I v = ids[t];
     if (v < 0 || v >= (I)vocab) return;
 #pragma unroll
@@ -776,7 +776,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_grad_short_kernel(const T* 
     if (first != t) return;
     __syncthreads();
     const int each = (many + kWaves - 1) / kWaves, from = min(wave * each, many), to = min(from + each, many);
-    for (int v0 = blockIdx.y * 64; v0 < vecs; v0 += gridDim.y * 64) {
+    for (int v0 = slab * 64; v0 < vecs; v0 += slabs * 64) {
         const int vec = min(v0 + lane, vecs - 1), col = min(vec * V, width - V);
         float sum[V] = {};
         add_rows<V>(dout, dout_stride, col, from, to, [&](int a) { return tokens[a]; }, sum);
@@ -822,7 +822,7 @@ struct GradOrder {
 
 template <typename T, typename S, int V, int L>
 __device__ inline void add_pieces(const GradOrder& o, const T* __restrict__ dout, int64_t dout_stride, int width, float scale, bool accumulate,
-                                  S* __restrict__ dtable, int64_t dtable_stride, float* __restrict__ parts, int group, int groups) {
+                                  S* __restrict__ dtable, int64_t dtable_stride, float* __restrict__ parts, int group, int groups, int slab, int slabs) {
     constexpr int kTeams = kRowThreads / L;
     __shared__ uint32_t keys[kTeams][kPiece + 2];  // from the place before the piece to the one behind it; vocab where there is none
     __shared__ int32_t tokens[kTeams][kPiece];
@@ -842,7 +842,7 @@ __device__ inline void add_pieces(const GradOrder& o, const T* __restrict__ dout
         int many = 0;  // of the piece's places have an id: the others are the last of all
         for (int a = 0; a < kPiece; ++a) many += key[a] < o.vocab;
         const int64_t piece = piece0 + team;
-        for (int vec = blockIdx.y * L + lane; vec < vecs && many > 0; vec += gridDim.y * L) {
+        for (int vec = slab * L + lane; vec < vecs && many > 0; vec += slabs * L) {
             const int col = min(vec * V, width - V), again = vec * V - col;
             float sum[V] = {};
             bool in = key[-1] == key[0];  // the run at hand began in the piece before
@@ -893,16 +893,19 @@ __device__ inline void clear_rows(const GradOrder& o, uint32_t end, int width, i
     }
 }
 
-// The first `adders` workgroups add pieces, the others (none if accumulate) clear those of the first `end` rows that have no id,
-// `per` at a time.
+// adders * slabs workgroups add pieces, a slab of columns each, the others (none if accumulate) clear those of the first `end` rows
+// that have no id, `per` at a time; in turn as long as there are both, for one sort waits for loads and the other stores.  (3000 ids,
+// 60000 rows of 4096 bf16: 106 us a call, with those that clear first 113.)
 template <typename T, typename S, int V, int L>
 __global__ __launch_bounds__(kRowThreads) void embed_grad_kernel(GradOrder o, const T* __restrict__ dout, int64_t dout_stride, int width, float scale,
                                                                  bool accumulate, S* __restrict__ dtable, int64_t dtable_stride,
-                                                                 float* __restrict__ parts, int adders, uint32_t end, int per, bool past) {
-    if ((int)blockIdx.x < adders)
-        add_pieces<T, S, V, L>(o, dout, dout_stride, width, scale, accumulate, dtable, dtable_stride, parts, blockIdx.x, adders);
-    else if (blockIdx.y == 0)
-        clear_rows<S, V>(o, end, width, per, dtable, dtable_stride, past, blockIdx.x - adders, gridDim.x - adders);
+                                                                 float* __restrict__ parts, int adders, int slabs, uint32_t end, int per, bool past) {
+    const int b = blockIdx.x, all = adders * slabs, both = min(all, (int)gridDim.x - all);
+    const int number = b < 2 * both ? b >> 1 : b - both;
+    if (b < 2 * both ? !(b & 1) : all > both)
+        add_pieces<T, S, V, L>(o, dout, dout_stride, width, scale, accumulate, dtable, dtable_stride, parts, number / slabs, adders, number % slabs, slabs);
+    else
+        clear_rows<S, V>(o, end, width, per, dtable, dtable_stride, past, number, gridDim.x - all);
 }
 
 // The rows of ids whose places lie in more than one piece: workgroups per piece, which have work if such a run begins there.  A run
