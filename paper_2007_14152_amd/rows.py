@@ -1,8 +1,9 @@
 """The ends of a mixture of networks (the second half of include/spdnn.h) on torch tensors.
 
 Argument marshalling only, as in the package's __init__: torch allocates the outputs and names the stream, the HIP kernels
-do the rest.  Every call enqueues on the current stream of its tensors' device and returns without waiting.  Rows may have
-any stride between them, their elements are adjacent; what the library refuses raises SpdnnError.
+do the rest.  Gradients are calls of their own (nothing is recorded for automatic ones).  Every call enqueues on the current
+stream of its tensors' device and returns without waiting.  Rows may have any stride between them, their elements are adjacent;
+what the library refuses raises SpdnnError.
 """
 from __future__ import annotations
 
