@@ -24,6 +24,15 @@ def _refuse(text, *args):
     raise SpdnnError(SPDNN_EINVAL, text % args)
 
 
+_MOST = 2 ** 31 - 1  # the library's sizes are of 32 bits; ctypes would pass on the last 32 of more without a word
+
+
+def _fits(name, *sizes):
+    for size in sizes:
+        if not -_MOST <= size <= _MOST:
+            _refuse("%s: a size of %d, at most %d", name, size, _MOST)
+
+
 def _type(dtype, name):
     code = _TYPES.get(dtype)
     if code is None:
@@ -40,6 +49,8 @@ def _rows(t, name, device=None, shape=None):
         _refuse("%s is on %s, not on %s", name, t.device, device)
     if shape is not None and size != shape:
         _refuse("%s: %s, not %s", name, shape, tuple(size))
+    if size[0] > _MOST or size[1] > _MOST:
+        _fits(name, *size)
     stride, step = t.stride()
     if step != 1 and size[1] > 1:
         _refuse("%s: the elements of a row must be adjacent", name)
@@ -58,6 +69,16 @@ def _array(t, name, dtypes, device, shape):
     return t.data_ptr()
 
 
+def _pairs(t, name):
+    """(rows, k) of what stands for every pair of a row and a slot."""
+    if t.dim() != 2:
+        _refuse("%s: a matrix, not %s", name, tuple(t.shape))
+    rows, k = t.shape
+    if rows > _MOST or k > _MOST:
+        _fits(name, rows, k)
+    return rows, k
+
+
 _F32 = (torch.float32,)
 _I32 = (torch.int32,)
 _BYTES = (torch.bool, torch.uint8)
@@ -70,6 +91,7 @@ _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index:
 
 @functools.lru_cache(maxsize=64)
 def _work_bytes(name, *sizes):
+    _fits(name, *sizes)
     need = ctypes.c_size_t()
     _check(getattr(lib(), name)(*sizes, ctypes.byref(need)))
     return need.value
@@ -88,9 +110,12 @@ def embed(table, ids, scale=1.0, dtype=None):
             return embed(table, ids, scale, dtype)
     if ids.dtype not in _IDS or ids.device != dev:
         _refuse("ids: int32 or int64 on %s, not %s on %s", dev, ids.dtype, ids.device)
+    n = ids.numel()
+    if n > _MOST:
+        _fits("ids", n)
     ids = ids.contiguous()
     out = table.new_empty((*ids.shape, width), dtype=dtype)
-    _check(lib().spdnn_embed(table.data_ptr(), ttype, vocab, width, tstride, ids.data_ptr(), _IDS[ids.dtype], ids.numel(),
+    _check(lib().spdnn_embed(table.data_ptr(), ttype, vocab, width, tstride, ids.data_ptr(), _IDS[ids.dtype], n,
                              scale, out.data_ptr(), otype, width, _stream(dev.index)))
     return out
 
@@ -141,6 +166,8 @@ def route(logits, k, bias=None, keep=None, score="softmax", normalise=True, scal
     if dev.index != _current():
         with torch.cuda.device(dev):
             return route(logits, k, bias, keep, score, normalise, scale)
+    if not -_MOST <= k <= _MOST:
+        _fits("k", k)
     bp = _array(bias, "bias", _F32, dev, (experts,))
     kp = _array(keep, "keep", _BYTES, dev, (rows,))
     chosen = logits.new_empty((rows, max(k, 0)), dtype=torch.int32)
@@ -159,9 +186,7 @@ def route_grad(dweight, logits, chosen, bias=None, score="softmax", normalise=Tr
     if dev.index != _current():
         with torch.cuda.device(dev):
             return route_grad(dweight, logits, chosen, bias, score, normalise, scale)
-    if chosen.dim() != 2:
-        _refuse("chosen: a matrix, not %s", tuple(chosen.shape))
-    k = chosen.shape[1]
+    k = _pairs(chosen, "chosen")[1]
     bp = _array(bias, "bias", _F32, dev, (experts,))
     cp = _array(chosen, "chosen", _I32, dev, (rows, k))
     wp = _array(dweight, "dweight", _F32, dev, (rows, k))
@@ -181,9 +206,7 @@ def dispatch(x, chosen, experts):
     if dev.index != _current():
         with torch.cuda.device(dev):
             return dispatch(x, chosen, experts)
-    if chosen.dim() != 2:
-        _refuse("chosen: a matrix, not %s", tuple(chosen.shape))
-    k = chosen.shape[1]
+    k = _pairs(chosen, "chosen")[1]
     cp = _array(chosen, "chosen", _I32, dev, (rows, k))
     need = _work_bytes("spdnn_dispatch_bytes", rows, k, experts)
     xs = x.new_empty((rows * k, width))
@@ -201,9 +224,7 @@ def _back(ys, place, weight, add):
     if dev.index != _current():
         with torch.cuda.device(dev):
             return _back(ys, place, weight, add)
-    if place.dim() != 2:
-        _refuse("place: a matrix, not %s", tuple(place.shape))
-    rows, k = place.shape
+    rows, k = _pairs(place, "place")
     width = ys.shape[1]
     if ys.shape[0] != rows * k:
         _refuse("ys: %d rows for %d x %d places", ys.shape[0], rows, k)
@@ -242,9 +263,7 @@ def combine_grad(dout, ys, place, weight, offsets):
     if dev.index != _current():
         with torch.cuda.device(dev):
             return combine_grad(dout, ys, place, weight, offsets)
-    if place.dim() != 2:
-        _refuse("place: a matrix, not %s", tuple(place.shape))
-    rows, k = place.shape
+    rows, k = _pairs(place, "place")
     width = ys.shape[1]
     if ys.shape[0] != rows * k:
         _refuse("ys: %d rows for %d x %d places", ys.shape[0], rows, k)
