@@ -171,3 +171,95 @@ def combine(ys, place, weight, add):
         out += add
         size += np.abs(add)
     return out, (k + 2) * U * size
+
+
+# ---------------------------------------------------------------------------
+# the router, all rows at once, with bounds that logits far below a row's largest do not widen
+# ---------------------------------------------------------------------------
+FAR = 110.0  # exp(-FAR) is less than half the smallest float
+TINY = SMALLEST[torch.float32]
+
+
+def router_input(seed, rows, experts, dtype, with_bias, masked):
+    """(logits, bias, keep) on the CPU.  masked: three tenths of the logits are -inf, or NaN in every fifth row, every seventh
+    column holds the type's lowest value (open, but last), and a fifth of the rows go to no expert."""
+    g = torch.Generator().manual_seed(seed)
+    logits = (torch.randn(rows, experts, generator=g) * 2).to(dtype)
+    bias = torch.randn(experts, generator=g) if with_bias else None
+    if not masked:
+        return logits, bias, None
+    off = torch.rand(rows, experts, generator=g) < 0.3
+    logits[off] = -float("inf")
+    logits[:, ::7] = torch.finfo(dtype).min
+    logits[::5] = torch.where(off[::5], float("nan"), logits[::5])
+    return logits, bias, torch.rand(rows, generator=g) < 0.8
+
+
+def choose_all(logits, k, bias=None, keep=None):
+    """choose for tensors of many rows: (chosen int32 [rows, k], open bool [rows, experts]) as arrays."""
+    r = logits.float().cpu()
+    if bias is not None:
+        r = r + bias.cpu()
+    is_open = r > -float("inf")
+    if keep is not None:
+        is_open &= keep.cpu()[:, None]
+    at = torch.sort(torch.where(is_open, r, -float("inf")), dim=1, descending=True, stable=True).indices[:, :k]
+    return torch.where(is_open.gather(1, at), at, -1).int().numpy(), is_open.numpy()
+
+
+def router(logits, is_open, chosen, score, normalise, scale, dweight):
+    """(weights, bound, gradient, bound); logits and dweight float64.
+
+    A weight is off by its exponent, which is rounded at the size of the difference D to the largest logit (and by log_sigmoid,
+    at the size Y of its value, on either side of that difference), by exp and log1p (4 U each), by the sum of m positive terms
+    (m U, and by what its terms are off), by the quotient and the scale.  Only terms within FAR of the largest count: the others
+    are zeros, or a few of the smallest floats.  A logit beyond 200 is its own log_sigmoid, exactly.  The gradient is a product
+    of a weight and a difference of terms that hold another, k of them added."""
+    rows, experts = logits.shape
+    k = chosen.shape[1]
+    valid = chosen >= 0
+    at = np.where(valid, chosen, 0)
+    with np.errstate(all="ignore"):
+        L = np.where(is_open, logits, -np.inf)
+        picked = np.where(valid, np.take_along_axis(L, at, 1), -np.inf)
+        everything = score == "softmax" and not normalise
+        if score == "sigmoid" and not normalise:
+            w = np.where(valid, sigmoid(picked), 0.0)
+            rel = np.full((rows, 1), 16.0)
+        else:
+            x, there = (L, is_open) if everything else (picked if score == "softmax" else log_sigmoid(picked), valid)
+            top = np.where(there, x, -np.inf).max(1, keepdims=True)
+            below = np.where(there, x - np.where(np.isfinite(top), top, 0.0), -np.inf)
+            e = np.exp(below)
+            total = e.sum(1, keepdims=True)
+            p = e / np.where(total > 0, total, 1.0)
+            near = there & (below > -FAR)
+            rel = 2 * np.where(near, -below, 0.0).max(1, keepdims=True) + x.shape[1] + 16
+            if score == "sigmoid":
+                rel = rel + 32 + 4 * np.where(near & (np.abs(picked) < 200), np.abs(x), 0.0).max(1, keepdims=True)
+            w = np.where(valid, np.take_along_axis(p, at, 1), 0.0) if everything else p
+        bound = 1.001 * rel * U * w * scale + 4 * TINY * max(1.0, scale)
+        g = np.where(valid, np.where(valid, dweight, 0.0) * scale, 0.0)
+        mean, size, most = (g * w).sum(1, keepdims=True), (np.abs(g) * w).sum(1, keepdims=True), np.abs(g).sum(1, keepdims=True)
+        d = np.zeros((rows, experts + 1))
+        dbound = np.zeros_like(d)
+        slot = np.where(valid, chosen, experts)
+        if everything:
+            spread = np.zeros_like(d)
+            np.put_along_axis(spread, slot, g, 1)
+            spread = spread[:, :-1]
+            any_slot = valid.any(1, keepdims=True)
+            d = np.where(any_slot, p * (spread - mean), 0.0)
+            dbound = np.where(any_slot, 1.001 * (2 * rel + k + 40) * U * p * (np.abs(spread) + size) + 8 * TINY * (np.abs(spread) + most + 1), 0.0)
+            return w * scale, bound, d, dbound
+        if normalise:
+            v, b = w * (g - mean), (2 * rel + k + 40) * U * w * (np.abs(g) + size)
+            if score == "sigmoid":
+                v, b = v * sigmoid(-picked), b * sigmoid(-picked)
+        else:
+            v = g * w * sigmoid(-picked)
+            b = 40 * U * np.abs(v)
+        v, b = np.where(valid, v, 0.0), np.where(valid, 1.001 * b + 8 * TINY * (np.abs(g) + most + 1), 0.0)
+        np.put_along_axis(d, slot, v, 1)
+        np.put_along_axis(dbound, slot, b, 1)
+        return w * scale, bound, d[:, :-1], dbound[:, :-1]

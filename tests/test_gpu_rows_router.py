@@ -45,3 +45,34 @@ def test_softmax_of_logits_that_are_exact(sp, rows, experts):
     d = -p * pe
     np.put_along_axis(d, want[:, :1], pe * (1 - pe), 1)
     ref.assert_within(got, d, (2 * experts + 24) * U * p * (1 + pe) + 3 * TINY, torch.float32)
+
+
+SCORES = [("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)]
+
+
+def check(sp, rows, experts, k, dtype, layout, with_bias, masked, score, normalise):
+    """route and route_grad against the reference whose bounds the masked logits do not widen."""
+    logits, bias, keep = ref.router_input(rows + experts + k, rows, experts, dtype, with_bias, masked)
+    on = logits.to(DEV)
+    if layout == "part":  # rows of a wider matrix, off by one element
+        on = torch.cat([on[:, :1], on, on[:, :2]], 1)[:, 1:experts + 1]
+    b = None if bias is None else bias.to(DEV)
+    chosen, is_open = ref.choose_all(logits, k, bias, keep)
+    dw = torch.randn(rows, k, generator=torch.Generator().manual_seed(k))
+    dw[torch.from_numpy(chosen < 0)] = float("nan")  # not used
+    l = np.where(is_open, ref.f64(logits), -np.inf)
+    w, wbound, d, dbound = ref.router(l, is_open, chosen, score, normalise, 2.5, ref.f64(dw))
+    got = sp.route(on, k, bias=b, keep=None if keep is None else keep.to(DEV), score=score, normalise=normalise, scale=2.5)
+    assert np.array_equal(got[0].cpu().numpy(), chosen)
+    ref.assert_within(got[1], w, wbound, torch.float32)
+    grad = sp.route_grad(dw.to(DEV), on, got[0], bias=b, score=score, normalise=normalise, scale=2.5)
+    ref.assert_within(grad, d, dbound, dtype)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype,layout,with_bias", [(torch.float32, "dense", False), (torch.bfloat16, "part", True), (torch.float16, "dense", True)])
+@pytest.mark.parametrize("score,normalise", SCORES)
+@pytest.mark.parametrize("rows,experts,k", [(1, 1, 1), (5, 3, 2), (64, 8, 2), (3, 16, 16), (33, 63, 4), (40, 100, 16), (130, 128, 1), (31, 256, 8),
+                                            (20, 257, 16), (27, 1000, 5), (14, 1024, 16)])
+def test_weights_and_gradient_of_masked_rows(sp, rows, experts, k, score, normalise, dtype, layout, with_bias, masked):
+    check(sp, rows, experts, k, dtype, layout, with_bias, masked, score, normalise)
