@@ -76,3 +76,25 @@ def check(sp, rows, experts, k, dtype, layout, with_bias, masked, score, normali
                                             (20, 257, 16), (27, 1000, 5), (14, 1024, 16)])
 def test_weights_and_gradient_of_masked_rows(sp, rows, experts, k, score, normalise, dtype, layout, with_bias, masked):
     check(sp, rows, experts, k, dtype, layout, with_bias, masked, score, normalise)
+
+
+@pytest.mark.parametrize("dtype,layout,with_bias,masked", [(torch.float32, "dense", False, False), (torch.float32, "part", True, True),
+                                                           (torch.bfloat16, "part", True, True), (torch.float16, "dense", False, True)])
+@pytest.mark.parametrize("score,normalise", SCORES)
+@pytest.mark.parametrize("rows,experts,k", [(4096, 256, 8), (4097, 256, 8), (4101, 1000, 5), (4099, 257, 16), (4098, 1024, 16), (4099, 400, 1),
+                                            (9001, 65, 2), (60000, 64, 4)])
+def test_many_rows(sp, rows, experts, k, score, normalise, dtype, layout, with_bias, masked):
+    """More rows than get a lane for every eight logits: teams of 8 and 16 lanes, which take a long row in turns."""
+    check(sp, rows, experts, k, dtype, layout, with_bias, masked, score, normalise)
+
+
+@pytest.mark.parametrize("rows,experts,k", [(4097, 300, 8), (4101, 1024, 16)])
+def test_many_rows_take_the_first_of_equals(sp, rows, experts, k):
+    few = torch.randint(-2, 3, (rows, experts), generator=torch.Generator().manual_seed(rows)).float()
+    few[1] = 0.0
+    few[1, ::2] = -0.0  # equal to 0
+    few[2] = -float("inf")
+    few[3, 7:] = float("nan")
+    want, _ = ref.choose_all(few, k)
+    assert want[1].tolist() == list(range(k)) and (want[2] == -1).all()
+    assert np.array_equal(sp.route(few.to(DEV), k)[0].cpu().numpy(), want)
