@@ -5,6 +5,7 @@ import os
 import re
 import subprocess
 import sys
+import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -48,24 +49,36 @@ def _resource_usage(text):
     return out
 
 
+def _report(res, cmd):
+    """What a step that failed has said, and the error."""
+    sys.stderr.write("\n".join(l for l in res.stderr.splitlines() if "kernel-resource-usage" not in l) + "\n")
+    raise subprocess.CalledProcessError(res.returncode, cmd)
+
+
 def build(verbose: bool = False, extra=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    flags = [f for f in HIPCC_FLAGS if f != "-shared"] + list(extra)
-    objects = [os.path.splitext(src)[0] + ".o" for src in SOURCES]
-    cmds = [[hipcc] + flags + ["-Rpass-analysis=kernel-resource-usage", "-c", src, "-o", obj] for src, obj in zip(SOURCES, objects)]
-    with ThreadPoolExecutor(len(cmds)) as side_by_side:
-        runs = list(side_by_side.map(lambda cmd: subprocess.run(cmd, stderr=subprocess.PIPE, text=True), cmds))
+    compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"] + ["-Rpass-analysis=kernel-resource-usage"] + list(extra)
     usage = {}
-    for cmd, res in zip(cmds, runs):
+    # In a folder of this build's own, so that no other build's files are in the way and nothing is left of one that fails.
+    with tempfile.TemporaryDirectory(prefix="_build.", dir=CSRC) as own:
+        objects = [os.path.join(own, os.path.splitext(os.path.basename(src))[0] + ".o") for src in SOURCES]
+        cmds = [[hipcc] + compile_flags + ["-c", src, "-o", obj] for src, obj in zip(SOURCES, objects)]
+        with ThreadPoolExecutor(len(cmds)) as side_by_side:
+            runs = list(side_by_side.map(lambda cmd: subprocess.run(cmd, stderr=subprocess.PIPE, text=True), cmds))
+        for cmd, res in zip(cmds, runs):
+            if verbose:
+                print(" ".join(cmd))
+            if res.returncode != 0:
+                _report(res, cmd)
+            usage.update(_resource_usage(res.stderr))
+        linked = os.path.join(own, os.path.basename(LIB))
+        cmd = [hipcc] + HIPCC_FLAGS + list(extra) + objects + ["-o", linked]
         if verbose:
             print(" ".join(cmd))
+        res = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
         if res.returncode != 0:
-            sys.stderr.write("\n".join(l for l in res.stderr.splitlines() if "kernel-resource-usage" not in l) + "\n")
-            raise subprocess.CalledProcessError(res.returncode, cmd)
-        usage.update(_resource_usage(res.stderr))
-    subprocess.run([hipcc] + HIPCC_FLAGS + objects + ["-o", LIB], check=True, stderr=subprocess.DEVNULL if not verbose else None)
-    for obj in objects:
-        os.remove(obj)
+            _report(res, cmd)
+        os.replace(linked, LIB)
     # Kernels that issue their global loads as inline instructions keep the loaded values in registers
     # the compiler believes to be ready; a spill between load and wait would save stale data.
     for kernel in NO_SCRATCH_KERNELS:
