@@ -146,6 +146,8 @@ def embed_grad(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
     work = dout.new_empty(need, dtype=torch.uint8) if need else None
     _check(lib().spdnn_embed_grad(dout.data_ptr(), itype, dstride, ids.data_ptr(), _IDS[ids.dtype], n, vocab, width, scale, add,
                                   out.data_ptr(), otype, ostride, work.data_ptr() if need else 0, need, _stream(dev.index)))
+    if add:
+        torch.autograd.graph.increment_version(out)  # changed in place: what an automatic gradient has kept of it is stale
     return out
 
 
