@@ -1,7 +1,8 @@
 """The ends of a mixture of networks (the second half of include/spdnn.h) on torch tensors.
 
 Argument marshalling only, as in the package's __init__: torch allocates the outputs and names the stream, the HIP kernels
-do the rest.  Gradients are calls of their own (nothing is recorded for automatic ones).  Every call enqueues on the current
+do the rest.  Gradients are calls of their own: nothing is recorded for automatic ones, and a call warns where an input asks for one
+(outside torch.no_grad()).  Every call enqueues on the current
 stream of its tensors' device and returns without waiting.  Rows may have any stride between them, their elements are adjacent;
 what the library refuses raises SpdnnError.
 """
@@ -9,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import warnings
 
 import torch
 
@@ -22,6 +24,13 @@ _SCORES = {"softmax": SPDNN_SOFTMAX, "sigmoid": SPDNN_SIGMOID}
 
 def _refuse(text, *args):
     raise SpdnnError(SPDNN_EINVAL, text % args)
+
+
+def _unrecorded(name, level=3):
+    """For a call of which an input asks for a gradient."""
+    if torch.is_grad_enabled():
+        warnings.warn("%s records no gradient for its inputs: call the gradient's operator, or wrap the call in torch.no_grad()" % name,
+                      stacklevel=level)
 
 
 _MOST = 2 ** 31 - 1  # the library's sizes are of 32 bits; ctypes would pass on the last 32 of more without a word
@@ -108,6 +117,8 @@ def embed(table, ids, scale=1.0, dtype=None):
     if dev.index != _current():
         with torch.cuda.device(dev):
             return embed(table, ids, scale, dtype)
+    if table.requires_grad:
+        _unrecorded("embed")
     if ids.dtype not in _IDS or ids.device != dev:
         _refuse("ids: int32 or int64 on %s, not %s on %s", dev, ids.dtype, ids.device)
     n = ids.numel()
@@ -134,6 +145,8 @@ def embed_grad(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
     if dev.index != _current():
         with torch.cuda.device(dev):
             return embed_grad(dout, ids, vocab, scale, dtype, out)
+    if dout.requires_grad or out is not None and out.requires_grad:
+        _unrecorded("embed_grad")
     if ids.dtype not in _IDS or ids.device != dev or ids.numel() != n:
         _refuse("ids: %d of int32 or int64 on %s, not %d of %s on %s", n, dev, ids.numel(), ids.dtype, ids.device)
     ids = ids.contiguous()
@@ -168,6 +181,8 @@ def route(logits, k, bias=None, keep=None, score="softmax", normalise=True, scal
     if dev.index != _current():
         with torch.cuda.device(dev):
             return route(logits, k, bias, keep, score, normalise, scale)
+    if logits.requires_grad or bias is not None and bias.requires_grad:
+        _unrecorded("route")
     if not -_MOST <= k <= _MOST:
         _fits("k", k)
     bp = _array(bias, "bias", _F32, dev, (experts,))
@@ -188,6 +203,8 @@ def route_grad(dweight, logits, chosen, bias=None, score="softmax", normalise=Tr
     if dev.index != _current():
         with torch.cuda.device(dev):
             return route_grad(dweight, logits, chosen, bias, score, normalise, scale)
+    if logits.requires_grad or dweight.requires_grad or bias is not None and bias.requires_grad:
+        _unrecorded("route_grad")
     k = _pairs(chosen, "chosen")[1]
     bp = _array(bias, "bias", _F32, dev, (experts,))
     cp = _array(chosen, "chosen", _I32, dev, (rows, k))
@@ -208,6 +225,8 @@ def dispatch(x, chosen, experts):
     if dev.index != _current():
         with torch.cuda.device(dev):
             return dispatch(x, chosen, experts)
+    if x.requires_grad:
+        _unrecorded("dispatch")
     k = _pairs(chosen, "chosen")[1]
     cp = _array(chosen, "chosen", _I32, dev, (rows, k))
     need = _work_bytes("spdnn_dispatch_bytes", rows, k, experts)
@@ -220,12 +239,14 @@ def dispatch(x, chosen, experts):
     return xs, offsets, place
 
 
-def _back(ys, place, weight, add):
+def _back(name, ys, place, weight, add):
     ytype, ystride = _rows(ys, "ys")
     dev = ys.device
     if dev.index != _current():
         with torch.cuda.device(dev):
-            return _back(ys, place, weight, add)
+            return _back(name, ys, place, weight, add)
+    if ys.requires_grad or weight is not None and weight.requires_grad or add is not None and add.requires_grad:
+        _unrecorded(name, 4)
     rows, k = _pairs(place, "place")
     width = ys.shape[1]
     if ys.shape[0] != rows * k:
@@ -249,12 +270,12 @@ def combine(ys, place, weight=None, add=None):
 
     ys: [rows * k, width]; weight: float32 [rows, k], ones if None; add: [rows, width] of ys's type (a residual), zeros if
     None.  Slots whose place is -1 are left out."""
-    return _back(ys, place, weight, add)
+    return _back("combine", ys, place, weight, add)
 
 
 def dispatch_grad(dxs, place):
     """Gradient of dispatch: the sum of the gradients of a row's copies."""
-    return _back(dxs, place, None, None)
+    return _back("dispatch_grad", dxs, place, None, None)
 
 
 def combine_grad(dout, ys, place, weight, offsets):
@@ -265,6 +286,8 @@ def combine_grad(dout, ys, place, weight, offsets):
     if dev.index != _current():
         with torch.cuda.device(dev):
             return combine_grad(dout, ys, place, weight, offsets)
+    if dout.requires_grad or ys.requires_grad or weight is not None and weight.requires_grad:
+        _unrecorded("combine_grad")
     rows, k = _pairs(place, "place")
     width = ys.shape[1]
     if ys.shape[0] != rows * k:
