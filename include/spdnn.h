@@ -331,7 +331,7 @@ int spdnn_embed_grad(const void* dout, int32_t dout_type, int64_t dout_stride, c
 /* The k experts of each row and their weights.
  *   logits : rows x experts of `type`, 1 <= k <= experts <= SPDNN_MAX_EXPERTS, k <= SPDNN_MAX_CHOSEN.
  *   bias   : experts floats that are added to the logits for the choice only (for example to even out the experts' loads),
- *            or NULL.
+ *            or NULL.  They go on the logit: a bias that was learned on s(l), as some routers choose by, chooses otherwise.
  *   keep   : rows bytes, 0 = the row goes to no expert and its logits are not read, or NULL.
  * An expert is open to a row if logit + bias, added in 32 bits, is greater than minus infinity (a NaN is not).  The row's
  * experts are the k open ones of the largest such sums, in descending order, the lower index first among equals; slots

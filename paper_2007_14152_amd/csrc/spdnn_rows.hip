@@ -137,7 +137,7 @@ struct GradWork {
     int passes, bits;
     GradWork(int32_t vocab, int32_t width, int32_t n) : keys{}, tokens{}, table(0), parts(0), bytes(0), passes(0), bits(0) {
         if (n <= spdnn::kFewIds) return;
-        int all = 0;  // bits of 0 .. vocab
+        int all = 0;  // bits of 0 .. vocab: ids outside the table are sorted as `vocab`, behind all others
         while ((int64_t)vocab >> all) ++all;
         passes = (all + 9) / 10;
         bits = (all + passes - 1) / passes;
@@ -156,9 +156,17 @@ struct GradWork {
 };
 static_assert(spdnn::kMostBins >= 1 << 10);
 constexpr int64_t kClearBytes = 128 << 10;  // of a table that a workgroup clears at a time
-constexpr int64_t kCountClears = 24 << 20, kPlaceClears = 40 << 20;  // ... that a launch of the sort clears beside
-constexpr int kSpareGroups = 768;           // workgroups for that
-constexpr int64_t kFewGroups = 4096;        // workgroups that add with few ids
+// What a launch of the sort clears beside: as much as is stored while the sort waits.  Nothing, this, twice this: 60000 ids, 65536 rows
+// of 1024 floats 87.6, 83.7 and 97.4 us; 3000 ids, 60000 rows of 4096 bf16 118, 105 and 104; 20000 ids, 30000 rows of 1024 floats 57.3,
+// 56.0 and 58.4.
+constexpr int64_t kCountClears = 24 << 20, kPlaceClears = 40 << 20;
+// Workgroups for that, three per CU.  256, 768 and 2048 of them, the same tables: 82.7, 83.7 and 83.7 us; 107, 105 and 105; 57.5, 56.0
+// and 55.9.
+constexpr int kSpareGroups = 768;
+// Workgroups that add with few ids: most end at once, for a frequent id's they have to be enough.  1024, 4096 and 16384 of them: 777
+// ids, 10007 rows of 1500 floats 17.3, 18.0 and 19.3 us; 1000 ids, 1000 rows of 8192 (bf16 to floats) 75, 33 and 45; 1024 times one id,
+// rows of 4096 333, 103 and 64.
+constexpr int64_t kFewGroups = 4096;
 
 // f(V) with the elements of a vector: V, or 1 where a row has less.
 template <int V, typename F>
@@ -186,7 +194,7 @@ void with_chosen(int32_t k, F f) {
 }
 
 // f(G) with the lanes that take a row of logits, at least G0: so many that a lane has kLogits of them, but a wave at most.  (The
-// gradient through a softmax over 256 logits, which then reads its row once: 16384 rows 10.7 us with 8 lanes, 9.0 with 32.)
+// gradient through a softmax over 256 logits, which then reads its row once: 16384 rows of floats 13.3 us with 8 lanes, 10.0 with 32.)
 template <int G0, typename F>
 void with_team(int32_t experts, F f) {
     if constexpr (G0 <= 8) {
@@ -199,7 +207,9 @@ void with_team(int32_t experts, F f) {
 
 // Up to so many rows the lanes of a route_kernel team are as many as the logits ask for; above, as few as the slots allow, for what
 // the lanes do together (merge lists) costs a wave the same whether it has one row or eight.  256 logits, 8 experts, 8 lanes and 32:
-// 64 rows 4.2 and 3.4 us, 2048 rows 4.4 and 3.6, 4096 rows 4.5 and 4.3, 16384 rows 5.9 and 9.3.
+// 64 rows 4.4 and 3.6 us, 2048 rows 4.6 and 3.8, 4096 rows 4.6 and 4.5, 16384 rows 6.0 and 9.5.  Where they meet depends on the lists:
+// 512 logits, 4 experts, 8 lanes and 64: 4096 rows 5.8 and 5.0, 8192 rows 6.6 and 7.3; 1024 logits, 16 experts, 16 lanes and 64: 2048
+// rows 7.5 both, 4096 rows 8.2 and 11.4; 1024 logits, 2 experts, 8 and 64: 8192 rows 9.4 and 8.0, 16384 rows 13.9 and 14.7.
 constexpr int32_t kFewRows = 4096;
 
 int launched() {

@@ -174,7 +174,7 @@ def route(logits, k, bias=None, keep=None, score="softmax", normalise=True, scal
     """(chosen int32 [rows, k], weight float32 [rows, k]): the k experts of each row with the largest logits (plus bias,
     which only the choice sees), and their weights; -1 and 0 where a row has no expert left.
 
-    bias: float32 [experts]; keep: bool [rows], False for rows that go to no expert (padding)."""
+    bias: float32 [experts], on the logit (not on its sigmoid, where some routers have it); keep: bool [rows], False for rows that go to no expert (padding)."""
     ltype, stride = _rows(logits, "logits")
     rows, experts = logits.shape
     dev = logits.device
