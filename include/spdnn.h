@@ -377,6 +377,69 @@ int spdnn_combine_grad(const void* dout, int32_t type, int32_t width, int64_t do
                        const int32_t* place, const float* weight, const int32_t* count, int32_t rows, int32_t k, void* dys,
                        int64_t dys_stride, float* dweight, void* hip_stream);
 
+/* ---- Dense products around the networks --------------------------------------------------------------------------------
+ *
+ * What a mixture computes besides: the layer norm before the router, the router's own product, and products with every
+ * expert's own weights on the rows that spdnn_dispatch has sorted; and the gradients.  The rules of the row operators above
+ * hold here too: no handle, arguments checked before any HIP call, no allocation, copy or wait, results that do not depend on
+ * timing, sums in 32 bits that are rounded once, rows of any stride (a row of weight may not be shared by dweight) and any
+ * alignment that the element type has, outputs that overlap no input.  Two calls that may run at the same time (on two
+ * streams, or in two graphs) need work memory of their own. */
+enum { SPDNN_ACT_NONE = 0, SPDNN_ACT_RELU = 1, SPDNN_ACT_CLIP = 2, SPDNN_ACT_GELU = 3, SPDNN_ACT_SILU = 4 };
+
+/* out[t] = act(x[t] W + b) + add[t] for rows x width matrices x, width x cols matrices W.
+ *   type      : of x and weight; out, pre and add are of out_type, type or SPDNN_F32.
+ *   offsets   : NULL: one W for all rows (experts = 1).  Otherwise device int32[experts + 1], ascending from 0 as spdnn_dispatch
+ *               gives them: rows offsets[e] .. offsets[e+1]-1 take W_e and b_e; out and pre are zero in the rows from
+ *               offsets[experts] on, where neither x nor add are read.  (Offsets that do not ascend within 0 .. rows give rows
+ *               that are wrong or not written; nothing outside the arrays is read or written.)
+ *   weight    : W[i][c] at weight[i * weight_stride + c], or at weight[c * weight_stride + i] if transposed; expert_stride
+ *               elements between experts' matrices.
+ *   bias      : experts x cols numbers of bias_type (type or SPDNN_F32), or NULL.
+ *   act       : SPDNN_ACT_NONE y, RELU max(y, 0), CLIP min(max(y, 0), 32), GELU y (1 + erf(y / sqrt 2)) / 2,
+ *               SILU y / (1 + exp(-y)); a NaN stays one.  It is taken of the sum in 32 bits.
+ *   add       : a residual, or NULL.
+ *   pre       : if not NULL, receives x[t] W + b (rounded to out_type), what spdnn_linear_grad starts from.
+ * 1 <= experts <= SPDNN_MAX_EXPERTS, 1 <= width, cols <= 2^30.  work: device memory, 256-byte aligned, >= spdnn_linear_bytes
+ * (grouped: whether offsets are given); contents scratch. */
+int spdnn_linear_bytes(int32_t rows, int32_t width, int32_t cols, int32_t grouped, int32_t experts, int32_t type, size_t* bytes);
+int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64_t x_stride, const int32_t* offsets,
+                 int32_t experts, const void* weight, int32_t transposed, int64_t weight_stride, int64_t expert_stride,
+                 int32_t cols, const void* bias, int32_t bias_type, int32_t act, const void* add, int64_t add_stride, void* out,
+                 int32_t out_type, int64_t out_stride, void* pre, int64_t pre_stride, void* work, size_t work_bytes,
+                 void* hip_stream);
+
+/* Gradients of spdnn_linear for the gradient dout of out (that of add is dout).  With d[t] = dout[t] * act'(pre[t]):
+ * dx[t] = d[t] W^T, of type; dW_e = sum over e's rows of x[t]^T d[t], stored as W is (transposed or not); db_e = sum over e's rows of
+ * d[t].  Any of dx, dweight and dbias may be NULL: it is not computed then, and x (only dweight needs it) and weight (only
+ * dx) are not read.
+ *   dout_type : of dout and pre, type or SPDNN_F32.  d is rounded to type for the products, where it is not dout itself.
+ *   grad_type : of dweight and dbias, type or SPDNN_F32.
+ * dx is zero in the rows of no expert, dweight and dbias for experts without rows.  Slopes: RELU 0 up to 0, CLIP 0 up to 0 and from 32 on. */
+int spdnn_linear_grad_bytes(int32_t rows, int32_t width, int32_t cols, int32_t grouped, int32_t experts, int32_t type,
+                            int32_t dout_type, int32_t act, int32_t transposed, size_t* bytes);
+int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, const void* pre, int64_t pre_stride, int32_t act,
+                      const void* x, int32_t type, int32_t rows, int32_t width, int64_t x_stride, const int32_t* offsets,
+                      int32_t experts, const void* weight, int32_t transposed, int64_t weight_stride, int64_t expert_stride,
+                      int32_t cols, void* dx, int64_t dx_stride, void* dweight, int64_t dweight_stride, int64_t dexpert_stride,
+                      void* dbias, int32_t grad_type, void* work, size_t work_bytes, void* hip_stream);
+
+/* out[t] = (x[t] - mean) * rstd * weight + bias, mean over the row's width numbers, rstd = 1 / sqrt(variance + eps), the variance
+ * that of the differences from the mean.  weight and bias: width numbers of param_type (type or SPDNN_F32), or NULL (ones,
+ * zeros); out_type: type or SPDNN_F32; stats: rows x 2 floats (mean, rstd) for spdnn_layer_norm_grad, or NULL. */
+int spdnn_layer_norm(const void* x, int32_t type, int32_t rows, int32_t width, int64_t x_stride, const void* weight,
+                     const void* bias, int32_t param_type, float eps, void* out, int32_t out_type, int64_t out_stride, float* stats,
+                     void* hip_stream);
+
+/* Gradients.  With h = (x - mean) * rstd and g = dout * weight: dx = rstd * (g - mean(g) - h * mean(g * h)) + add (the gradient
+ * that x has from elsewhere, in a residual block; may be NULL); dweight = sum over rows of dout * h, dbias = sum of dout, of grad_type
+ * (type or SPDNN_F32); either may be NULL.  x, dout, add and dx are of type.  work: as above, needed for dweight and dbias. */
+int spdnn_layer_norm_grad_bytes(int32_t rows, int32_t width, size_t* bytes);
+int spdnn_layer_norm_grad(const void* dout, int32_t type, int64_t dout_stride, const void* x, int32_t rows, int32_t width,
+                          int64_t x_stride, const float* stats, const void* weight, int32_t param_type, const void* add,
+                          int64_t add_stride, void* dx, int64_t dx_stride, void* dweight, void* dbias, int32_t grad_type, void* work,
+                          size_t work_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

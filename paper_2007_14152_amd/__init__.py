@@ -41,6 +41,11 @@ SPDNN_I32 = 0
 SPDNN_I64 = 1
 SPDNN_SOFTMAX = 0
 SPDNN_SIGMOID = 1
+SPDNN_ACT_NONE = 0
+SPDNN_ACT_RELU = 1
+SPDNN_ACT_CLIP = 2
+SPDNN_ACT_GELU = 3
+SPDNN_ACT_SILU = 4
 SPDNN_MAX_EXPERTS = 1024
 SPDNN_MAX_CHOSEN = 16
 
@@ -51,7 +56,9 @@ EXPORTS = ("spdnn_weights_bytes", "spdnn_work_bytes", "spdnn_create", "spdnn_inf
            "spdnn_csr_passes", "spdnn_create_csr", "spdnn_layer_passes", "spdnn_ooc_bytes", "spdnn_create_ooc",
            "spdnn_one_launch", "spdnn_get_launches", "spdnn_row_kernel",
            "spdnn_embed", "spdnn_embed_grad_bytes", "spdnn_embed_grad", "spdnn_route", "spdnn_route_grad",
-           "spdnn_dispatch_bytes", "spdnn_dispatch", "spdnn_combine", "spdnn_combine_grad")
+           "spdnn_dispatch_bytes", "spdnn_dispatch", "spdnn_combine", "spdnn_combine_grad",
+           "spdnn_linear_bytes", "spdnn_linear", "spdnn_linear_grad_bytes", "spdnn_linear_grad",
+           "spdnn_layer_norm", "spdnn_layer_norm_grad_bytes", "spdnn_layer_norm_grad")
 KERNEL_NAMES = {0: "fused_layer_kernel<false>", 1: "fused_layer_kernel<true>", 2: "fused_wide_kernel",
                 3: "fused_pair_kernel", 4: "fused_wide_pair_kernel", 5: "fused_wide_pair4_kernel", 6: "fused_row2_kernel",
                 7: "fused_flat_kernel"}
@@ -109,6 +116,15 @@ def lib():
         L.spdnn_dispatch.argtypes = [vp, i32, i32, i32, vp, i32, i32, i64, vp, i64, vp, vp, vp, sz, vp]
         L.spdnn_combine.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, vp, i64, vp, i64, vp]
         L.spdnn_combine_grad.argtypes = [vp, i32, i32, i64, vp, i64, vp, vp, vp, i32, i32, vp, i64, vp, vp]
+        L.spdnn_linear_bytes.argtypes = [i32, i32, i32, i32, i32, i32, psz]
+        L.spdnn_linear.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, i32, i64, i64, i32, vp, i32, i32, vp, i64, vp, i32, i64, vp, i64,
+                                   vp, sz, vp]
+        L.spdnn_linear_grad_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, i32, psz]
+        L.spdnn_linear_grad.argtypes = [vp, i32, i64, vp, i64, i32, vp, i32, i32, i32, i64, vp, i32, vp, i32, i64, i64, i32, vp, i64,
+                                        vp, i64, i64, vp, i32, vp, sz, vp]
+        L.spdnn_layer_norm.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, f32, vp, i32, i64, vp, vp]
+        L.spdnn_layer_norm_grad_bytes.argtypes = [i32, i32, psz]
+        L.spdnn_layer_norm_grad.argtypes = [vp, i32, i64, vp, i32, i32, i64, vp, vp, i32, vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]
         for n in EXPORTS:
             if n != "spdnn_last_error":
                 getattr(L, n).restype = ctypes.c_int
@@ -496,9 +512,17 @@ class Model:
 ROW_OPERATORS = ("embed", "embed_grad", "route", "route_grad", "dispatch", "dispatch_grad", "combine", "combine_grad")
 
 
+# Dense products and layer norm around them (dense.py).
+DENSE_OPERATORS = ("linear", "linear_grad", "grouped_linear", "grouped_linear_grad", "layer_norm", "layer_norm_grad")
+
+
 def __getattr__(name):
     if name in ROW_OPERATORS:
         from . import rows
         globals().update({n: getattr(rows, n) for n in ROW_OPERATORS})
+        return globals()[name]
+    if name in DENSE_OPERATORS:
+        from . import dense
+        globals().update({n: getattr(dense, n) for n in DENSE_OPERATORS})
         return globals()[name]
     raise AttributeError("module %r has no attribute %r" % (__name__, name))

@@ -7,47 +7,17 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "spdnn_check.h"
 #include "spdnn_error.h"
 #include "spdnn_rows_kernels.h"
 
 namespace {
 
-using spdnn::fail;
+using namespace spdnn;
 
-constexpr size_t kAlign = 256;
 constexpr int64_t kMostPairs = 1 << 30;   // rows * k
-constexpr int32_t kMostWidth = 1 << 30;   // columns: a vector beyond a row's end must not pass 32 bits
 constexpr int64_t kMostGroups = 1 << 20;  // workgroups of a launch; more rows take turns
 
-int size_of(int32_t type) { return type == SPDNN_F32 ? 4 : type == SPDNN_BF16 || type == SPDNN_F16 ? 2 : 0; }
-
-// A matrix of rows: not NULL where there is a row, aligned to its elements; rows that are written are apart from each other.
-enum Access { kRead, kWritten };
-int check_rows(const char* what, const void* p, int32_t type, int64_t rows, int32_t width, int64_t stride, Access access) {
-    const int size = size_of(type);
-    if (!size) return fail(SPDNN_EINVAL, "%s: type must be SPDNN_F32, SPDNN_BF16 or SPDNN_F16", what);
-    if (stride < (access == kWritten ? width : 0))
-        return fail(SPDNN_EINVAL, "%s: a stride of %lld elements, width %d", what, (long long)stride, width);
-    if (rows > 0 && stride > INT64_MAX / 8 / rows) return fail(SPDNN_EINVAL, "%s: stride %lld is too large", what, (long long)stride);
-    if (rows > 0 && !p) return fail(SPDNN_EINVAL, "%s is NULL", what);
-    if (reinterpret_cast<uintptr_t>(p) % size) return fail(SPDNN_EINVAL, "%s is not aligned to its elements", what);
-    return SPDNN_OK;
-}
-int check_array(const char* what, const void* p, int64_t n, int size) {
-    if (n > 0 && !p) return fail(SPDNN_EINVAL, "%s is NULL", what);
-    if (reinterpret_cast<uintptr_t>(p) % size) return fail(SPDNN_EINVAL, "%s is not aligned to its elements", what);
-    return SPDNN_OK;
-}
-#define CHECK(expr)                        \
-    do {                                   \
-        const int rc_ = (expr);            \
-        if (rc_ != SPDNN_OK) return rc_;   \
-    } while (0)
-
-int check_width(int32_t width) {
-    if (width < 1 || width > kMostWidth) return fail(SPDNN_EINVAL, "need 1 <= width <= %d", kMostWidth);
-    return SPDNN_OK;
-}
 int check_pairs(int32_t rows, int32_t k, int32_t experts) {
     if (rows < 0) return fail(SPDNN_EINVAL, "rows < 0");
     if (k < 1 || k > SPDNN_MAX_CHOSEN) return fail(SPDNN_EINVAL, "need 1 <= k <= %d", SPDNN_MAX_CHOSEN);
@@ -61,13 +31,6 @@ int check_route(int32_t rows, int32_t experts, int32_t k, const float* bias, int
     if (score != SPDNN_SOFTMAX && score != SPDNN_SIGMOID) return fail(SPDNN_EINVAL, "score must be SPDNN_SOFTMAX or SPDNN_SIGMOID");
     return check_array("bias", bias, 0, 4);
 }
-int check_work(const void* work, size_t bytes, size_t need) {
-    if (bytes < need) return fail(SPDNN_ESIZE, "work has %zu bytes, %zu needed", bytes, need);
-    if (need && !work) return fail(SPDNN_EINVAL, "work is NULL");
-    if (reinterpret_cast<uintptr_t>(work) % kAlign) return fail(SPDNN_EINVAL, "work must be 256-byte aligned");
-    return SPDNN_OK;
-}
-
 dim3 groups(int64_t n) { return dim3((unsigned)std::max<int64_t>(1, std::min(n, kMostGroups))); }
 
 // Outputs of this many bytes go past the caches, for whoever reads them next does not find them there (256 MB at the most) anyway,
@@ -107,13 +70,6 @@ dim3 groups(const spdnn::Tiles& g) {
     return dim3((unsigned)x, (unsigned)std::min((g.vecs + g.slab - 1) / g.slab, 1024));
 }
 
-// f(T{}) with the C++ type of an SPDNN_F32 ...
-template <typename F>
-void with_type(int32_t type, F f) {
-    if (type == SPDNN_F32) f(float{});
-    else if (type == SPDNN_BF16) f(__bf16{});
-    else f(_Float16{});
-}
 template <typename F>
 void with_ids(int32_t type, F f) {
     if (type == SPDNN_I32) f(int32_t{});
@@ -211,11 +167,6 @@ void with_team(int32_t experts, F f) {
 // 512 logits, 4 experts, 8 lanes and 64: 4096 rows 5.8 and 5.0, 8192 rows 6.6 and 7.3; 1024 logits, 16 experts, 16 lanes and 64: 2048
 // rows 7.5 both, 4096 rows 8.2 and 11.4; 1024 logits, 2 experts, 8 and 64: 8192 rows 9.4 and 8.0, 16384 rows 13.9 and 14.7.
 constexpr int32_t kFewRows = 4096;
-
-int launched() {
-    HIP_TRY(hipGetLastError());
-    return SPDNN_OK;
-}
 
 }  // namespace
 
