@@ -16,7 +16,7 @@ namespace {
 using namespace spdnn;
 
 constexpr int64_t kMostGroups = 1 << 20;
-constexpr int64_t kMostTiles = 1 << 30;
+constexpr int64_t kMostTiles = 1 << 30;  // of a launch
 
 int step_of(int32_t type) { return type == SPDNN_F32 ? 32 : 64; }
 size_t aligned(size_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
@@ -52,55 +52,114 @@ int check_output(const char* what, const void* p, int32_t out_type, int32_t type
     return SPDNN_OK;
 }
 
-// How a product is cut.
-constexpr int kTile = 128;
-struct Cut {
-    int64_t mtiles, ntiles;
-    int64_t splits, per_split;  // of k
-    size_t parts;               // bytes
+// How a product is cut: into tiles of bm x bn, and of k (a multiple of a step each).
+struct Plan {
+    bool dma;      // operands go straight to LDS
+    int few;       // linear_short_kernel: fragments of rows in a tile (1, 2 or 4); 0: linear_kernel
+    bool narrow;   // and whether its tiles have 16 columns instead of 64
+    int bm, bn;
+    int64_t mtiles, ntiles, splits, per_split;
+    size_t parts;  // bytes
 };
-// Splits: as many as give every CU a workgroup, of kLeastSteps steps of k at least.
-constexpr int64_t kGroupsWanted = 256, kLeastSteps = 8;
-int64_t splits_of(int64_t tiles, int64_t steps) { return std::max<int64_t>(1, std::min(kGroupsWanted / std::max<int64_t>(tiles, 1), steps / kLeastSteps)); }
 
-Cut cut_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t experts, int32_t type) {
-    Cut c;
-    c.mtiles = grouped ? rows / kTile + experts + 1 : ceil_div(rows, kTile);
-    c.ntiles = ceil_div(cols, kTile);
-    const int64_t busy = grouped ? std::min<int64_t>(c.mtiles, rows) : c.mtiles;
+// Workgroups that the CUs ask for at least.
+constexpr int64_t kGroupsWanted = 256;
+// How long n tiles of 128 x 128 take (two workgroups per CU, or one where there are few), and tiles of 256 x 256, one per CU: with 4096 k
+// of bf16 one tile of 128 on a CU takes 48 us, two 74, one of 256 104.
+int64_t cost_128(int64_t n) { return n / 512 * 74 + (n % 512 > 256 ? 74 : n % 512 > 0 ? 48 : 0); }
+int64_t cost_256(int64_t n) { return (n + 255) / 256 * 104; }
+
+Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t experts, int32_t type, bool dma, Adjacent adj) {
+    Plan p{};
+    p.dma = dma;
+    const int64_t sets = grouped ? std::max<int64_t>(1, std::min(experts, rows)) : 1;
     const int64_t steps = ceil_div(k, step_of(type));
-    c.splits = splits_of(busy * c.ntiles, steps);
-    c.per_split = ceil_div(steps, c.splits) * step_of(type);
-    c.splits = ceil_div(k, c.per_split);
-    c.parts = c.splits > 1 ? aligned((size_t)c.splits * rows * cols * sizeof(float)) : 0;
-    return c;
+    const auto tiles = [&](int bm, int bn) { return (grouped ? rows / bm + sets : ceil_div(rows, bm)) * ceil_div(cols, bn); };  // that have rows
+    const int64_t each = ceil_div(rows, sets);
+    int64_t least = 8;  // steps of a split
+    if (dma && each <= (grouped ? 48 : 128)) {
+        p.few = each <= (grouped ? 8 : 16) ? 1 : each <= (grouped ? 20 : 32) ? 2 : 4;
+        p.bm = 16 * p.few;
+        // Tiles of 16 columns where those of 64 leave CUs idle; but columns of adjacent k, or k that are not many: 32 bytes of a row of
+        // W at a time come from memory at two thirds of the rate.  One row: 4096 x 1024 6.2 us with 16 columns, 9.0 with 64; 4096 x 4096
+        // 9.8 and 10.5 (k adjacent 6.0 and 10.0); 16384 x 4096 33.2 and, with k in four splits, 29.3 (k adjacent 21.4).
+        p.narrow = tiles(p.bm, 64) < kGroupsWanted && (adj == Adjacent::K || steps < 128 || grouped);
+        p.bn = p.narrow ? 16 : 64;
+        least = 32;
+    } else if (dma && cost_256(tiles(256, 256)) < cost_128(tiles(128, 128))) {
+        p.bm = p.bn = 256;
+    } else {
+        p.bm = p.bn = 128;
+    }
+    p.mtiles = grouped ? rows / p.bm + experts + 1 : ceil_div(rows, p.bm);
+    p.ntiles = ceil_div(cols, p.bn);
+    p.splits = std::max<int64_t>(1, std::min(kGroupsWanted / std::max<int64_t>(tiles(p.bm, p.bn), 1), steps / least));
+    p.per_split = ceil_div(steps, p.splits) * step_of(type);
+    p.splits = ceil_div(k, p.per_split);
+    p.parts = p.splits > 1 ? aligned((size_t)p.splits * rows * cols * sizeof(float)) : 0;
+    return p;
 }
-Cut cut_grad(int32_t rows, int32_t m, int32_t n, bool grouped, int32_t experts, int32_t type) {
-    Cut c;
-    c.mtiles = ceil_div(m, kTile);
-    c.ntiles = ceil_div(n, kTile);
-    c.splits = splits_of(c.mtiles * c.ntiles * experts, ceil_div(ceil_div(rows, experts), step_of(type)));
-    c.per_split = 0;
-    c.parts = c.splits > 1 ? aligned((size_t)c.splits * experts * m * n * sizeof(float)) : 0;
-    (void)grouped;
-    return c;
-}
-int check_tiles(const Cut& c, int64_t sets) {
-    if ((double)c.mtiles * (double)c.ntiles * (double)c.splits * (double)sets > (double)kMostTiles)
-        return fail(SPDNN_EINVAL, "sizes too large: more than 2^30 tiles");
+int check_tiles(const Plan& p, int32_t sets) {
+    if ((double)p.mtiles * p.ntiles * p.splits * sets > (double)kMostTiles) return fail(SPDNN_EINVAL, "sizes too large: more than 2^30 tiles");
     return SPDNN_OK;
 }
+// The most work memory that any alignment asks for.
+int most_parts(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t experts, int32_t type, size_t* parts) {
+    *parts = 0;
+    for (const Adjacent adj : {Adjacent::K, Adjacent::L})
+        for (const bool dma : {false, true}) {
+            const Plan p = plan_product(rows, k, cols, grouped, experts, type, dma, adj);
+            CHECK(check_tiles(p, 1));
+            *parts = std::max(*parts, p.parts);
+        }
+    return SPDNN_OK;
+}
+Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32_t type, bool dma) {
+    Plan p{};
+    p.dma = dma;
+    const auto tiles = [&](int b) { return ceil_div(m, b) * ceil_div(n, b) * experts; };
+    p.bm = p.bn = dma && cost_256(tiles(256)) < cost_128(tiles(128)) ? 256 : 128;
+    p.mtiles = ceil_div(m, p.bm);
+    p.ntiles = ceil_div(n, p.bn);
+    p.splits = std::max<int64_t>(1, std::min(kGroupsWanted / tiles(p.bm), ceil_div(ceil_div(rows, experts), step_of(type)) / 8));
+    p.parts = p.splits > 1 ? aligned((size_t)p.splits * experts * m * n * sizeof(float)) : 0;
+    return p;
+}
+// Whether an operand can go straight to LDS: everything aligned to 16 bytes, tiles within reach of 32-bit offsets, and rows of k that
+// do not overlap.
+bool dma_side(const Side& s, Adjacent adj, int32_t along, int32_t type) {
+    const int size = size_of(type);
+    if ((uintptr_t)s.p % 16 || s.line % 16 || s.set % 16 || (int64_t)along * size % 16) return false;
+    return s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size);
+}
 
-void run_product(int32_t type, Adjacent adj, const Cut& c, Product p, Ending e, hipStream_t s) {
+template <typename T, Adjacent ADJ, int R>
+void launch_few(const Plan& c, dim3 grid, const Product& p, const Ending& e, hipStream_t s) {
+    constexpr int KW = R == 4 ? 2 : 4, NARROW_KW = R == 4 ? 4 : 8;
+    if (c.narrow) linear_short_kernel<T, ADJ, R, 1, NARROW_KW, 2><<<grid, NARROW_KW * 64, 0, s>>>(p, e);
+    else linear_short_kernel<T, ADJ, R, 4, KW, 2><<<grid, KW * 64, 0, s>>>(p, e);
+}
+template <typename T, Adjacent ADJ>
+void launch_product(const Plan& c, const Product& p, const Ending& e, hipStream_t s) {
+    const dim3 grid((unsigned)(c.mtiles * c.ntiles * c.splits));
+    if (c.few == 1) launch_few<T, ADJ, 1>(c, grid, p, e, s);
+    else if (c.few == 2) launch_few<T, ADJ, 2>(c, grid, p, e, s);
+    else if (c.few == 4) launch_few<T, ADJ, 4>(c, grid, p, e, s);
+    else if (c.bm == 256) linear_kernel<T, ADJ, 8, 2, 4, true><<<grid, 512, 0, s>>>(p, e);
+    else if (c.dma) linear_kernel<T, ADJ, 4, 2, 2, true><<<grid, 256, 0, s>>>(p, e);
+    else linear_kernel<T, ADJ, 4, 2, 2, false><<<grid, 256, 0, s>>>(p, e);
+}
+void run_product(int32_t type, Adjacent adj, Product p, Ending e, hipStream_t s) {
+    const bool dma = dma_side(p.x, Adjacent::K, p.width, type) && dma_side(p.w, adj, adj == Adjacent::K ? p.width : p.cols, type);
+    const Plan c = plan_product(p.rows, p.width, p.cols, p.offsets != nullptr, p.experts, type, dma, adj);
     p.mtiles = (int32_t)c.mtiles;
     p.ntiles = (int32_t)c.ntiles;
     p.splits = (int32_t)c.splits;
     p.per_split = c.per_split;
-    const dim3 grid((unsigned)(c.mtiles * c.ntiles * c.splits));
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
-        if (adj == Adjacent::K) linear_kernel<T, Adjacent::K, 4, 2, 2><<<grid, 256, 0, s>>>(p, e);
-        else linear_kernel<T, Adjacent::L, 4, 2, 2><<<grid, 256, 0, s>>>(p, e);
+        if (adj == Adjacent::K) launch_product<T, Adjacent::K>(c, p, e, s);
+        else launch_product<T, Adjacent::L>(c, p, e, s);
         if (c.splits > 1) {
             const int64_t items = (int64_t)p.rows * ceil_div(p.cols, kEnd);
             linear_join_kernel<T><<<dim3((unsigned)std::min(ceil_div(items, 256), kMostGroups)), 256, 0, s>>>(p, e);
@@ -112,20 +171,26 @@ void run_product(int32_t type, Adjacent adj, const Cut& c, Product p, Ending e, 
 struct GradWork {
     bool own_d;
     int64_t d_stride;  // elements
-    size_t d, parts, bytes;
-    Cut dx, dw;
+    size_t d, bytes;
     int64_t bias_splits;
-    GradWork(int32_t rows, int32_t width, int32_t cols, bool grouped, int32_t experts, int32_t type, int32_t dout_type, int32_t act, int32_t transposed) {
-        own_d = act != SPDNN_ACT_NONE || dout_type != type;
-        d_stride = ceil_div(cols, 16) * 16;
-        d = own_d ? aligned((size_t)rows * d_stride * size_of(type)) : 0;
-        dx = cut_product(rows, cols, width, grouped, experts, type);
-        dw = transposed ? cut_grad(rows, cols, width, grouped, experts, type) : cut_grad(rows, width, cols, grouped, experts, type);
-        bias_splits = std::max<int64_t>(1, std::min(1024 / (ceil_div(cols, 64) * experts), ceil_div(rows, experts) / 32));
-        parts = std::max({dx.parts, dw.parts, bias_splits > 1 ? aligned((size_t)bias_splits * experts * cols * sizeof(float)) : 0});
-        bytes = d + parts;
-    }
 };
+int grad_work(int32_t rows, int32_t width, int32_t cols, bool grouped, int32_t experts, int32_t type, int32_t dout_type, int32_t act, bool transposed,
+              GradWork* w) {
+    w->own_d = act != SPDNN_ACT_NONE || dout_type != type;
+    w->d_stride = ceil_div(cols, 16) * 16;
+    w->d = w->own_d ? aligned((size_t)rows * w->d_stride * size_of(type)) : 0;
+    w->bias_splits = std::max<int64_t>(1, std::min(1024 / (ceil_div(cols, 64) * experts), ceil_div(rows, experts) / 32));
+    size_t parts = 0;
+    CHECK(most_parts(rows, cols, width, grouped, experts, type, &parts));
+    for (const bool dma : {false, true}) {
+        const Plan p = plan_grad(rows, transposed ? cols : width, transposed ? width : cols, experts, type, dma);
+        CHECK(check_tiles(p, experts));
+        parts = std::max(parts, p.parts);
+    }
+    if (w->bias_splits > 1) parts = std::max(parts, aligned((size_t)w->bias_splits * experts * cols * sizeof(float)));
+    w->bytes = w->d + parts;
+    return SPDNN_OK;
+}
 
 int check_act(int32_t act) {
     if (act < SPDNN_ACT_NONE || act > SPDNN_ACT_SILU) return fail(SPDNN_EINVAL, "act must be one of SPDNN_ACT_NONE ... SPDNN_ACT_SILU");
@@ -139,10 +204,7 @@ extern "C" {
 int spdnn_linear_bytes(int32_t rows, int32_t width, int32_t cols, int32_t grouped, int32_t experts, int32_t type, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
     CHECK(check_sizes(rows, width, cols, experts, type));
-    const Cut c = cut_product(rows, width, cols, grouped != 0, experts, type);
-    CHECK(check_tiles(c, 1));
-    *bytes = c.parts;
-    return SPDNN_OK;
+    return most_parts(rows, width, cols, grouped != 0, experts, type, bytes);
 }
 
 int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64_t x_stride, const int32_t* offsets, int32_t experts,
@@ -166,7 +228,6 @@ int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64
     CHECK(check_work(work, work_bytes, need));
     if (rows == 0) return SPDNN_OK;
     const int size = size_of(type), out_size = size_of(out_type);
-    const Cut c = cut_product(rows, width, cols, offsets != nullptr, experts, type);
     Product p{};
     p.x = {(const char*)x, x_stride * size, 0};
     p.w = {(const char*)weight, weight_stride * size, expert_stride * size};
@@ -188,7 +249,7 @@ int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64
     e.cols = cols;
     e.act = act;
     e.out_f32 = out_type == SPDNN_F32;
-    run_product(type, transposed ? Adjacent::K : Adjacent::L, c, p, e, (hipStream_t)hip_stream);
+    run_product(type, transposed ? Adjacent::K : Adjacent::L, p, e, (hipStream_t)hip_stream);
     return launched();
 }
 
@@ -198,9 +259,8 @@ int spdnn_linear_grad_bytes(int32_t rows, int32_t width, int32_t cols, int32_t g
     CHECK(check_sizes(rows, width, cols, experts, type));
     CHECK(check_output("dout", nullptr, dout_type, type));
     CHECK(check_act(act));
-    const GradWork w(rows, width, cols, grouped != 0, experts, type, dout_type, act, transposed);
-    CHECK(check_tiles(w.dx, 1));
-    CHECK(check_tiles(w.dw, experts));
+    GradWork w;
+    CHECK(grad_work(rows, width, cols, grouped != 0, experts, type, dout_type, act, transposed != 0, &w));
     *bytes = w.bytes;
     return SPDNN_OK;
 }
@@ -226,7 +286,8 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
     if (dbias) CHECK(check_array("dbias", dbias, 0, size_of(grad_type)));
     CHECK(check_work(work, work_bytes, need));
     const hipStream_t s = (hipStream_t)hip_stream;
-    const GradWork w(rows, width, cols, offsets != nullptr, experts, type, dout_type, act, transposed);
+    GradWork w;
+    CHECK(grad_work(rows, width, cols, offsets != nullptr, experts, type, dout_type, act, transposed != 0, &w));
     const int size = size_of(type);
     float* const parts = (float*)((char*)work + w.d);
     const void* d = dout;
@@ -262,7 +323,7 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         e.cols = width;
         e.act = SPDNN_ACT_NONE;
         e.out_f32 = type == SPDNN_F32;
-        run_product(type, transposed ? Adjacent::L : Adjacent::K, w.dx, p, e, s);
+        run_product(type, transposed ? Adjacent::L : Adjacent::K, p, e, s);
     }
     if (dweight) {
         const Side sx{(const char*)x, x_stride * size, 0}, sd{(const char*)d, d_stride * size, 0};
@@ -274,10 +335,12 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         p.m = transposed ? cols : width;
         p.n = transposed ? width : cols;
         p.experts = experts;
-        p.mtiles = (int32_t)w.dw.mtiles;
-        p.ntiles = (int32_t)w.dw.ntiles;
-        p.splits = (int32_t)w.dw.splits;
         p.parts = parts;
+        const bool dma = dma_side(p.a, Adjacent::L, p.m, type) && dma_side(p.b, Adjacent::L, p.n, type);
+        const Plan c = plan_grad(rows, p.m, p.n, experts, type, dma);
+        p.mtiles = (int32_t)c.mtiles;
+        p.ntiles = (int32_t)c.ntiles;
+        p.splits = (int32_t)c.splits;
         Ending e{};
         e.out = (char*)dweight;
         e.out_line = dweight_stride * size_of(grad_type);
@@ -287,8 +350,11 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         e.out_f32 = grad_type == SPDNN_F32;
         with_type(type, [&](auto tt) {
             using T = decltype(tt);
-            weight_grad_kernel<T, 4, 2, 2><<<dim3((unsigned)(w.dw.mtiles * w.dw.ntiles * experts * w.dw.splits)), 256, 0, s>>>(p, e);
-            if (w.dw.splits > 1) {
+            const dim3 grid((unsigned)(c.mtiles * c.ntiles * experts * c.splits));
+            if (c.bm == 256) weight_grad_kernel<T, 8, 2, 4, true><<<grid, 512, 0, s>>>(p, e);
+            else if (c.dma) weight_grad_kernel<T, 4, 2, 2, true><<<grid, 256, 0, s>>>(p, e);
+            else weight_grad_kernel<T, 4, 2, 2, false><<<grid, 256, 0, s>>>(p, e);
+            if (c.splits > 1) {
                 const int64_t items = (int64_t)experts * p.m * ceil_div(p.n, kEnd);
                 weight_grad_join_kernel<T><<<dim3((unsigned)std::min(ceil_div(items, 256), kMostGroups)), 256, 0, s>>>(p, e);
             }

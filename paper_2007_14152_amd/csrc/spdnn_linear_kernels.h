@@ -153,6 +153,62 @@ struct ByRegisters {
     }
 };
 
+// Loads of a tile straight into LDS, 16 bytes a lane.  What is not there comes as zeros, from the range check of the buffer: lines
+// beyond the last, and what lies behind the last k (Adjacent::K: a lane whose chunk does has kOutside added to its offset).  Lines and
+// the first chunk are aligned to 16 bytes and have whole chunks, a tile's lines lie within kDmaSpan bytes, and the k rows of
+// Adjacent::L do not overlap.
+//
+// They are written as instructions: the compiler would let the transposing LDS reads wait for all loads of this kind that are under way,
+// for it cannot tell that they go to the other stage.  Whoever reads what they have stored waits with loads_done() and a barrier first.
+constexpr uint32_t kOutside = 1u << 31;
+using Memory __attribute__((ext_vector_type(4))) = int;  // address, bytes, format: the same for all lanes
+__device__ inline void load_to_lds(Memory memory, uint32_t offset, char* lds, const int more) {
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane((int)to)), "i"(more), "v"(offset), "s"(memory)
+                 : "memory", "scc", "m0");
+}
+__device__ inline void loads_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+constexpr int64_t kDmaSpan = 1 << 30;
+template <typename T, Adjacent ADJ, int LINES, int THREADS>
+struct ByDma {
+    using G = Tile<T, ADJ, LINES, THREADS>;
+    static constexpr int kRows = THREADS / G::kPerRow;  // memory rows that all lanes take at a time
+    // The swizzle repeats after so many of them (16 rows): a lane's offsets are that many and multiples of a number that all share.
+    static constexpr int kBases = kRows % 16 == 0 ? 1 : 16 / kRows;
+    static_assert(kRows % 16 == 0 || 16 % kRows == 0);
+    static_assert(G::kChunks % kBases == 0);
+    uint32_t from[kBases];
+    uint32_t line, step;
+    __device__ void begin(int64_t line_bytes, int thread) {
+        line = (uint32_t)line_bytes;
+        step = kRows * kBases * line;
+#pragma unroll
+        for (int c = 0; c < kBases; ++c) {
+            const auto at = G::at(c * THREADS + thread);
+            from[c] = (uint32_t)at.row * line + at.chunk * 16;
+        }
+    }
+    // lines, ks: what there is of both from p on.
+    __device__ void load(const char* p, char* tile, int lines, int64_t ks, int thread, int wave) const {
+        const int k = (int)min(ks, (int64_t)G::kStep);  // nothing is loaded if there is none
+        const uint32_t bytes = k <= 0 ? 0 : ADJ == Adjacent::K ? (lines - 1) * line + k * (uint32_t)sizeof(T) : (k - 1) * line + lines * (uint32_t)sizeof(T);
+        const uint64_t base = (uint64_t)p;
+        const Memory memory = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff),
+                               __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+        uint32_t at[kBases];
+#pragma unroll
+        for (int c = 0; c < kBases; ++c) at[c] = from[c];
+        if (ADJ == Adjacent::K && k < G::kStep)
+#pragma unroll
+            for (int c = 0; c < kBases; ++c)
+                if (G::at(c * THREADS + thread).chunk * G::kChunk >= k) at[c] += kOutside;
+#pragma unroll
+        for (int c = 0; c < G::kChunks; ++c) load_to_lds(memory, at[c % kBases] + c / kBases * step, tile + wave * 1024, c * (THREADS * 16));
+    }
+};
+
 // --- what is done with the sums ---------------------------------------------
 
 struct Ending {
@@ -292,7 +348,7 @@ struct Shape {
     static constexpr int kN = WN * 64;
 };
 
-template <typename T, Adjacent AA, Adjacent AB, int MF, int WM, int WN>
+template <typename T, Adjacent AA, Adjacent AB, int MF, int WM, int WN, bool DMA>
 struct TileProduct {
     using S = Shape<T, MF, WM, WN>;
     using A = Tile<T, AA, S::kM, S::kThreads>;
@@ -317,6 +373,36 @@ struct TileProduct {
                 for (int n = 0; n < 4; ++n) acc[m][n] = mma(b[n], a[m], acc[m][n]);
         }
     }
+    static constexpr int kPart = MF / 2 > 0 ? MF / 2 : 1;
+    static constexpr int kReadsA = kPart * (AA == Adjacent::K ? 1 : sizeof(T) == 2 ? 2 : 4);
+    static constexpr int kReadsB = 4 * (AB == Adjacent::K ? 1 : sizeof(T) == 2 ? 2 : 4);
+    __device__ static void read_b(const char* stage, int half, int lane, int wn, Frag<T> (&b)[4]) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) b[n] = B::read(stage + A::kBytes, wn * 64 + n * 16, half, lane);
+    }
+    __device__ static void read_a(const char* stage, int half, int part, int lane, int wm, Frag<T> (&a)[kPart]) {
+#pragma unroll
+        for (int m = 0; m < kPart; ++m) a[m] = A::read(stage, (wm * MF + part * kPart + m) * 16, half, lane);
+    }
+    template <int PART>
+    __device__ void multiply(const Frag<T> (&a)[kPart], const Frag<T> (&b)[4]) {
+#pragma unroll
+        for (int m = 0; m < kPart; ++m)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) acc[PART * kPart + m][n] = mma(b[n], a[m], acc[PART * kPart + m][n]);
+    }
+    // READS reads of what comes next between the products of now.
+    template <int READS>
+    __device__ static void interleave() {
+        constexpr int kProducts = kPart * 4 * (sizeof(T) == 2 ? 1 : 4);
+        constexpr int kBetween = kProducts / READS > 0 ? kProducts / READS : 1;
+        constexpr int kTogether = (READS + kProducts - 1) / kProducts;
+#pragma unroll
+        for (int i = 0; i < READS / kTogether; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, kTogether, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, kBetween, 0);
+        }
+    }
     // a, b: the first number of the tile's lines at the first k; alines, blines: lines there are; ks: k there are.
     __device__ void run(char* lds, const char* a, int64_t aline, int alines, const char* b, int64_t bline, int blines, int64_t ks) {
         const int thread = threadIdx.x, lane = thread % 64, wave = thread / 64, wm = wave / WN, wn = wave % WN;
@@ -326,6 +412,59 @@ struct TileProduct {
             for (int n = 0; n < 4; ++n) acc[m][n] = Acc{0, 0, 0, 0};
         const int64_t astep = AA == Adjacent::K ? 128 : aline * A::kStep;
         const int64_t bstep = AB == Adjacent::K ? 128 : bline * B::kStep;
+        if constexpr (DMA) {
+            const int w = __builtin_amdgcn_readfirstlane(wave);
+            ByDma<T, AA, S::kM, S::kThreads> da;
+            ByDma<T, AB, S::kN, S::kThreads> db;
+            da.begin(aline, thread);
+            db.begin(bline, thread);
+            const auto load = [&](char* to) {
+                da.load(a, to, alines, ks, thread, w);
+                db.load(b, to + A::kBytes, blines, ks, thread, w);
+                ks -= A::kStep;
+                a += astep;
+                b += bstep;
+            };
+            if (ks <= 0) return;
+            // Four parts a step: while the products of one run, what the next needs is read.  The reads of the last part are those of the next
+            // step's first (behind the last step, of what stands there, which nothing uses).
+            Frag<T> fa[2][kPart], fb[2][4];
+            int64_t steps = (ks + A::kStep - 1) / A::kStep;
+            load(lds);
+            loads_done();
+            __builtin_amdgcn_s_barrier();
+            if (ks > 0) load(lds + kStage);
+            int at = 0;
+            read_b(lds, 0, lane, wn, fb[0]);
+            read_a(lds, 0, 0, lane, wm, fa[0]);
+            do {
+                const char* now = lds + at;
+                read_a(now, 0, 1, lane, wm, fa[1]);
+                multiply<0>(fa[0], fb[0]);
+                interleave<kReadsA>();
+                read_b(now, 1, lane, wn, fb[1]);
+                read_a(now, 1, 0, lane, wm, fa[0]);
+                multiply<1>(fa[1], fb[0]);
+                interleave<kReadsA + kReadsB>();
+                read_a(now, 1, 1, lane, wm, fa[1]);
+                multiply<0>(fa[0], fb[1]);
+                interleave<kReadsA>();
+                __builtin_amdgcn_sched_barrier(0);
+                loads_done();
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                if (ks > 0) load(lds + at);
+                at = kStage - at;
+                now = lds + at;
+                read_b(now, 0, lane, wn, fb[0]);
+                read_a(now, 0, 0, lane, wm, fa[0]);
+                multiply<1>(fa[1], fb[1]);
+                interleave<kReadsA + kReadsB>();
+                __builtin_amdgcn_sched_barrier(0);
+            } while (--steps > 0);
+            __syncthreads();
+            return;
+        }
         ByRegisters<T, AA, S::kM, S::kThreads> ra;
         ByRegisters<T, AB, S::kN, S::kThreads> rb;
         char* now = lds;
@@ -394,9 +533,9 @@ struct Product {
     float* parts;
 };
 
-template <typename T, Adjacent AB, int MF, int WM, int WN>
+template <typename T, Adjacent AB, int MF, int WM, int WN, bool DMA>
 __global__ __launch_bounds__(WM* WN * 64) void linear_kernel(Product p, Ending e) {
-    using P = TileProduct<T, Adjacent::K, AB, MF, WM, WN>;
+    using P = TileProduct<T, Adjacent::K, AB, MF, WM, WN, DMA>;
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const int per = p.mtiles * p.ntiles;
@@ -433,6 +572,114 @@ __global__ __launch_bounds__(WM* WN * 64) void linear_kernel(Product p, Ending e
                 if (col + i < p.cols) to[i] = sum[i];
         }
     });
+}
+
+// The same for few rows (R * 16 of a tile), where the weights' bytes are what counts.  Every wave has all of the tile (NF * 16 columns) and
+// every KW-th step of k, for which it keeps D stages of its own in LDS under way, without a barrier; the waves' sums are added in order.
+template <typename T, Adjacent AB, int R, int NF, int KW, int D>
+__global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending e) {
+    using A = Tile<T, Adjacent::K, R * 16, 64>;
+    using B = Tile<T, AB, NF * 16, 64>;
+    constexpr int kStage = A::kBytes + B::kBytes, kOwn = D * kStage, kSums = R * 16 * NF * 64;
+    static_assert(kSums <= kOwn);
+    constexpr int BM = R * 16, BN = NF * 16;
+    __shared__ __align__(16) char lds[KW * kOwn];
+    const int per = p.mtiles * p.ntiles;
+    const int t = xcd_order(blockIdx.x, gridDim.x);
+    const int split = t / per;
+    const TileAt tile = banded(t - split * per, p.mtiles, p.ntiles, 8);
+    const RowTile r = row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
+    if (r.first >= r.last) return;
+    const int n0 = tile.n * BN;
+    if (r.set == p.experts) {  // rows of no expert
+        if (split == 0 && p.splits == 1)
+            for (int64_t row = r.first + threadIdx.x / (BN / kEnd); row < min(r.last, r.first + BM); row += KW * 64 / (BN / kEnd)) {
+                const int col = n0 + threadIdx.x % (BN / kEnd) * kEnd;
+                if (col < p.cols) end_zeros<T>(e, row, col);
+            }
+        return;
+    }
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t k0 = split * p.per_split + wave * A::kStep;
+    int64_t ks = min(p.per_split - wave * A::kStep, p.width - k0);  // from this wave's first step on
+    const int alines = (int)min((int64_t)BM, r.last - r.first), blines = min(BN, p.cols - n0);
+    const char* a = p.x.p + r.first * p.x.line + k0 * (int64_t)sizeof(T);
+    const char* b = p.w.p + r.set * p.w.set + (AB == Adjacent::K ? n0 * p.w.line + k0 * (int64_t)sizeof(T) : k0 * p.w.line + n0 * (int64_t)sizeof(T));
+    const int64_t astep = KW * 128, bstep = AB == Adjacent::K ? KW * 128 : p.w.line * A::kStep * KW;
+    ByDma<T, Adjacent::K, R * 16, 64> da;
+    ByDma<T, AB, BN, 64> db;
+    da.begin(p.x.line, lane);
+    db.begin(p.w.line, lane);
+    char* const own = lds + wave * kOwn;
+    const auto load = [&](int stage) {
+        da.load(a, own + stage * kStage, alines, ks, lane, 0);
+        db.load(b, own + stage * kStage + A::kBytes, blines, ks, lane, 0);
+        ks -= KW * A::kStep;
+        a += astep;
+        b += bstep;
+    };
+    Acc acc[R][NF];
+#pragma unroll
+    for (int m = 0; m < R; ++m)
+#pragma unroll
+        for (int n = 0; n < NF; ++n) acc[m][n] = Acc{0, 0, 0, 0};
+    int64_t steps = ks > 0 ? (ks - 1) / (KW * A::kStep) + 1 : 0;
+#pragma unroll
+    for (int i = 0; i < D; ++i) load(i);
+    int stage = 0;
+    for (; steps > 0; --steps) {
+        constexpr int kLater = (D - 1) * (A::kChunks + B::kChunks);  // loads that were asked for behind this stage's
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLater) : "memory");
+        Frag<T> fa[2][R], fb[2][NF];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int n = 0; n < NF; ++n) fb[half][n] = B::read(own + stage * kStage + A::kBytes, n * 16, half, lane);
+#pragma unroll
+            for (int m = 0; m < R; ++m) fa[half][m] = A::read(own + stage * kStage, m * 16, half, lane);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load(stage);
+        stage = stage == D - 1 ? 0 : stage + 1;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int m = 0; m < R; ++m)
+#pragma unroll
+                for (int n = 0; n < NF; ++n) acc[m][n] = mma(fb[half][n], fa[half][m], acc[m][n]);
+    }
+    loads_done();  // (those behind the last step too: they store zeros)
+#pragma unroll
+    for (int m = 0; m < R; ++m)
+#pragma unroll
+        for (int n = 0; n < NF; ++n)
+            *reinterpret_cast<Acc*>(own + (m * 16 + lane % 16) * (NF * 64) + ((n * 4 + lane / 16) ^ (lane % (NF * 4))) * 16) = acc[m][n];
+    __syncthreads();
+    for (int i = threadIdx.x; i < BM * (BN / kEnd); i += KW * 64) {
+        const int line = i / (BN / kEnd), c = i % (BN / kEnd) * 2;
+        const int64_t row = r.first + line;
+        const int col = n0 + c * 4;
+        if (row >= r.last || col >= p.cols) continue;
+        float sum[kEnd] = {};
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+            const Acc lo = *reinterpret_cast<const Acc*>(lds + w * kOwn + line * (NF * 64) + (c ^ (line % (NF * 4))) * 16);
+            const Acc hi = *reinterpret_cast<const Acc*>(lds + w * kOwn + line * (NF * 64) + ((c + 1) ^ (line % (NF * 4))) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sum[j] += lo[j];
+                sum[j + 4] += hi[j];
+            }
+        }
+        if (p.splits == 1) {
+            end_sums<T>(e, r.set, row, col, sum);
+        } else {
+            float* const to = p.parts + ((int64_t)split * p.rows + row) * p.cols + col;
+#pragma unroll
+            for (int j = 0; j < kEnd; ++j)
+                if (col + j < p.cols) to[j] = sum[j];
+        }
+    }
 }
 
 // Parts of sums added up, split by split.
@@ -531,9 +778,9 @@ __device__ inline RowRange grad_rows(const int32_t* offsets, int32_t rows, int s
     return {first, min(first + per, last)};
 }
 
-template <typename T, int MF, int WM, int WN>
+template <typename T, int MF, int WM, int WN, bool DMA>
 __global__ __launch_bounds__(WM* WN * 64) void weight_grad_kernel(WeightGrad p, Ending e) {
-    using P = TileProduct<T, Adjacent::L, Adjacent::L, MF, WM, WN>;
+    using P = TileProduct<T, Adjacent::L, Adjacent::L, MF, WM, WN, DMA>;
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const int per = p.mtiles * p.ntiles;

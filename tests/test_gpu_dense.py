@@ -67,7 +67,9 @@ def loads(seed, rows, experts, dropped=0):
 
 # one token to a few hundred, sizes around a fragment, a step of k, a tile; several tiles; splits
 SIZES = [(1, 1, 1), (1, 64, 64), (1, 4096, 64), (2, 7, 5), (3, 33, 130), (15, 32, 16), (16, 31, 17), (17, 64, 100), (33, 65, 63), (64, 128, 128),
-         (65, 100, 200), (127, 96, 129), (129, 250, 127), (257, 64, 300), (300, 777, 520), (5, 8200, 96), (1000, 48, 33)]
+         (65, 100, 200), (127, 96, 129), (129, 250, 127), (257, 64, 300), (300, 777, 520), (5, 8200, 96), (1000, 48, 33),
+         # chunks of 16 bytes, and steps of k that are not whole
+         (40, 72, 136), (130, 1000, 264), (90, 520, 40), (200, 8, 8), (1, 8200, 4104), (20, 136, 4160)]
 
 
 @pytest.mark.parametrize("layout", ["dense", "part"])
@@ -106,6 +108,39 @@ def test_linear_grad_exact(sp, rows, width, cols, dtype, transposed):
     part = sp.linear_grad(laid(dout, "one"), x.to(DEV), stored(w, transposed), for_x=False, for_bias=False)
     assert part[0] is None and part[2] is None
     equal(part[1], x.double().t() @ dout.double())
+
+
+# many tiles: more rows and columns than 256 CUs take at a time in tiles of 128
+MANY = [(2900, 200, 2904), (2905, 136, 3000), (8200, 24, 1100), (1030, 328, 8136), (2900, 77, 2903)]
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("rows,width,cols", MANY)
+def test_many_tiles_exact(sp, rows, width, cols, dtype, transposed):
+    g = torch.Generator().manual_seed(rows + width + cols)
+    x, w, bias = whole(g, (rows, width), dtype), whole(g, (width, cols), dtype), whole(g, (cols,), dtype, 9)
+    equal(sp.linear(x.to(DEV), stored(w, transposed), bias=bias.to(DEV), act="relu"), (x.double() @ w.double() + bias.double()).clamp(min=0), "out")
+    # the same numbers as a gradient: of W [cols, rows], whose batch is the width
+    d, y = x.t().contiguous(), w
+    dw = sp.linear_grad(y.to(DEV), d.to(DEV), stored(whole(g, (rows, cols), dtype), transposed), dtype=F32, for_x=False, for_bias=False)[1]
+    equal(dw, d.double().t() @ y.double(), "dweight")
+    dx = sp.linear_grad(x.to(DEV), torch.zeros(rows, cols, dtype=dtype, device=DEV), stored(w.t().contiguous(), transposed), for_weight=False)[0]
+    equal(dx, x.double() @ w.double(), "dx")
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dtype", ref.TYPES)
+def test_many_grouped_tiles_exact(sp, dtype, transposed):
+    g = torch.Generator().manual_seed(6)
+    rows, experts, width, cols = 9000, 5, 104, 1800
+    offsets = torch.tensor([0, 3000, 3000, 3007, 6500, 8800], dtype=torch.int32)
+    x, w, dout = whole(g, (rows, width), dtype), whole(g, (experts, width, cols), dtype), whole(g, (rows, cols), dtype)
+    want, grads = ref.linear(x, w, offsets=offsets)[0], ref.linear_grad(dout, x, w, offsets=offsets)[0]
+    x[8800:], dout[8800:] = float("nan"), float("nan")
+    equal(sp.grouped_linear(x.to(DEV), offsets.to(DEV), stored(w, transposed)), want)
+    for what, a, b in zip(("dx", "dweight", "dbias"), sp.grouped_linear_grad(dout.to(DEV), x.to(DEV), offsets.to(DEV), stored(w, transposed), dtype=F32), grads):
+        equal(a, b, what)
 
 
 GROUPS = [(1, 2, 64, 64, 0), (8, 256, 64, 80, 0), (40, 3, 33, 50, 7), (256, 64, 128, 64, 20), (300, 5, 65, 130, 0), (513, 300, 40, 24, 100),
