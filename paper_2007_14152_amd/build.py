@@ -12,13 +12,15 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(CSRC, "libspdnn.so")
 SOURCES = [os.path.join(CSRC, "spdnn.hip"), os.path.join(CSRC, "spdnn_rows.hip"), os.path.join(CSRC, "spdnn_linear.hip"),
+           os.path.join(CSRC, "spdnn_linear_f32.hip"), os.path.join(CSRC, "spdnn_linear_bf16.hip"), os.path.join(CSRC, "spdnn_linear_f16.hip"),
            os.path.join(CSRC, "spdnn_norm.hip")]
 HEADERS = [os.path.join(CSRC, "spdnn_kernels.h"), os.path.join(CSRC, "spdnn_order.h"),
            os.path.join(CSRC, "spdnn_layout.h"), os.path.join(CSRC, "spdnn_row2.h"),
            os.path.join(CSRC, "spdnn_flat.h"), os.path.join(CSRC, "spdnn_resident.h"), os.path.join(CSRC, "spdnn_few.h"), os.path.join(CSRC, "spdnn_strided.h"), os.path.join(CSRC, "spdnn_cut.h"),
            os.path.join(CSRC, "spdnn_profile.h"),
            os.path.join(CSRC, "spdnn_error.h"), os.path.join(CSRC, "spdnn_rows_kernels.h"),
-           os.path.join(CSRC, "spdnn_check.h"), os.path.join(CSRC, "spdnn_vec.h"), os.path.join(CSRC, "spdnn_linear_kernels.h"), os.path.join(CSRC, "spdnn_norm_kernels.h"),
+           os.path.join(CSRC, "spdnn_check.h"), os.path.join(CSRC, "spdnn_vec.h"), os.path.join(CSRC, "spdnn_linear_kernels.h"),
+           os.path.join(CSRC, "spdnn_linear_launch.h"), os.path.join(CSRC, "spdnn_linear_typed.h"), os.path.join(CSRC, "spdnn_norm_kernels.h"),
            os.path.join(os.path.dirname(_HERE), "include", "spdnn.h")]
 # host build of the connection-ordering routine, for tests of the set-up logic without a GPU
 ORDER_HOST_LIB = os.path.join(CSRC, "libspdnn_order_host.so")

@@ -9,7 +9,7 @@
 
 #include "spdnn_check.h"
 #include "spdnn_error.h"
-#include "spdnn_linear_kernels.h"
+#include "spdnn_linear_launch.h"
 
 namespace {
 
@@ -51,16 +51,6 @@ int check_output(const char* what, const void* p, int32_t out_type, int32_t type
     (void)p;
     return SPDNN_OK;
 }
-
-// How a product is cut: into tiles of bm x bn, and of k (a multiple of a step each).
-struct Plan {
-    bool dma;      // operands go straight to LDS
-    int few;       // linear_short_kernel: fragments of rows in a tile (1, 2 or 4); 0: linear_kernel
-    bool narrow;   // and whether its tiles have 16 columns instead of 64
-    int bm, bn;
-    int64_t mtiles, ntiles, splits, per_split;
-    size_t parts;  // bytes
-};
 
 // Workgroups that the CUs ask for at least.
 constexpr int64_t kGroupsWanted = 256;
@@ -133,22 +123,6 @@ bool dma_side(const Side& s, Adjacent adj, int32_t along, int32_t type) {
     return s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size);
 }
 
-template <typename T, Adjacent ADJ, int R>
-void launch_few(const Plan& c, dim3 grid, const Product& p, const Ending& e, hipStream_t s) {
-    constexpr int KW = R == 4 ? 2 : 4, NARROW_KW = R == 4 ? 4 : 8;
-    if (c.narrow) linear_short_kernel<T, ADJ, R, 1, NARROW_KW, 2><<<grid, NARROW_KW * 64, 0, s>>>(p, e);
-    else linear_short_kernel<T, ADJ, R, 4, KW, 2><<<grid, KW * 64, 0, s>>>(p, e);
-}
-template <typename T, Adjacent ADJ>
-void launch_product(const Plan& c, const Product& p, const Ending& e, hipStream_t s) {
-    const dim3 grid((unsigned)(c.mtiles * c.ntiles * c.splits));
-    if (c.few == 1) launch_few<T, ADJ, 1>(c, grid, p, e, s);
-    else if (c.few == 2) launch_few<T, ADJ, 2>(c, grid, p, e, s);
-    else if (c.few == 4) launch_few<T, ADJ, 4>(c, grid, p, e, s);
-    else if (c.bm == 256) linear_kernel<T, ADJ, 8, 2, 4, true><<<grid, 512, 0, s>>>(p, e);
-    else if (c.dma) linear_kernel<T, ADJ, 4, 2, 2, true><<<grid, 256, 0, s>>>(p, e);
-    else linear_kernel<T, ADJ, 4, 2, 2, false><<<grid, 256, 0, s>>>(p, e);
-}
 void run_product(int32_t type, Adjacent adj, Product p, Ending e, hipStream_t s) {
     const bool dma = dma_side(p.x, Adjacent::K, p.width, type) && dma_side(p.w, adj, adj == Adjacent::K ? p.width : p.cols, type);
     const Plan c = plan_product(p.rows, p.width, p.cols, p.offsets != nullptr, p.experts, type, dma, adj);
@@ -156,15 +130,7 @@ void run_product(int32_t type, Adjacent adj, Product p, Ending e, hipStream_t s)
     p.ntiles = (int32_t)c.ntiles;
     p.splits = (int32_t)c.splits;
     p.per_split = c.per_split;
-    with_type(type, [&](auto tt) {
-        using T = decltype(tt);
-        if (adj == Adjacent::K) launch_product<T, Adjacent::K>(c, p, e, s);
-        else launch_product<T, Adjacent::L>(c, p, e, s);
-        if (c.splits > 1) {
-            const int64_t items = (int64_t)p.rows * ceil_div(p.cols, kEnd);
-            linear_join_kernel<T><<<dim3((unsigned)std::min(ceil_div(items, 256), kMostGroups)), 256, 0, s>>>(p, e);
-        }
-    });
+    with_type(type, [&](auto tt) { launch_product<decltype(tt)>(c, adj, p, e, s); });
 }
 
 // Work memory of the gradients: d in the rows' type where dout is not that already, and parts, which the three steps use in turn.
@@ -185,7 +151,7 @@ int grad_work(int32_t rows, int32_t width, int32_t cols, bool grouped, int32_t e
     for (const bool dma : {false, true}) {
         const Plan p = plan_grad(rows, transposed ? cols : width, transposed ? width : cols, experts, type, dma);
         CHECK(check_tiles(p, experts));
-        parts = std::max(parts, p.parts);
+        parts = std::max(parts, p.parts + (p.splits > 1 ? aligned((size_t)p.splits * experts * cols * sizeof(float)) : 0));
     }
     if (w->bias_splits > 1) parts = std::max(parts, aligned((size_t)w->bias_splits * experts * cols * sizeof(float)));
     w->bytes = w->d + parts;
@@ -295,16 +261,9 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
     if (w.own_d && rows > 0) {
         d = work;
         d_stride = w.d_stride;
-        const int64_t items = (int64_t)rows * ceil_div(cols, 8);
-        const dim3 grid((unsigned)std::min(ceil_div(items, 256), kMostGroups));
         with_type(type, [&](auto tt) {
-            using T = decltype(tt);
-            const auto run = [&](auto td) {
-                using D = decltype(td);
-                slope_kernel<T, D><<<grid, 256, 0, s>>>((const D*)dout, dout_stride, act == SPDNN_ACT_NONE ? nullptr : (const D*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)work, d_stride);
-            };
-            if (dout_type == type) run(T{});
-            else run(float{});
+            launch_slope<decltype(tt)>(dout_type == SPDNN_F32, dout, dout_stride, act == SPDNN_ACT_NONE ? nullptr : pre, pre_stride, act, rows, cols, offsets, experts, work,
+                                       d_stride, s);
         });
     }
     if (dx && rows > 0) {
@@ -341,6 +300,10 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         p.mtiles = (int32_t)c.mtiles;
         p.ntiles = (int32_t)c.ntiles;
         p.splits = (int32_t)c.splits;
+        p.bias_parts = (float*)((char*)parts + c.parts);
+        p.dbias = dbias;
+        p.bias_f32 = grad_type == SPDNN_F32;
+        p.d_is_a = transposed != 0;
         Ending e{};
         e.out = (char*)dweight;
         e.out_line = dweight_stride * size_of(grad_type);
@@ -348,28 +311,12 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         e.cols = p.n;
         e.act = SPDNN_ACT_NONE;
         e.out_f32 = grad_type == SPDNN_F32;
+        with_type(type, [&](auto tt) { launch_weight_grad<decltype(tt)>(c, p, e, s); });
+    } else if (dbias) {
         with_type(type, [&](auto tt) {
-            using T = decltype(tt);
-            const dim3 grid((unsigned)(c.mtiles * c.ntiles * experts * c.splits));
-            if (c.bm == 256) weight_grad_kernel<T, 8, 2, 4, true><<<grid, 512, 0, s>>>(p, e);
-            else if (c.dma) weight_grad_kernel<T, 4, 2, 2, true><<<grid, 256, 0, s>>>(p, e);
-            else weight_grad_kernel<T, 4, 2, 2, false><<<grid, 256, 0, s>>>(p, e);
-            if (c.splits > 1) {
-                const int64_t items = (int64_t)experts * p.m * ceil_div(p.n, kEnd);
-                weight_grad_join_kernel<T><<<dim3((unsigned)std::min(ceil_div(items, 256), kMostGroups)), 256, 0, s>>>(p, e);
-            }
+            launch_bias_grad<decltype(tt)>(d, d_stride, offsets, rows, cols, experts, (int32_t)w.bias_splits, parts, dbias, grad_type == SPDNN_F32, s);
         });
     }
-    if (dbias)
-        with_type(type, [&](auto tt) {
-            using T = decltype(tt);
-            const dim3 grid((unsigned)ceil_div(cols, 64), (unsigned)experts, (unsigned)w.bias_splits);
-            bias_grad_kernel<T><<<grid, 256, 0, s>>>((const T*)d, d_stride, offsets, rows, cols, (int32_t)w.bias_splits, parts, dbias, grad_type == SPDNN_F32);
-            if (w.bias_splits > 1) {
-                const int64_t n = (int64_t)experts * cols;
-                bias_grad_join_kernel<T><<<dim3((unsigned)ceil_div(n, 256)), 256, 0, s>>>(parts, (int32_t)w.bias_splits, n, dbias, grad_type == SPDNN_F32);
-            }
-        });
     return launched();
 }
 

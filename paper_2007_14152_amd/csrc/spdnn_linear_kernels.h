@@ -4,7 +4,9 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
+#include "../../include/spdnn.h"
 #include "spdnn_vec.h"
 
 #pragma clang fp contract(off)
@@ -32,23 +34,46 @@ __device__ inline Acc mma(Frag<float> a, Frag<float> b, Acc c) {  // 4 instructi
 
 constexpr float kClip = 32.0f;  // that of the sparse networks
 
+// exp and erf for results of 16 bits (EXACT: of 32).  exp2 of the hardware: off by an ulp and by 2 U |x| of its argument.  erf by the
+// rational approximation of Abramowitz and Stegun 7.1.26, off by 1.5e-7, with 1 / (1 + p x) from the hardware's reciprocal; expf and
+// erff take three times as many instructions, and the slopes of 8000 x 16384 numbers then take 183 us where memory asks for 125.
+template <bool EXACT>
+__device__ inline float act_exp(float x) {
+    if constexpr (EXACT) return expf(x);
+    else return __builtin_amdgcn_exp2f(x * 1.44269504f);
+}
+template <bool EXACT>
+__device__ inline float act_erf(float x, float exp_of_minus_square) {
+    if constexpr (EXACT) return erff(x);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, fabsf(x), 1.0f));
+    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    return copysignf(fmaf(-poly, exp_of_minus_square, 1.0f), x);
+}
 // A NaN stays one.
-__device__ inline float activated(float x, int act) {
+template <bool EXACT>
+__device__ __forceinline__ float activated(float x, int act) {
     switch (act) {
         case SPDNN_ACT_RELU: return x < 0.0f ? 0.0f : x;
         case SPDNN_ACT_CLIP: return x < 0.0f ? 0.0f : x > kClip ? kClip : x;
-        case SPDNN_ACT_GELU: return 0.5f * x * (1.0f + erff(x * 0.70710678f));
-        case SPDNN_ACT_SILU: return x / (1.0f + expf(-x));
+        case SPDNN_ACT_GELU: {
+            const float z = x * 0.70710678f;
+            return 0.5f * x * (1.0f + act_erf<EXACT>(z, EXACT ? 0.0f : act_exp<EXACT>(-z * z)));
+        }
+        case SPDNN_ACT_SILU: return EXACT ? x / (1.0f + expf(-x)) : x * __builtin_amdgcn_rcpf(1.0f + act_exp<EXACT>(-x));
     }
     return x;
 }
+template <bool EXACT>
 __device__ inline float act_slope(float x, int act) {
     switch (act) {
         case SPDNN_ACT_RELU: return x <= 0.0f ? 0.0f : 1.0f;
         case SPDNN_ACT_CLIP: return x <= 0.0f || x >= kClip ? 0.0f : 1.0f;
-        case SPDNN_ACT_GELU: return 0.5f * (1.0f + erff(x * 0.70710678f)) + x * (0.39894228f * expf(-0.5f * x * x));
+        case SPDNN_ACT_GELU: {
+            const float z = x * 0.70710678f, bell = act_exp<EXACT>(-0.5f * x * x);
+            return fmaf(x, 0.39894228f * bell, 0.5f + 0.5f * act_erf<EXACT>(z, bell));
+        }
         case SPDNN_ACT_SILU: {
-            const float s = 1.0f / (1.0f + expf(-x));
+            const float s = EXACT ? 1.0f / (1.0f + expf(-x)) : __builtin_amdgcn_rcpf(1.0f + act_exp<EXACT>(-x));
             return s + x * s * (1.0f - s);
         }
     }
@@ -228,60 +253,109 @@ struct Ending {
 
 constexpr int kEnd = 8;  // columns that a lane ends at a time
 
-template <typename T, typename O>
-__device__ inline void end_sums(const Ending& e, int set, int64_t row, int col, const float (&sum)[kEnd]) {
-    const int here = min(kEnd, e.cols - col);
-    float y[kEnd];
-#pragma unroll
-    for (int i = 0; i < kEnd; ++i) y[i] = sum[i];
-    if (e.bias) {
+// What the eight columns of a lane need besides their sums, asked for before these are there: b is the same for all rows of a tile.
+using Words __attribute__((ext_vector_type(4))) = float;
+template <typename T>
+struct Biases {
+    float b[kEnd];
+    __device__ __forceinline__ void load(const Ending& e, int set, int col) {
         const int64_t at = (int64_t)set * e.cols + col;
-        const auto take = [&](auto* b) {
-            if (here == kEnd) {
-                const auto v = load_vec<kEnd>(b + at);
 #pragma unroll
-                for (int i = 0; i < kEnd; ++i) y[i] += (float)v[i];
-            } else {
+        for (int i = 0; i < kEnd; ++i) b[i] = 0.0f;
+        if (!e.bias || col + kEnd > e.cols) return;
+        if (e.bias_f32) {
+            const auto v = load_vec<kEnd>((const float*)e.bias + at);
 #pragma unroll
-                for (int i = 0; i < kEnd; ++i)
-                    if (i < here) y[i] += (float)b[at + i];
-            }
-        };
-        if (e.bias_f32) take((const float*)e.bias);
-        else take((const T*)e.bias);
-    }
-    const auto put = [&](char* to, int64_t line) {
-        O* const o = reinterpret_cast<O*>(to + row * line) + col;
-        if (here == kEnd) {
-            store_vec<kEnd, O>(o, rounded_vec<O, kEnd>(y), false);
+            for (int i = 0; i < kEnd; ++i) b[i] = v[i];
         } else {
+            const auto v = load_vec<kEnd>((const T*)e.bias + at);
 #pragma unroll
-            for (int i = 0; i < kEnd; ++i)
-                if (i < here) o[i] = rounded<O>(y[i]);
+            for (int i = 0; i < kEnd; ++i) b[i] = (float)v[i];
         }
-    };
-    if (e.pre) put(e.pre, e.pre_line);
-    if (e.act != SPDNN_ACT_NONE)
+    }
+};
+template <typename T>
+struct Added {
+    Words raw[2];
+    __device__ __forceinline__ void load(const Ending& e, int64_t row, int col) {
+        if (!e.add || col + kEnd > e.cols) return;
+        if constexpr (sizeof(T) == 2)
+            if (!e.out_f32) {
+                raw[0] = __builtin_bit_cast(Words, load_vec<kEnd>(reinterpret_cast<const T*>(e.add + row * e.add_line) + col));
+                return;
+            }
+        const float* const from = reinterpret_cast<const float*>(e.add + row * e.add_line) + col;
+        raw[0] = load_vec<4>(from);
+        raw[1] = load_vec<4>(from + 4);
+    }
+    template <typename O>
+    __device__ __forceinline__ void add_to(float (&y)[kEnd]) const {
+        if constexpr (sizeof(O) == 4) {
 #pragma unroll
-        for (int i = 0; i < kEnd; ++i) y[i] = activated(y[i], e.act);
-    if (e.add) {
-        const O* const a = reinterpret_cast<const O*>(e.add + row * e.add_line) + col;
-        if (here == kEnd) {
-            const auto v = load_vec<kEnd>(a);
+            for (int i = 0; i < kEnd; ++i) y[i] += raw[i / 4][i % 4];
+        } else {
+            typedef O Eight __attribute__((ext_vector_type(8)));
+            const Eight v = __builtin_bit_cast(Eight, raw[0]);
 #pragma unroll
             for (int i = 0; i < kEnd; ++i) y[i] += (float)v[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < kEnd; ++i)
-                if (i < here) y[i] += (float)a[i];
         }
     }
-    put(e.out + set * e.out_set, e.out_line);
+};
+
+// One number, where a row has less than eight left.
+template <typename T, typename O>
+__device__ inline void end_one(const Ending& e, int set, int64_t row, int col, float y) {
+    if (e.bias) {
+        const int64_t at = (int64_t)set * e.cols + col;
+        y += e.bias_f32 ? ((const float*)e.bias)[at] : (float)((const T*)e.bias)[at];
+    }
+    if (e.pre) reinterpret_cast<O*>(e.pre + row * e.pre_line)[col] = rounded<O>(y);
+    y = activated<sizeof(O) == 4>(y, e.act);
+    if (e.add) y += (float)reinterpret_cast<const O*>(e.add + row * e.add_line)[col];
+    reinterpret_cast<O*>(e.out + set * e.out_set + row * e.out_line)[col] = rounded<O>(y);
 }
+template <typename T, typename O>
+__device__ __forceinline__ void end_eight(const Ending& e, int set, int64_t row, int col, float (&y)[kEnd], const Biases<T>& bias, const Added<T>& added) {
+#pragma unroll
+    for (int i = 0; i < kEnd; ++i) y[i] += bias.b[i];
+    if (e.pre) store_vec<kEnd, O>(reinterpret_cast<O*>(e.pre + row * e.pre_line) + col, rounded_vec<O, kEnd>(y), false);
+    if (e.act != SPDNN_ACT_NONE)
+#pragma unroll
+        for (int i = 0; i < kEnd; ++i) y[i] = activated<sizeof(O) == 4>(y[i], e.act);
+    if (e.add) added.template add_to<O>(y);
+    store_vec<kEnd, O>(reinterpret_cast<O*>(e.out + set * e.out_set + row * e.out_line) + col, rounded_vec<O, kEnd>(y), false);
+}
+// one(i): the sum of column col + i, wanted where the row has less than eight.
+template <typename T, typename F>
+__device__ __forceinline__ void end_sums(const Ending& e, int set, int64_t row, int col, float (&sum)[kEnd], const Biases<T>& bias, const Added<T>& added, F one) {
+    const bool f32 = sizeof(T) == 2 && e.out_f32;
+    if (col + kEnd <= e.cols) {
+        if (f32) end_eight<T, float>(e, set, row, col, sum, bias, added);
+        else end_eight<T, T>(e, set, row, col, sum, bias, added);
+    } else {
+#pragma unroll 1
+        for (int i = 0; col + i < e.cols; ++i) {
+            if (f32) end_one<T, float>(e, set, row, col + i, one(i));
+            else end_one<T, T>(e, set, row, col + i, one(i));
+        }
+    }
+}
+// For sums that a lane has in registers.
 template <typename T>
-__device__ inline void end_sums(const Ending& e, int set, int64_t row, int col, const float (&sum)[kEnd]) {
-    if (sizeof(T) == 2 && e.out_f32) end_sums<T, float>(e, set, row, col, sum);
-    else end_sums<T, T>(e, set, row, col, sum);
+__device__ __forceinline__ void join_end(const Ending& e, int set, int64_t row, int col, float (&sum)[kEnd]) {
+    Biases<T> bias;
+    Added<T> added;
+    bias.load(e, set, col);
+    added.load(e, row, col);
+    float kept[kEnd];
+#pragma unroll
+    for (int i = 0; i < kEnd; ++i) kept[i] = sum[i];
+    end_sums<T>(e, set, row, col, sum, bias, added, [&](int j) {
+        float one = 0;
+#pragma unroll
+        for (int i = 0; i < kEnd; ++i) one = i == j ? kept[i] : one;
+        return one;
+    });
 }
 // Zeros, for rows of no expert.
 template <typename T>
@@ -358,22 +432,23 @@ struct TileProduct {
     static constexpr int kLds = 2 * kStage > kEndBytes ? 2 * kStage : kEndBytes;
 
     Acc acc[MF][4];
+    Acc sums[MF > 4 ? MF : 4];  // over k of the lines of b (OF_B) or of a (OF_A): products with ones, beside the others
 
-    __device__ void step(const char* stage, int lane, int wm, int wn) {
+    enum { NO_SUMS = 0, OF_A = 1, OF_B = 2 };
+    template <int OF>
+    __device__ __forceinline__ void step(const char* stage, int lane, int wm, int wn) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            Frag<T> a[MF], b[4];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) b[n] = B::read(stage + A::kBytes, wn * 64 + n * 16, half, lane);
-#pragma unroll
-            for (int m = 0; m < MF; ++m) a[m] = A::read(stage, (wm * MF + m) * 16, half, lane);
-#pragma unroll
-            for (int m = 0; m < MF; ++m)
-#pragma unroll
-                for (int n = 0; n < 4; ++n) acc[m][n] = mma(b[n], a[m], acc[m][n]);
+            Frag<T> a[2][kPart], b[4];
+            read_b(stage, half, lane, wn, b);
+            read_a(stage, half, 0, lane, wm, a[0]);
+            read_a(stage, half, 1, lane, wm, a[1]);
+            multiply<0, OF>(a[0], b);
+            multiply<1, OF>(a[1], b);
         }
     }
-    static constexpr int kPart = MF / 2 > 0 ? MF / 2 : 1;
+    static_assert(MF % 2 == 0);
+    static constexpr int kPart = MF / 2;
     static constexpr int kReadsA = kPart * (AA == Adjacent::K ? 1 : sizeof(T) == 2 ? 2 : 4);
     static constexpr int kReadsB = 4 * (AB == Adjacent::K ? 1 : sizeof(T) == 2 ? 2 : 4);
     __device__ static void read_b(const char* stage, int half, int lane, int wn, Frag<T> (&b)[4]) {
@@ -384,8 +459,16 @@ struct TileProduct {
 #pragma unroll
         for (int m = 0; m < kPart; ++m) a[m] = A::read(stage, (wm * MF + part * kPart + m) * 16, half, lane);
     }
-    template <int PART>
-    __device__ void multiply(const Frag<T> (&a)[kPart], const Frag<T> (&b)[4]) {
+    template <int PART, int OF>
+    __device__ __forceinline__ void multiply(const Frag<T> (&a)[kPart], const Frag<T> (&b)[4]) {
+        Frag<T> ones;
+        for (int i = 0; i < A::kChunk; ++i) ones[i] = (T)1.0f;
+        if constexpr (OF == OF_B && PART == 0)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) sums[n] = mma(b[n], ones, sums[n]);
+        if constexpr (OF == OF_A)
+#pragma unroll
+            for (int m = 0; m < kPart; ++m) sums[PART * kPart + m] = mma(ones, a[m], sums[PART * kPart + m]);
 #pragma unroll
         for (int m = 0; m < kPart; ++m)
 #pragma unroll
@@ -404,12 +487,16 @@ struct TileProduct {
         }
     }
     // a, b: the first number of the tile's lines at the first k; alines, blines: lines there are; ks: k there are.
-    __device__ void run(char* lds, const char* a, int64_t aline, int alines, const char* b, int64_t bline, int blines, int64_t ks) {
+    template <int OF>
+    __device__ __forceinline__ void run(char* lds, const char* a, int64_t aline, int alines, const char* b, int64_t bline, int blines, int64_t ks) {
         const int thread = threadIdx.x, lane = thread % 64, wave = thread / 64, wm = wave / WN, wn = wave % WN;
 #pragma unroll
         for (int m = 0; m < MF; ++m)
 #pragma unroll
             for (int n = 0; n < 4; ++n) acc[m][n] = Acc{0, 0, 0, 0};
+        if constexpr (OF != NO_SUMS)
+#pragma unroll
+            for (int i = 0; i < (OF == OF_A ? MF : 4); ++i) sums[i] = Acc{0, 0, 0, 0};
         const int64_t astep = AA == Adjacent::K ? 128 : aline * A::kStep;
         const int64_t bstep = AB == Adjacent::K ? 128 : bline * B::kStep;
         if constexpr (DMA) {
@@ -440,14 +527,14 @@ struct TileProduct {
             do {
                 const char* now = lds + at;
                 read_a(now, 0, 1, lane, wm, fa[1]);
-                multiply<0>(fa[0], fb[0]);
+                multiply<0, OF>(fa[0], fb[0]);
                 interleave<kReadsA>();
                 read_b(now, 1, lane, wn, fb[1]);
                 read_a(now, 1, 0, lane, wm, fa[0]);
-                multiply<1>(fa[1], fb[0]);
+                multiply<1, OF>(fa[1], fb[0]);
                 interleave<kReadsA + kReadsB>();
                 read_a(now, 1, 1, lane, wm, fa[1]);
-                multiply<0>(fa[0], fb[1]);
+                multiply<0, OF>(fa[0], fb[1]);
                 interleave<kReadsA>();
                 __builtin_amdgcn_sched_barrier(0);
                 loads_done();
@@ -458,7 +545,7 @@ struct TileProduct {
                 now = lds + at;
                 read_b(now, 0, lane, wn, fb[0]);
                 read_a(now, 0, 0, lane, wm, fa[0]);
-                multiply<1>(fa[1], fb[1]);
+                multiply<1, OF>(fa[1], fb[1]);
                 interleave<kReadsA + kReadsB>();
                 __builtin_amdgcn_sched_barrier(0);
             } while (--steps > 0);
@@ -484,7 +571,7 @@ struct TileProduct {
                 ra.load(a, aline, alines, ks, thread);
                 rb.load(b, bline, blines, ks, thread);
             }
-            step(now, lane, wm, wn);
+            step<OF>(now, lane, wm, wn);
             if (ks > 0) {
                 ra.store(next, thread);
                 rb.store(next + A::kBytes, thread);
@@ -495,13 +582,16 @@ struct TileProduct {
             next = t;
         }
     }
-    // f(line of a, first of 8 lines of b, sums) for all of the tile, by way of LDS: rows of 64 sums of a wave's own, chunk c of row r at
-    // place c ^ r % 16.
-    template <typename F>
-    __device__ void each(char* lds, F f) {
-        constexpr int kTurn = MF < 4 ? MF : 4;
+    // Ends the tile by way of LDS: rows of 64 sums of a wave's own, chunk c of row r at place c ^ r % 16.  first, last: out's rows; n0: the
+    // first column; parts: where sums go that are not all there yet (rows of out's), or null.  What add has is asked for kAhead rows a
+    // lane at a time: with one workgroup on a CU nothing else hides it.
+    __device__ __forceinline__ void end(char* lds, const Ending& e, int set, int64_t first, int64_t last, int n0, float* parts) {
+        constexpr int kTurn = MF < 4 ? MF : 4, kAhead = kTurn < 2 ? 2 : 4;
         const int thread = threadIdx.x, lane = thread % 64, wave = thread / 64, wm = wave / WN, wn = wave % WN;
         char* const own = lds + wave * (kTurn * 16 * 256);
+        const int c = lane % 8 * 2, col = n0 + wn * 64 + c * 4;
+        Biases<T> bias;
+        if (!parts) bias.load(e, set, col);
 #pragma unroll
         for (int m0 = 0; m0 < MF; m0 += kTurn) {
 #pragma unroll
@@ -511,12 +601,30 @@ struct TileProduct {
                     *reinterpret_cast<Acc*>(own + (m * 16 + lane % 16) * 256 + ((n * 4 + lane / 16) ^ (lane % 16)) * 16) = acc[m0 + m][n];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
-            for (int r0 = 0; r0 < kTurn * 16; r0 += 8) {
-                const int r = r0 + lane / 8, c = lane % 8 * 2;
-                const Acc lo = *reinterpret_cast<const Acc*>(own + r * 256 + (c ^ (r % 16)) * 16);
-                const Acc hi = *reinterpret_cast<const Acc*>(own + r * 256 + ((c + 1) ^ (r % 16)) * 16);
-                const float sum[kEnd] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                f((wm * MF + m0) * 16 + r, wn * 64 + c * 4, sum);
+            for (int r0 = 0; r0 < kTurn * 16; r0 += 8 * kAhead) {
+                const int64_t row0 = first + (wm * MF + m0) * 16 + r0 + lane / 8;
+                Added<T> added[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (!parts && row0 + i * 8 < last) added[i].load(e, row0 + i * 8, col);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int r = r0 + i * 8 + lane / 8;
+                    const int64_t row = row0 + i * 8;
+                    if (row >= last || col >= e.cols) continue;
+                    const char* const at = own + r * 256;
+                    const Acc lo = *reinterpret_cast<const Acc*>(at + (c ^ (r % 16)) * 16);
+                    const Acc hi = *reinterpret_cast<const Acc*>(at + ((c + 1) ^ (r % 16)) * 16);
+                    float sum[kEnd] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    if (parts) {
+                        float* const to = parts + row * e.cols + col;
+#pragma unroll
+                        for (int j = 0; j < kEnd; ++j)
+                            if (col + j < e.cols) to[j] = sum[j];
+                    } else {
+                        end_sums<T>(e, set, row, col, sum, bias, added[i], [&](int j) { return *reinterpret_cast<const float*>(at + ((c + j / 4) ^ (r % 16)) * 16 + j % 4 * 4); });
+                    }
+                }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
@@ -558,20 +666,8 @@ __global__ __launch_bounds__(WM* WN * 64) void linear_kernel(Product p, Ending e
     const char* const a = p.x.p + r.first * p.x.line + k0 * sizeof(T);
     const char* const b = p.w.p + r.set * p.w.set + (AB == Adjacent::K ? n0 * p.w.line + k0 * sizeof(T) : k0 * p.w.line + n0 * sizeof(T));
     P product;
-    product.run(lds, a, p.x.line, (int)min((int64_t)BM, r.last - r.first), b, p.w.line, min(BN, p.cols - n0), ks);
-    product.each(lds, [&](int line, int col, const float(&sum)[kEnd]) {
-        const int64_t row = r.first + line;
-        col += n0;
-        if (row >= r.last || col >= p.cols) return;
-        if (p.splits == 1) {
-            end_sums<T>(e, r.set, row, col, sum);
-        } else {
-            float* const to = p.parts + ((int64_t)split * p.rows + row) * p.cols + col;
-#pragma unroll
-            for (int i = 0; i < kEnd; ++i)
-                if (col + i < p.cols) to[i] = sum[i];
-        }
-    });
+    product.template run<P::NO_SUMS>(lds, a, p.x.line, (int)min((int64_t)BM, r.last - r.first), b, p.w.line, min(BN, p.cols - n0), ks);
+    product.end(lds, e, r.set, r.first, min(r.last, r.first + BM), n0, p.splits > 1 ? p.parts + (int64_t)split * p.rows * p.cols : nullptr);
 }
 
 // The same for few rows (R * 16 of a tile), where the weights' bytes are what counts.  Every wave has all of the tile (NF * 16 columns) and
@@ -672,7 +768,16 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
             }
         }
         if (p.splits == 1) {
-            end_sums<T>(e, r.set, row, col, sum);
+            Biases<T> bias;
+            Added<T> added;
+            bias.load(e, r.set, col);
+            added.load(e, row, col);
+            end_sums<T>(e, r.set, row, col, sum, bias, added, [&](int j) {
+                float one = 0;
+#pragma unroll
+                for (int w = 0; w < KW; ++w) one += *reinterpret_cast<const float*>(lds + w * kOwn + line * (NF * 64) + ((c + j / 4) ^ (line % (NF * 4))) * 16 + j % 4 * 4);
+                return one;
+            });
         } else {
             float* const to = p.parts + ((int64_t)split * p.rows + row) * p.cols + col;
 #pragma unroll
@@ -713,7 +818,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(Product p, Ending e) {
             for (int j = 0; j < kEnd; ++j)
                 if (col + j < p.cols) sum[j] += from[j];
         }
-        end_sums<T>(e, set, row, col, sum);
+        join_end<T>(e, set, row, col, sum);
     }
 }
 
@@ -742,11 +847,11 @@ __global__ __launch_bounds__(256) void slope_kernel(const D* dout, int64_t dout_
             if (at) {
                 const auto z = load_vec<V>(at);
 #pragma unroll
-                for (int j = 0; j < V; ++j) y[j] *= act_slope((float)z[j], act);
+                for (int j = 0; j < V; ++j) y[j] *= act_slope<sizeof(T) == 4>((float)z[j], act);
             }
             store_vec<V, T>(to, rounded_vec<T, V>(y), false);
         } else {
-            for (int j = 0; col + j < cols; ++j) to[j] = rounded<T>((float)from[j] * (at ? act_slope((float)at[j], act) : 1.0f));
+            for (int j = 0; col + j < cols; ++j) to[j] = rounded<T>((float)from[j] * (at ? act_slope<sizeof(T) == 4>((float)at[j], act) : 1.0f));
         }
     }
 }
@@ -759,6 +864,10 @@ struct WeightGrad {
     int32_t rows, m, n, experts;
     int32_t mtiles, ntiles, splits;
     float* parts;
+    float* bias_parts;
+    void* dbias;  // null: not asked for here
+    bool bias_f32;
+    bool d_is_a;
 };
 
 // Rows of expert `set` that split `split` adds.
@@ -792,20 +901,35 @@ __global__ __launch_bounds__(WM* WN * 64) void weight_grad_kernel(WeightGrad p, 
     const char* const a = p.a.p + r.first * p.a.line + m0 * sizeof(T);
     const char* const b = p.b.p + r.first * p.b.line + n0 * sizeof(T);
     P product;
-    product.run(lds, a, p.a.line, min(BM, p.m - m0), b, p.b.line, min(BN, p.n - n0), r.last - r.first);
-    product.each(lds, [&](int line, int col, const float(&sum)[kEnd]) {
-        line += m0;
-        col += n0;
-        if (line >= p.m || col >= p.n) return;
-        if (p.splits == 1) {
-            end_sums<T>(e, set, line, col, sum);
-        } else {
-            float* const to = p.parts + (((int64_t)split * p.experts + set) * p.m + line) * p.n + col;
+    const auto run = [&](auto of) __attribute__((always_inline)) {
+        product.template run<decltype(of)::value>(lds, a, p.a.line, min(BM, p.m - m0), b, p.b.line, min(BN, p.n - n0), r.last - r.first);
+    };
+    // The sums of d's columns: the workgroups of the first tiles along W's other side multiply d with ones besides.  (A pass over d of its
+    // own took 225 us for 8000 x 16384 bf16, beside 920 for the product.)
+    const auto put = [&](int col, int cols, float sum) {
+        if (col >= cols) return;
+        const int64_t at = (int64_t)set * cols + col;
+        if (p.splits > 1) p.bias_parts[split * (int64_t)p.experts * cols + at] = sum;
+        else if (p.bias_f32) ((float*)p.dbias)[at] = sum;
+        else ((T*)p.dbias)[at] = rounded<T>(sum);
+    };
+    const int lane = threadIdx.x % 64, wm = threadIdx.x / 64 / WN, wn = threadIdx.x / 64 % WN;
+    if (p.dbias && !p.d_is_a && tile.m == 0) {
+        run(std::integral_constant<int, P::OF_B>{});
+        if (wm == 0 && lane % 16 == 0)
 #pragma unroll
-            for (int i = 0; i < kEnd; ++i)
-                if (col + i < p.n) to[i] = sum[i];
-        }
-    });
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) put(n0 + wn * 64 + n * 16 + lane / 4 + q, p.n, product.sums[n][q]);
+    } else if (p.dbias && p.d_is_a && tile.n == 0) {
+        run(std::integral_constant<int, P::OF_A>{});
+        if (wn == 0 && lane < 16)
+#pragma unroll
+            for (int m = 0; m < MF; ++m) put(m0 + (wm * MF + m) * 16 + lane, p.m, product.sums[m][0]);
+    } else {
+        run(std::integral_constant<int, P::NO_SUMS>{});
+    }
+    product.end(lds, e, set, m0, min(p.m, m0 + BM), n0, p.splits > 1 ? p.parts + ((int64_t)split * p.experts + set) * p.m * p.n : nullptr);
 }
 
 template <typename T>
@@ -822,7 +946,7 @@ __global__ __launch_bounds__(256) void weight_grad_join_kernel(WeightGrad p, End
             for (int j = 0; j < kEnd; ++j)
                 if (col + j < p.n) sum[j] += from[j];
         }
-        end_sums<T>(e, (int)(line / p.m), line % p.m, col, sum);
+        join_end<T>(e, (int)(line / p.m), line % p.m, col, sum);
     }
 }
 

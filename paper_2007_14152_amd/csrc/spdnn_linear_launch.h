@@ -1,0 +1,34 @@
+// Launches of the dense products' kernels for one type of rows; a translation unit for each (spdnn_linear_f32.hip ...).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "spdnn_linear_kernels.h"
+
+namespace spdnn {
+
+// How a product is cut: into tiles of bm x bn, and of k (a multiple of a step each).
+struct Plan {
+    bool dma;      // operands go straight to LDS
+    int few;       // linear_short_kernel: fragments of rows in a tile (1, 2 or 4); 0: linear_kernel
+    bool narrow;   // and whether its tiles have 16 columns instead of 64
+    int bm, bn;
+    int64_t mtiles, ntiles, splits, per_split;
+    size_t parts;  // bytes
+};
+
+template <typename T>
+void launch_product(const Plan& c, Adjacent adj, const Product& p, const Ending& e, hipStream_t s);
+// dout is of T or of float.
+template <typename T>
+void launch_slope(bool dout_f32, const void* dout, int64_t dout_stride, const void* pre, int64_t pre_stride, int act, int32_t rows, int32_t cols,
+                  const int32_t* offsets, int32_t experts, void* d, int64_t d_stride, hipStream_t s);
+template <typename T>
+void launch_weight_grad(const Plan& c, const WeightGrad& p, const Ending& e, hipStream_t s);
+template <typename T>
+void launch_bias_grad(const void* d, int64_t d_stride, const int32_t* offsets, int32_t rows, int32_t cols, int32_t experts, int32_t splits, float* parts,
+                      void* dbias, bool f32, hipStream_t s);
+
+}  // namespace spdnn
