@@ -52,12 +52,43 @@ int check_output(const char* what, const void* p, int32_t out_type, int32_t type
     return SPDNN_OK;
 }
 
-// Workgroups that the CUs ask for at least.
-constexpr int64_t kGroupsWanted = 256;
-// How long n tiles of 128 x 128 take (two workgroups per CU, or one where there are few), and tiles of 256 x 256, one per CU: with 4096 k
-// of bf16 one tile of 128 on a CU takes 48 us, two 74, one of 256 104.
-int64_t cost_128(int64_t n) { return n / 512 * 74 + (n % 512 > 256 ? 74 : n % 512 > 0 ? 48 : 0); }
-int64_t cost_256(int64_t n) { return (n + 255) / 256 * 104; }
+constexpr int64_t kGroupsWanted = 256;     // workgroups that the CUs ask for at least
+constexpr size_t kMostParts = 256 << 20;  // bytes that sums in parts may take
+
+// How long n tiles of b x b take, us for 4096 k, as measured for one to four workgroups on every CU (a CU holds four of 64, two of 128, one
+// of 256); what is left over of full rounds takes what its own number of workgroups does.
+double cost(int b, int64_t n, int32_t type) {
+    struct Row {
+        int per_cu;
+        double us[4];
+    };
+    static const Row k16[3] = {{4, {36, 39, 48, 56}}, {2, {57, 80}}, {1, {112}}};
+    static const Row k32[3] = {{4, {93, 149, 209, 269}}, {2, {275, 491}}, {1, {966}}};
+    const Row& r = (type == SPDNN_F32 ? k32 : k16)[b == 64 ? 0 : b == 128 ? 1 : 2];
+    const int64_t full = 256 * r.per_cu, rest = n % full;
+    return n / full * r.us[r.per_cu - 1] + (rest ? r.us[(rest - 1) / 256] : 0.0);
+}
+// The tile and the number of parts of k with which `tiles(b)` tiles take least.  Parts are written and read once more, out_bytes a part,
+// which a join of 6 us does at 4 TB/s; a round of workgroups begins and ends in 3 us.  (777 x 1500 x 1021 floats: 110 us with tiles of 128,
+// 40 with tiles of 64.)
+template <typename F>
+void choose(F tiles, int64_t steps, size_t out_bytes, int32_t type, bool dma, int* b, int64_t* splits) {
+    const double of_4096 = (double)steps * step_of(type) / 4096;
+    double best = 1e300;
+    for (const int tile : {256, 128, 64}) {
+        if (!dma && tile != 128) continue;
+        for (int64_t s = 1; s <= 64; s *= 2) {
+            if (s > 1 && (steps / s < 4 || s * out_bytes > kMostParts)) break;
+            const int64_t n = tiles(tile) * s;
+            const double us = cost(tile, n, type) * of_4096 / s + 3.0 * ceil_div(n, 256 * (256 / tile)) + (s > 1 ? 6.0 + 2.0 * s * out_bytes / 4e6 : 0.0);
+            if (us < best) {
+                best = us;
+                *b = tile;
+                *splits = s;
+            }
+        }
+    }
+}
 
 Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t experts, int32_t type, bool dma, Adjacent adj) {
     Plan p{};
@@ -66,7 +97,6 @@ Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t e
     const int64_t steps = ceil_div(k, step_of(type));
     const auto tiles = [&](int bm, int bn) { return (grouped ? rows / bm + sets : ceil_div(rows, bm)) * ceil_div(cols, bn); };  // that have rows
     const int64_t each = ceil_div(rows, sets);
-    int64_t least = 8;  // steps of a split
     if (dma && each <= (grouped ? 48 : 128)) {
         p.few = each <= (grouped ? 8 : 16) ? 1 : each <= (grouped ? 20 : 32) ? 2 : 4;
         p.bm = 16 * p.few;
@@ -75,18 +105,28 @@ Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t e
         // 9.8 and 10.5 (k adjacent 6.0 and 10.0); 16384 x 4096 33.2 and, with k in four splits, 29.3 (k adjacent 21.4).
         p.narrow = tiles(p.bm, 64) < kGroupsWanted && (adj == Adjacent::K || steps < 128 || grouped);
         p.bn = p.narrow ? 16 : 64;
-        least = 32;
-    } else if (dma && cost_256(tiles(256, 256)) < cost_128(tiles(128, 128))) {
-        p.bm = p.bn = 256;
+        p.splits = std::max<int64_t>(1, std::min(kGroupsWanted / std::max<int64_t>(tiles(p.bm, p.bn), 1), steps / 32));
     } else {
-        p.bm = p.bn = 128;
+        choose([&](int b) { return tiles(b, b); }, steps, (size_t)rows * cols * sizeof(float), type, dma, &p.bm, &p.splits);
+        p.bn = p.bm;
     }
     p.mtiles = grouped ? rows / p.bm + experts + 1 : ceil_div(rows, p.bm);
     p.ntiles = ceil_div(cols, p.bn);
-    p.splits = std::max<int64_t>(1, std::min(kGroupsWanted / std::max<int64_t>(tiles(p.bm, p.bn), 1), steps / least));
     p.per_split = ceil_div(steps, p.splits) * step_of(type);
     p.splits = ceil_div(k, p.per_split);
     p.parts = p.splits > 1 ? aligned((size_t)p.splits * rows * cols * sizeof(float)) : 0;
+    return p;
+}
+Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32_t type, bool dma) {
+    Plan p{};
+    p.dma = dma;
+    const auto tiles = [&](int b) { return ceil_div(m, b) * ceil_div(n, b) * experts; };
+    const int64_t steps = std::max<int64_t>(1, ceil_div(ceil_div(rows, experts), step_of(type)));
+    choose(tiles, steps, (size_t)experts * m * n * sizeof(float), type, dma, &p.bm, &p.splits);
+    p.bn = p.bm;
+    p.mtiles = ceil_div(m, p.bm);
+    p.ntiles = ceil_div(n, p.bn);
+    p.parts = p.splits > 1 ? aligned((size_t)p.splits * experts * m * n * sizeof(float)) : 0;
     return p;
 }
 int check_tiles(const Plan& p, int32_t sets) {
@@ -104,23 +144,12 @@ int most_parts(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t expe
         }
     return SPDNN_OK;
 }
-Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32_t type, bool dma) {
-    Plan p{};
-    p.dma = dma;
-    const auto tiles = [&](int b) { return ceil_div(m, b) * ceil_div(n, b) * experts; };
-    p.bm = p.bn = dma && cost_256(tiles(256)) < cost_128(tiles(128)) ? 256 : 128;
-    p.mtiles = ceil_div(m, p.bm);
-    p.ntiles = ceil_div(n, p.bn);
-    p.splits = std::max<int64_t>(1, std::min(kGroupsWanted / tiles(p.bm), ceil_div(ceil_div(rows, experts), step_of(type)) / 8));
-    p.parts = p.splits > 1 ? aligned((size_t)p.splits * experts * m * n * sizeof(float)) : 0;
-    return p;
-}
-// Whether an operand can go straight to LDS: everything aligned to 16 bytes, tiles within reach of 32-bit offsets, and rows of k that
-// do not overlap.
+
+// Whether an operand can go straight to LDS: rows of whole words of 4 bytes, tiles within reach of 32-bit offsets, and rows of k that do
+// not overlap.
 bool dma_side(const Side& s, Adjacent adj, int32_t along, int32_t type) {
     const int size = size_of(type);
-    if ((uintptr_t)s.p % 16 || s.line % 16 || s.set % 16 || (int64_t)along * size % 16) return false;
-    return s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size);
+    return (int64_t)along * size % 4 == 0 && s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size);
 }
 
 void run_product(int32_t type, Adjacent adj, Product p, Ending e, hipStream_t s) {

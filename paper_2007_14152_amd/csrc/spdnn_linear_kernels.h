@@ -179,9 +179,9 @@ struct ByRegisters {
 };
 
 // Loads of a tile straight into LDS, 16 bytes a lane.  What is not there comes as zeros, from the range check of the buffer: lines
-// beyond the last, and what lies behind the last k (Adjacent::K: a lane whose chunk does has kOutside added to its offset).  Lines and
-// the first chunk are aligned to 16 bytes and have whole chunks, a tile's lines lie within kDmaSpan bytes, and the k rows of
-// Adjacent::L do not overlap.
+// beyond the last, and what lies behind the last k (Adjacent::K: a lane whose chunk does has kOutside added to its offset; of a chunk
+// that is there in part, clear() clears the rest).  Addresses may have any alignment; memory rows have whole words of 4 bytes, which is
+// what the range check goes by, a tile's lines lie within kDmaSpan bytes, and the k rows of Adjacent::L do not overlap.
 //
 // They are written as instructions: the compiler would let the transposing LDS reads wait for all loads of this kind that are under way,
 // for it cannot tell that they go to the other stage.  Whoever reads what they have stored waits with loads_done() and a barrier first.
@@ -214,6 +214,13 @@ struct ByDma {
             const auto at = G::at(c * THREADS + thread);
             from[c] = (uint32_t)at.row * line + at.chunk * 16;
         }
+    }
+    // Clears what the last chunk of k has behind the last k: ks of a step that is not whole.  To be called between barriers.
+    __device__ static void clear(char* tile, int ks, int thread) {
+        if constexpr (ADJ == Adjacent::K)
+            for (int line = thread; line < LINES; line += THREADS)
+                for (int i = ks % G::kChunk; i < G::kChunk; ++i)
+                    reinterpret_cast<T*>(tile + line * 128 + (ks / G::kChunk ^ (line >> 1 & 7)) * 16)[i] = (T)0.0f;
     }
     // lines, ks: what there is of both from p on.
     __device__ void load(const char* p, char* tile, int lines, int64_t ks, int thread, int wave) const {
@@ -414,32 +421,37 @@ __device__ inline RowTile row_tile(const int32_t* offsets, int experts, int32_t 
 
 // --- the product of a tile --------------------------------------------------
 //
-// A workgroup of WM x WN waves, each with MF x 4 fragments: WM * MF * 16 lines of a, WN * 64 lines of b.
-template <typename T, int MF, int WM, int WN>
+// A workgroup of WM x WN waves, each with MF x NF fragments: WM * MF * 16 lines of a, WN * NF * 16 lines of b.
+template <int MF, int NF, int WM, int WN>
 struct Shape {
+    static constexpr int kMF = MF, kNF = NF, kWM = WM, kWN = WN;
     static constexpr int kThreads = WM * WN * 64;
     static constexpr int kM = WM * MF * 16;
-    static constexpr int kN = WN * 64;
+    static constexpr int kN = WN * NF * 16;
 };
+using Large = Shape<8, 4, 2, 4>;   // 256 x 256
+using Middle = Shape<4, 4, 2, 2>;  // 128 x 128
+using Small = Shape<2, 2, 2, 2>;   // 64 x 64
 
-template <typename T, Adjacent AA, Adjacent AB, int MF, int WM, int WN, bool DMA>
+template <typename T, Adjacent AA, Adjacent AB, typename SHAPE, bool DMA>
 struct TileProduct {
-    using S = Shape<T, MF, WM, WN>;
+    using S = SHAPE;
+    static constexpr int MF = S::kMF, NF = S::kNF, WM = S::kWM, WN = S::kWN;
     using A = Tile<T, AA, S::kM, S::kThreads>;
     using B = Tile<T, AB, S::kN, S::kThreads>;
     static constexpr int kStage = A::kBytes + B::kBytes;
-    static constexpr int kEndBytes = WM * WN * (MF < 4 ? MF : 4) * 16 * 64 * 4;
+    static constexpr int kEndBytes = WM * WN * (MF < 4 ? MF : 4) * 16 * NF * 64;
     static constexpr int kLds = 2 * kStage > kEndBytes ? 2 * kStage : kEndBytes;
 
-    Acc acc[MF][4];
-    Acc sums[MF > 4 ? MF : 4];  // over k of the lines of b (OF_B) or of a (OF_A): products with ones, beside the others
+    Acc acc[MF][NF];
+    Acc sums[MF > NF ? MF : NF];  // over k of the lines of b (OF_B) or of a (OF_A): products with ones, beside the others
 
     enum { NO_SUMS = 0, OF_A = 1, OF_B = 2 };
     template <int OF>
     __device__ __forceinline__ void step(const char* stage, int lane, int wm, int wn) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            Frag<T> a[2][kPart], b[4];
+            Frag<T> a[2][kPart], b[NF];
             read_b(stage, half, lane, wn, b);
             read_a(stage, half, 0, lane, wm, a[0]);
             read_a(stage, half, 1, lane, wm, a[1]);
@@ -450,34 +462,34 @@ struct TileProduct {
     static_assert(MF % 2 == 0);
     static constexpr int kPart = MF / 2;
     static constexpr int kReadsA = kPart * (AA == Adjacent::K ? 1 : sizeof(T) == 2 ? 2 : 4);
-    static constexpr int kReadsB = 4 * (AB == Adjacent::K ? 1 : sizeof(T) == 2 ? 2 : 4);
-    __device__ static void read_b(const char* stage, int half, int lane, int wn, Frag<T> (&b)[4]) {
+    static constexpr int kReadsB = NF * (AB == Adjacent::K ? 1 : sizeof(T) == 2 ? 2 : 4);
+    __device__ static void read_b(const char* stage, int half, int lane, int wn, Frag<T> (&b)[NF]) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n) b[n] = B::read(stage + A::kBytes, wn * 64 + n * 16, half, lane);
+        for (int n = 0; n < NF; ++n) b[n] = B::read(stage + A::kBytes, (wn * NF + n) * 16, half, lane);
     }
     __device__ static void read_a(const char* stage, int half, int part, int lane, int wm, Frag<T> (&a)[kPart]) {
 #pragma unroll
         for (int m = 0; m < kPart; ++m) a[m] = A::read(stage, (wm * MF + part * kPart + m) * 16, half, lane);
     }
     template <int PART, int OF>
-    __device__ __forceinline__ void multiply(const Frag<T> (&a)[kPart], const Frag<T> (&b)[4]) {
+    __device__ __forceinline__ void multiply(const Frag<T> (&a)[kPart], const Frag<T> (&b)[NF]) {
         Frag<T> ones;
         for (int i = 0; i < A::kChunk; ++i) ones[i] = (T)1.0f;
         if constexpr (OF == OF_B && PART == 0)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) sums[n] = mma(b[n], ones, sums[n]);
+            for (int n = 0; n < NF; ++n) sums[n] = mma(b[n], ones, sums[n]);
         if constexpr (OF == OF_A)
 #pragma unroll
             for (int m = 0; m < kPart; ++m) sums[PART * kPart + m] = mma(ones, a[m], sums[PART * kPart + m]);
 #pragma unroll
         for (int m = 0; m < kPart; ++m)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) acc[PART * kPart + m][n] = mma(b[n], a[m], acc[PART * kPart + m][n]);
+            for (int n = 0; n < NF; ++n) acc[PART * kPart + m][n] = mma(b[n], a[m], acc[PART * kPart + m][n]);
     }
     // READS reads of what comes next between the products of now.
     template <int READS>
     __device__ static void interleave() {
-        constexpr int kProducts = kPart * 4 * (sizeof(T) == 2 ? 1 : 4);
+        constexpr int kProducts = kPart * NF * (sizeof(T) == 2 ? 1 : 4);
         constexpr int kBetween = kProducts / READS > 0 ? kProducts / READS : 1;
         constexpr int kTogether = (READS + kProducts - 1) / kProducts;
 #pragma unroll
@@ -493,10 +505,10 @@ struct TileProduct {
 #pragma unroll
         for (int m = 0; m < MF; ++m)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) acc[m][n] = Acc{0, 0, 0, 0};
+            for (int n = 0; n < NF; ++n) acc[m][n] = Acc{0, 0, 0, 0};
         if constexpr (OF != NO_SUMS)
 #pragma unroll
-            for (int i = 0; i < (OF == OF_A ? MF : 4); ++i) sums[i] = Acc{0, 0, 0, 0};
+            for (int i = 0; i < (OF == OF_A ? MF : NF); ++i) sums[i] = Acc{0, 0, 0, 0};
         const int64_t astep = AA == Adjacent::K ? 128 : aline * A::kStep;
         const int64_t bstep = AB == Adjacent::K ? 128 : bline * B::kStep;
         if constexpr (DMA) {
@@ -515,11 +527,19 @@ struct TileProduct {
             if (ks <= 0) return;
             // Four parts a step: while the products of one run, what the next needs is read.  The reads of the last part are those of the next
             // step's first (behind the last step, of what stands there, which nothing uses).
-            Frag<T> fa[2][kPart], fb[2][4];
+            Frag<T> fa[2][kPart], fb[2][NF];
             int64_t steps = (ks + A::kStep - 1) / A::kStep;
+            const int rest = AA == Adjacent::K || AB == Adjacent::K ? (int)(ks % A::kStep) : 0;  // k of the last step, if it has a chunk in part
+            const auto clear = [&](char* stage) __attribute__((noinline)) {
+                ByDma<T, AA, S::kM, S::kThreads>::clear(stage, rest, threadIdx.x);
+                ByDma<T, AB, S::kN, S::kThreads>::clear(stage + A::kBytes, rest, threadIdx.x);
+                loads_done();
+                __builtin_amdgcn_s_barrier();
+            };
             load(lds);
             loads_done();
             __builtin_amdgcn_s_barrier();
+            if (rest % A::kChunk && steps == 1) clear(lds);
             if (ks > 0) load(lds + kStage);
             int at = 0;
             read_b(lds, 0, lane, wn, fb[0]);
@@ -540,6 +560,7 @@ struct TileProduct {
                 loads_done();
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
+                if (rest % A::kChunk && steps == 2) clear(lds + kStage - at);
                 if (ks > 0) load(lds + at);
                 at = kStage - at;
                 now = lds + at;
@@ -582,14 +603,15 @@ struct TileProduct {
             next = t;
         }
     }
-    // Ends the tile by way of LDS: rows of 64 sums of a wave's own, chunk c of row r at place c ^ r % 16.  first, last: out's rows; n0: the
+    // Ends the tile by way of LDS: rows of NF * 16 sums of a wave's own, chunk c of row r at place c ^ r (its last bits).  first, last: out's rows; n0: the
     // first column; parts: where sums go that are not all there yet (rows of out's), or null.  What add has is asked for kAhead rows a
     // lane at a time: with one workgroup on a CU nothing else hides it.
     __device__ __forceinline__ void end(char* lds, const Ending& e, int set, int64_t first, int64_t last, int n0, float* parts) {
-        constexpr int kTurn = MF < 4 ? MF : 4, kAhead = kTurn < 2 ? 2 : 4;
+        constexpr int kTurn = MF < 4 ? MF : 4, kLanes = NF * 2, kRows = 64 / kLanes, kAhead = kTurn * 16 / kRows < 4 ? kTurn * 16 / kRows : 4;
+        constexpr int kLine = NF * 64, kMask = NF * 4 - 1;
         const int thread = threadIdx.x, lane = thread % 64, wave = thread / 64, wm = wave / WN, wn = wave % WN;
-        char* const own = lds + wave * (kTurn * 16 * 256);
-        const int c = lane % 8 * 2, col = n0 + wn * 64 + c * 4;
+        char* const own = lds + wave * (kTurn * 16 * kLine);
+        const int c = lane % kLanes * 2, col = n0 + wn * (NF * 16) + c * 4;
         Biases<T> bias;
         if (!parts) bias.load(e, set, col);
 #pragma unroll
@@ -597,24 +619,24 @@ struct TileProduct {
 #pragma unroll
             for (int m = 0; m < kTurn; ++m)
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    *reinterpret_cast<Acc*>(own + (m * 16 + lane % 16) * 256 + ((n * 4 + lane / 16) ^ (lane % 16)) * 16) = acc[m0 + m][n];
+                for (int n = 0; n < NF; ++n)
+                    *reinterpret_cast<Acc*>(own + (m * 16 + lane % 16) * kLine + ((n * 4 + lane / 16) ^ (lane & kMask)) * 16) = acc[m0 + m][n];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
-            for (int r0 = 0; r0 < kTurn * 16; r0 += 8 * kAhead) {
-                const int64_t row0 = first + (wm * MF + m0) * 16 + r0 + lane / 8;
+            for (int r0 = 0; r0 < kTurn * 16; r0 += kRows * kAhead) {
+                const int64_t row0 = first + (wm * MF + m0) * 16 + r0 + lane / kLanes;
                 Added<T> added[kAhead];
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i)
-                    if (!parts && row0 + i * 8 < last) added[i].load(e, row0 + i * 8, col);
+                    if (!parts && row0 + i * kRows < last) added[i].load(e, row0 + i * kRows, col);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
-                    const int r = r0 + i * 8 + lane / 8;
-                    const int64_t row = row0 + i * 8;
+                    const int r = r0 + i * kRows + lane / kLanes;
+                    const int64_t row = row0 + i * kRows;
                     if (row >= last || col >= e.cols) continue;
-                    const char* const at = own + r * 256;
-                    const Acc lo = *reinterpret_cast<const Acc*>(at + (c ^ (r % 16)) * 16);
-                    const Acc hi = *reinterpret_cast<const Acc*>(at + ((c + 1) ^ (r % 16)) * 16);
+                    const char* const at = own + r * kLine;
+                    const Acc lo = *reinterpret_cast<const Acc*>(at + (c ^ (r & kMask)) * 16);
+                    const Acc hi = *reinterpret_cast<const Acc*>(at + ((c + 1) ^ (r & kMask)) * 16);
                     float sum[kEnd] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
                     if (parts) {
                         float* const to = parts + row * e.cols + col;
@@ -622,7 +644,7 @@ struct TileProduct {
                         for (int j = 0; j < kEnd; ++j)
                             if (col + j < e.cols) to[j] = sum[j];
                     } else {
-                        end_sums<T>(e, set, row, col, sum, bias, added[i], [&](int j) { return *reinterpret_cast<const float*>(at + ((c + j / 4) ^ (r % 16)) * 16 + j % 4 * 4); });
+                        end_sums<T>(e, set, row, col, sum, bias, added[i], [&](int j) { return *reinterpret_cast<const float*>(at + ((c + j / 4) ^ (r & kMask)) * 16 + j % 4 * 4); });
                     }
                 }
             }
@@ -641,9 +663,9 @@ struct Product {
     float* parts;
 };
 
-template <typename T, Adjacent AB, int MF, int WM, int WN, bool DMA>
-__global__ __launch_bounds__(WM* WN * 64) void linear_kernel(Product p, Ending e) {
-    using P = TileProduct<T, Adjacent::K, AB, MF, WM, WN, DMA>;
+template <typename T, Adjacent AB, typename SHAPE, bool DMA>
+__global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Ending e) {
+    using P = TileProduct<T, Adjacent::K, AB, SHAPE, DMA>;
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const int per = p.mtiles * p.ntiles;
@@ -720,12 +742,19 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
 #pragma unroll
         for (int n = 0; n < NF; ++n) acc[m][n] = Acc{0, 0, 0, 0};
     int64_t steps = ks > 0 ? (ks - 1) / (KW * A::kStep) + 1 : 0;
+    const int64_t last = ks - (steps - 1) * (KW * A::kStep);  // k of this wave's last step
+    const int rest = last < A::kStep ? (int)last : 0;
 #pragma unroll
     for (int i = 0; i < D; ++i) load(i);
     int stage = 0;
     for (; steps > 0; --steps) {
         constexpr int kLater = (D - 1) * (A::kChunks + B::kChunks);  // loads that were asked for behind this stage's
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLater) : "memory");
+        if (steps == 1 && rest % A::kChunk) {
+            da.clear(own + stage * kStage, rest, lane);
+            db.clear(own + stage * kStage + A::kBytes, rest, lane);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
         Frag<T> fa[2][R], fb[2][NF];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -887,9 +916,10 @@ __device__ inline RowRange grad_rows(const int32_t* offsets, int32_t rows, int s
     return {first, min(first + per, last)};
 }
 
-template <typename T, int MF, int WM, int WN, bool DMA>
-__global__ __launch_bounds__(WM* WN * 64) void weight_grad_kernel(WeightGrad p, Ending e) {
-    using P = TileProduct<T, Adjacent::L, Adjacent::L, MF, WM, WN, DMA>;
+template <typename T, typename SHAPE, bool DMA>
+__global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad p, Ending e) {
+    using P = TileProduct<T, Adjacent::L, Adjacent::L, SHAPE, DMA>;
+    constexpr int MF = P::MF, NF = P::NF, WN = P::WN;
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const int per = p.mtiles * p.ntiles;
@@ -918,9 +948,9 @@ __global__ __launch_bounds__(WM* WN * 64) void weight_grad_kernel(WeightGrad p, 
         run(std::integral_constant<int, P::OF_B>{});
         if (wm == 0 && lane % 16 == 0)
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
+            for (int n = 0; n < NF; ++n)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) put(n0 + wn * 64 + n * 16 + lane / 4 + q, p.n, product.sums[n][q]);
+                for (int q = 0; q < 4; ++q) put(n0 + (wn * NF + n) * 16 + lane / 4 + q, p.n, product.sums[n][q]);
     } else if (p.dbias && p.d_is_a && tile.n == 0) {
         run(std::integral_constant<int, P::OF_A>{});
         if (wn == 0 && lane < 16)
