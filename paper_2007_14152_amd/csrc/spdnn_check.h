@@ -16,7 +16,7 @@
 namespace spdnn {
 
 constexpr size_t kAlign = 256;
-constexpr int32_t kMostWidth = 1 << 30;   // columns: a vector beyond a row's end must not pass 32 bits
+constexpr int32_t kMostWidth = 1 << 30;  // columns: a vector beyond a row's end must not pass 32 bits
 
 inline int size_of(int32_t type) { return type == SPDNN_F32 ? 4 : type == SPDNN_BF16 || type == SPDNN_F16 ? 2 : 0; }
 
@@ -55,6 +55,12 @@ inline void with_type(int32_t type, F f) {
     else if (type == SPDNN_BF16) f(__bf16{});
     else f(_Float16{});
 }
+
+// Outputs of this many bytes go past the caches, for whoever reads them next does not find them there (256 MB at the most) anyway,
+// and so do inputs that are read once.  Rows of 4096 bf16 by id, alone and with a kernel behind that reads them, through -> past:
+// 400 MB 128 -> 117 and 266 -> 256 us, 200 MB 70 -> 62 and 141 -> 137, 128 MB 42 -> 41 and 83 -> 87, 16 MB 10.4 -> 11.8 and
+// 15.9 -> 17.5.  combine of 4 such rows each, its input through -> past: 512 MB 128 -> 112 us, 256 MB 64 -> 60, 128 MB 28.5 -> 35.6.
+constexpr int64_t kPastBytes = 160 << 20;
 
 inline int launched() {
     HIP_TRY(hipGetLastError());

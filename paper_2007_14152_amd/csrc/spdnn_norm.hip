@@ -29,10 +29,10 @@ bool with_row(int32_t width, F f) {
 #define SPDNN_ROW(U, G, THREADS) f(std::integral_constant<int, U>{}, std::integral_constant<int, G>{}, std::integral_constant<int, THREADS>{})
     if (vecs <= 64) SPDNN_ROW(1, 64, 256);
     else if (vecs <= 128) SPDNN_ROW(2, 64, 256);
-    else if (vecs <= 256) SPDNN_ROW(4, 64, 256);
-    else if (vecs <= 512) SPDNN_ROW(8, 64, 256);
+    else if (vecs <= 256) SPDNN_ROW(1, 256, 256);
+    else if (vecs <= 512) SPDNN_ROW(2, 256, 256);
     else if (vecs <= 1024) SPDNN_ROW(4, 256, 256);
-    else if (vecs <= 2048) SPDNN_ROW(8, 256, 256);
+    else if (vecs <= 2048) SPDNN_ROW(2, 1024, 1024);
     else if (vecs <= 4096) SPDNN_ROW(4, 1024, 1024);
     else return false;
 #undef SPDNN_ROW
@@ -41,10 +41,15 @@ bool with_row(int32_t width, F f) {
 template <typename T, typename F>
 bool with_row_of(int32_t width, F f) {
     constexpr int V = 16 / sizeof(T);
-    if (width >= V) return with_row<V>(width, [&](auto u, auto g, auto threads) { f(std::integral_constant<int, V>{}, u, g, threads); });
-    return with_row<1>(width, [&](auto u, auto g, auto threads) { f(std::integral_constant<int, 1>{}, u, g, threads); });
+    if (width < V) return with_row<1>(width, [&](auto u, auto g, auto threads) { f(std::integral_constant<int, 1>{}, std::true_type{}, u, g, threads); });
+    return with_row<V>(width, [&](auto u, auto g, auto threads) {
+        if (width % V == 0) f(std::integral_constant<int, V>{}, std::true_type{}, u, g, threads);
+        else f(std::integral_constant<int, V>{}, std::false_type{}, u, g, threads);
+    });
 }
 
+// Threads that take rows in turn, a few to every lane of the chip.
+constexpr int64_t kNormThreads = 2048 * 256;
 // Workgroups that add columns: each leaves a part.
 constexpr int64_t kParts = 512;
 int64_t parts_of(int32_t rows) { return std::min<int64_t>(rows, kParts); }
@@ -67,15 +72,15 @@ int spdnn_layer_norm(const void* x, int32_t type, int32_t rows, int32_t width, i
     if (!(eps >= 0.0f)) return fail(SPDNN_EINVAL, "need eps >= 0");
     if (rows == 0) return SPDNN_OK;
     const hipStream_t s = (hipStream_t)hip_stream;
-    const Norm p{rows, width, weight, bias, param_type == SPDNN_F32, eps, (float2*)stats};
+    const Norm p{rows, width, weight, bias, param_type == SPDNN_F32, eps, (float2*)stats, (int64_t)rows * width * size_of(out_type) >= kPastBytes};
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
         const auto run = [&](auto to) {
             using O = decltype(to);
-            const bool held = with_row_of<T>(width, [&](auto v, auto u, auto g, auto threads) {
+            const bool held = with_row_of<T>(width, [&](auto v, auto whole, auto u, auto g, auto threads) {
                 constexpr int G = decltype(g)::value, THREADS = decltype(threads)::value;
-                const int64_t groups = std::min<int64_t>((rows - 1) / (THREADS / G) + 1, kMostGroups);
-                layer_norm_kernel<T, O, decltype(v)::value, decltype(u)::value, G, THREADS><<<dim3((unsigned)groups), THREADS, 0, s>>>(p, (const T*)x, x_stride, (O*)out, out_stride);
+                const int64_t groups = std::min<int64_t>((rows - 1) / (THREADS / G) + 1, kNormThreads / THREADS);
+                layer_norm_kernel<T, O, decltype(v)::value, decltype(whole)::value, decltype(u)::value, G, THREADS><<<dim3((unsigned)groups), THREADS, 0, s>>>(p, (const T*)x, x_stride, (O*)out, out_stride);
             });
             if (!held)
                 layer_norm_long_kernel<T, O><<<dim3((unsigned)std::min<int64_t>(rows, kMostGroups)), 1024, 0, s>>>(p, (const T*)x, x_stride, (O*)out, out_stride);
@@ -115,15 +120,15 @@ int spdnn_layer_norm_grad(const void* dout, int32_t type, int64_t dout_stride, c
     }
     const hipStream_t s = (hipStream_t)hip_stream;
     const int64_t most = parts_of(rows);
-    const NormGrad p{rows, width, (const float2*)stats, weight, param_type == SPDNN_F32, sums ? (float*)work : nullptr};
+    const NormGrad p{rows, width, (const float2*)stats, weight, param_type == SPDNN_F32, sums ? (float*)work : nullptr, (int64_t)rows * width * size_of(type) >= kPastBytes};
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
         int64_t parts = 0;
         if (rows > 0) {
-            const bool held = with_row_of<T>(width, [&](auto v, auto u, auto g, auto threads) {
+            const bool held = with_row_of<T>(width, [&](auto v, auto whole, auto u, auto g, auto threads) {
                 constexpr int G = decltype(g)::value, THREADS = decltype(threads)::value;
                 parts = std::min<int64_t>((rows - 1) / (THREADS / G) + 1, most);
-                layer_norm_grad_kernel<T, decltype(v)::value, decltype(u)::value, G, THREADS><<<dim3((unsigned)parts), THREADS, 0, s>>>(p, (const T*)dout, dout_stride, (const T*)x, x_stride, (const T*)add, add_stride, (T*)dx, dx_stride);
+                layer_norm_grad_kernel<T, decltype(v)::value, decltype(whole)::value, decltype(u)::value, G, THREADS><<<dim3((unsigned)parts), THREADS, 0, s>>>(p, (const T*)dout, dout_stride, (const T*)x, x_stride, (const T*)add, add_stride, (T*)dx, dx_stride);
             });
             if (!held) {
                 layer_norm_grad_long_kernel<T><<<dim3((unsigned)std::min<int64_t>(rows, kMostGroups)), 1024, 0, s>>>(p, (const T*)dout, dout_stride, (const T*)x, x_stride, (const T*)add, add_stride, (T*)dx, dx_stride);

@@ -64,31 +64,52 @@ struct Norm {
     bool param_f32;
     float eps;
     float2* stats;
+    bool past;  // stores that leave nothing in the caches
 };
 
 // out[t] = (x[t] - mean) * rstd * weight + bias.  A team of G lanes (a wave, or the workgroup) has a row, U vectors a lane, in
-// registers: it is read once, and the variance is that of the differences from the mean, which does not cancel.
-template <typename T, typename O, int V, int U, int G, int THREADS>
+// registers: it is read once, and the variance is that of the differences from the mean, which does not cancel.  (WHOLE: V divides the
+// width, and no vector has numbers of the one before it.)  A team takes rows in turn, with the next row under way and the parameters in registers.
+template <typename T, typename O, int V, bool WHOLE, int U, int G, int THREADS>
 __global__ __launch_bounds__(THREADS) void layer_norm_kernel(Norm p, const T* __restrict__ x, int64_t x_stride, O* __restrict__ out, int64_t out_stride) {
     __shared__ float lds[G > 64 ? 2 * (G / 64) : 1];
+    constexpr int TEAMS = THREADS / G;
     const int lane = threadIdx.x % G;
     const int vecs = (p.width - 1) / V + 1;
     const float inv = 1.0f / (float)p.width;
-    constexpr int TEAMS = THREADS / G;
-    for (int64_t row0 = (int64_t)blockIdx.x * TEAMS; row0 < p.rows; row0 += (int64_t)gridDim.x * TEAMS) {
-        const int64_t row = row0 + threadIdx.x / G;
-        if (G == 64 && row >= p.rows) break;
-        Pack<T, V> v[U];
+    int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / G;
+    if (row >= p.rows) return;  // of a whole team
+    const auto load = [&](int64_t r, Pack<T, V>(&v)[U]) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (u * G + lane < vecs) v[u] = load_vec<V>(x + row * x_stride + NormAt<V>(u * G + lane, p.width).col);
+            if (u * G + lane < vecs) v[u] = load_vec<V>(x + r * x_stride + NormAt<V>(u * G + lane, p.width).col);
+    };
+    Pack<T, V> v[U], next[U];
+    load(row, v);
+    float w[U][V], b[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[u][i] = 1.0f;
+            b[u][i] = 0.0f;
+        }
+        if (u * G + lane < vecs) {
+            const int col = NormAt<V>(u * G + lane, p.width).col;
+            if (p.weight) load_param<V>(p.weight, p.param_f32, (const T*)nullptr, col, w[u]);
+            if (p.bias) load_param<V>(p.bias, p.param_f32, (const T*)nullptr, col, b[u]);
+        }
+    }
+    while (true) {
+        const int64_t then = row + (int64_t)gridDim.x * TEAMS;
+        if (then < p.rows) load(then, next);
         float sum[1] = {0};
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u * G + lane < vecs) {
                 const int again = NormAt<V>(u * G + lane, p.width).again;
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[0] += i < again ? 0.0f : (float)v[u][i];
+                for (int i = 0; i < V; ++i) sum[0] += !WHOLE && i < again ? 0.0f : (float)v[u][i];
             }
         team_sums<G>(sum, lds);
         const float mean = sum[0] * inv;
@@ -100,7 +121,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_kernel(Norm p, const T* __
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float d = (float)v[u][i] - mean;
-                    square[0] += i < again ? 0.0f : d * d;
+                    square[0] += !WHOLE && i < again ? 0.0f : d * d;
                 }
             }
         team_sums<G>(square, lds);
@@ -109,22 +130,15 @@ __global__ __launch_bounds__(THREADS) void layer_norm_kernel(Norm p, const T* __
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u * G + lane < vecs) {
-                const int col = NormAt<V>(u * G + lane, p.width).col;
-                float y[V], w[V];
+                float y[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) y[i] = ((float)v[u][i] - mean) * rstd;
-                if (p.weight) {
-                    load_param<V>(p.weight, p.param_f32, (const T*)nullptr, col, w);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) y[i] *= w[i];
-                }
-                if (p.bias) {
-                    load_param<V>(p.bias, p.param_f32, (const T*)nullptr, col, w);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) y[i] += w[i];
-                }
-                store_vec<V, O>(out + row * out_stride + col, rounded_vec<O, V>(y), false);
+                for (int i = 0; i < V; ++i) y[i] = ((float)v[u][i] - mean) * rstd * w[u][i] + b[u][i];
+                store_vec<V, O>(out + row * out_stride + NormAt<V>(u * G + lane, p.width).col, rounded_vec<O, V>(y), p.past);
             }
+        if (then >= p.rows) break;
+        row = then;
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = next[u];
     }
 }
 
@@ -163,12 +177,13 @@ struct NormGrad {
     const void* weight;
     bool param_f32;
     float* parts;  // [workgroup][dweight, dbias][width], or null
+    bool past;     // stores that leave nothing in the caches
 };
 
 // With h = (x - mean) * rstd and g = dout * weight: dx = rstd * (g - mean(g) - h * mean(g * h)) + add, and for a part of the rows
 // the sums of dout * h and of dout, column by column.  A team takes rows in turn and keeps its columns' sums in registers; the teams
 // of a workgroup are added in order through LDS.
-template <typename T, int V, int U, int G, int THREADS>
+template <typename T, int V, bool WHOLE, int U, int G, int THREADS>
 __global__ __launch_bounds__(THREADS) void layer_norm_grad_kernel(NormGrad p, const T* __restrict__ dout, int64_t dout_stride, const T* __restrict__ x,
                                                                   int64_t x_stride, const T* __restrict__ add, int64_t add_stride, T* __restrict__ dx,
                                                                   int64_t dx_stride) {
@@ -178,36 +193,48 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_kernel(NormGrad p, co
     const int lane = threadIdx.x % G, team = threadIdx.x / G;
     const int vecs = (p.width - 1) / V + 1;
     const float inv = 1.0f / (float)p.width;
-    float dw[U][V], db[U][V];
+    float w[U][V], dw[U][V], db[U][V];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) dw[u][i] = db[u][i] = 0.0f;
-    for (int64_t row0 = (int64_t)blockIdx.x * TEAMS; row0 < p.rows; row0 += (int64_t)gridDim.x * TEAMS) {
-        const int64_t row = row0 + team;
-        if (G == 64 && row >= p.rows) break;
-        Pack<T, V> vx[U], vd[U];
+        for (int i = 0; i < V; ++i) {
+            w[u][i] = 1.0f;
+            dw[u][i] = db[u][i] = 0.0f;
+        }
+        if (p.weight && u * G + lane < vecs) load_param<V>(p.weight, p.param_f32, (const T*)nullptr, NormAt<V>(u * G + lane, p.width).col, w[u]);
+    }
+    struct Row {
+        Pack<T, V> x[U], d[U], add[U];
+        float2 st;
+    };
+    const auto load = [&](int64_t r, Row& to) {
+        to.st = p.stats[r];
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u * G + lane < vecs) {
                 const int col = NormAt<V>(u * G + lane, p.width).col;
-                vx[u] = load_vec<V>(x + row * x_stride + col);
-                vd[u] = load_vec<V>(dout + row * dout_stride + col);
+                to.x[u] = load_vec<V>(x + r * x_stride + col);
+                to.d[u] = load_vec<V>(dout + r * dout_stride + col);
+                if (add) to.add[u] = load_vec<V>(add + r * add_stride + col);
             }
-        const float2 st = p.stats[row];
+    };
+    int64_t row = (int64_t)blockIdx.x * TEAMS + team;
+    Row now, next;
+    if (row < p.rows) load(row, now);
+    while (row < p.rows) {
+        const int64_t then = row + (int64_t)gridDim.x * TEAMS;
+        if (then < p.rows) load(then, next);
         float sums[2] = {0, 0};
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u * G + lane < vecs) {
-                const NormAt<V> at(u * G + lane, p.width);
-                float w[V];
-                if (p.weight) load_param<V>(p.weight, p.param_f32, (const T*)nullptr, at.col, w);
+                const int again = NormAt<V>(u * G + lane, p.width).again;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float h = ((float)vx[u][i] - st.x) * st.y, d = (float)vd[u][i];
-                    const float g = p.weight ? d * w[i] : d;
-                    sums[0] += i < at.again ? 0.0f : g;
-                    sums[1] += i < at.again ? 0.0f : g * h;
+                    const float h = ((float)now.x[u][i] - now.st.x) * now.st.y, d = (float)now.d[u][i];
+                    const float g = d * w[u][i];
+                    sums[0] += !WHOLE && i < again ? 0.0f : g;
+                    sums[1] += !WHOLE && i < again ? 0.0f : g * h;
                     dw[u][i] += d * h;
                     db[u][i] += d;
                 }
@@ -217,22 +244,17 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_kernel(NormGrad p, co
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u * G + lane < vecs) {
-                const NormAt<V> at(u * G + lane, p.width);
-                float w[V], y[V];
-                if (p.weight) load_param<V>(p.weight, p.param_f32, (const T*)nullptr, at.col, w);
+                float y[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float h = ((float)vx[u][i] - st.x) * st.y, d = (float)vd[u][i];
-                    const float g = p.weight ? d * w[i] : d;
-                    y[i] = st.y * (g - a - h * b);
+                    const float h = ((float)now.x[u][i] - now.st.x) * now.st.y;
+                    y[i] = now.st.y * ((float)now.d[u][i] * w[u][i] - a - h * b);
+                    if (add) y[i] += (float)now.add[u][i];
                 }
-                if (add) {
-                    const Pack<T, V> r = load_vec<V>(add + row * add_stride + at.col);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) y[i] += (float)r[i];
-                }
-                store_vec<V, T>(dx + row * dx_stride + at.col, rounded_vec<T, V>(y), false);
+                store_vec<V, T>(dx + row * dx_stride + NormAt<V>(u * G + lane, p.width).col, rounded_vec<T, V>(y), p.past);
             }
+        row = then;
+        now = next;
     }
     if (!p.parts) return;
     float* const own = p.parts + (int64_t)blockIdx.x * 2 * p.width;

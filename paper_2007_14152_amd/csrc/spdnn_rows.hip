@@ -33,12 +33,6 @@ int check_route(int32_t rows, int32_t experts, int32_t k, const float* bias, int
 }
 dim3 groups(int64_t n) { return dim3((unsigned)std::max<int64_t>(1, std::min(n, kMostGroups))); }
 
-// Outputs of this many bytes go past the caches, for whoever reads them next does not find them there (256 MB at the most) anyway,
-// and so do inputs that are read once.  Rows of 4096 bf16 by id, alone and with a kernel behind that reads them, through -> past:
-// 400 MB 128 -> 117 and 266 -> 256 us, 200 MB 70 -> 62 and 141 -> 137, 128 MB 42 -> 41 and 83 -> 87, 16 MB 10.4 -> 11.8 and
-// 15.9 -> 17.5.  combine of 4 such rows each, its input through -> past: 512 MB 128 -> 112 us, 256 MB 64 -> 60, 128 MB 28.5 -> 35.6.
-constexpr int64_t kPastBytes = 160 << 20;
-
 // Tiles of rows x width elements in vectors of v, `unroll` a lane at a time, out_bytes of output in all: as many rows to a tile as
 // fill its workgroup's turns best, but not so many that less than two workgroups per CU are left.
 constexpr int64_t kTilesAtLeast = 512;
