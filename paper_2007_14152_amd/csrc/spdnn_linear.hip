@@ -55,32 +55,33 @@ int check_output(const char* what, const void* p, int32_t out_type, int32_t type
 constexpr int64_t kGroupsWanted = 256;     // workgroups that the CUs ask for at least
 constexpr size_t kMostParts = 256 << 20;  // bytes that sums in parts may take
 
-// How long n tiles of b x b take, us for 4096 k, as measured for one to four workgroups on every CU (a CU holds four of 64, two of 128, one
-// of 256); what is left over of full rounds takes what its own number of workgroups does.
-double cost(int b, int64_t n, int32_t type) {
+// How long n tiles of b x b take with `k` k each, us.  A CU holds four workgroups with tiles of 64, two of 128, one of 256; `us` is a
+// round of one to four of them on every CU for 4096 k, `ends` what a round takes besides.  Measured with K = 64 to 4096; what is left over
+// of full rounds takes what its own number of workgroups does.  longest: k of the longest tile, which no order of the others hides.
+double cost(int b, int64_t n, double k, double longest, int32_t type) {
     struct Row {
         int per_cu;
-        double us[4];
+        double us[4], ends;
     };
-    static const Row k16[3] = {{4, {36, 39, 48, 56}}, {2, {57, 80}}, {1, {112}}};
-    static const Row k32[3] = {{4, {93, 149, 209, 269}}, {2, {275, 491}}, {1, {966}}};
+    static const Row k16[3] = {{4, {32, 35, 44, 52}, 3.5}, {2, {52, 73}, 7}, {1, {104}, 10}};
+    static const Row k32[3] = {{4, {93, 149, 209, 269}, 4}, {2, {275, 491}, 9}, {1, {966}, 18}};
     const Row& r = (type == SPDNN_F32 ? k32 : k16)[b == 64 ? 0 : b == 128 ? 1 : 2];
     const int64_t full = 256 * r.per_cu, rest = n % full;
-    return n / full * r.us[r.per_cu - 1] + (rest ? r.us[(rest - 1) / 256] : 0.0);
+    const double rounds = n / full * r.us[r.per_cu - 1] + (rest ? r.us[(rest - 1) / 256] : 0.0);
+    return std::max(rounds * k, r.us[r.per_cu - 1] * longest) / 4096 + r.ends * ceil_div(n, full);
 }
 // The tile and the number of parts of k with which `tiles(b)` tiles take least.  Parts are written and read once more, out_bytes a part,
-// which a join of 6 us does at 4 TB/s; a round of workgroups begins and ends in 3 us.  (777 x 1500 x 1021 floats: 110 us with tiles of 128,
-// 40 with tiles of 64.)
+// which a join of 6 us does at 4 TB/s.  uneven: how many times the k of all on average the longest tile may have.  (777 x 1500 x 1021 floats: 110 us
+// with tiles of 128, 40 with tiles of 64.  dW of 12 experts of 10007 rows in all, 1500 x 777 floats: 532 us with tiles of 128.)
 template <typename F>
-void choose(F tiles, int64_t steps, size_t out_bytes, int32_t type, bool dma, int* b, int64_t* splits) {
-    const double of_4096 = (double)steps * step_of(type) / 4096;
+void choose(F tiles, int64_t steps, double uneven, size_t out_bytes, int32_t type, bool dma, int* b, int64_t* splits) {
+    const double k = (double)steps * step_of(type);
     double best = 1e300;
     for (const int tile : {256, 128, 64}) {
         if (!dma && tile != 128) continue;
         for (int64_t s = 1; s <= 64; s *= 2) {
             if (s > 1 && (steps / s < 4 || s * out_bytes > kMostParts)) break;
-            const int64_t n = tiles(tile) * s;
-            const double us = cost(tile, n, type) * of_4096 / s + 3.0 * ceil_div(n, 256 * (256 / tile)) + (s > 1 ? 6.0 + 2.0 * s * out_bytes / 4e6 : 0.0);
+            const double us = cost(tile, tiles(tile) * s, k / s, uneven * k / s, type) + (s > 1 ? 6.0 + 2.0 * s * out_bytes / 4e6 : 0.0);
             if (us < best) {
                 best = us;
                 *b = tile;
@@ -107,7 +108,7 @@ Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t e
         p.bn = p.narrow ? 16 : 64;
         p.splits = std::max<int64_t>(1, std::min(kGroupsWanted / std::max<int64_t>(tiles(p.bm, p.bn), 1), steps / 32));
     } else {
-        choose([&](int b) { return tiles(b, b); }, steps, (size_t)rows * cols * sizeof(float), type, dma, &p.bm, &p.splits);
+        choose([&](int b) { return tiles(b, b); }, steps, 1.0, (size_t)rows * cols * sizeof(float), type, dma, &p.bm, &p.splits);
         p.bn = p.bm;
     }
     p.mtiles = grouped ? rows / p.bm + experts + 1 : ceil_div(rows, p.bm);
@@ -122,7 +123,7 @@ Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32_t type
     p.dma = dma;
     const auto tiles = [&](int b) { return ceil_div(m, b) * ceil_div(n, b) * experts; };
     const int64_t steps = std::max<int64_t>(1, ceil_div(ceil_div(rows, experts), step_of(type)));
-    choose(tiles, steps, (size_t)experts * m * n * sizeof(float), type, dma, &p.bm, &p.splits);
+    choose(tiles, steps, experts > 1 ? 3.0 : 1.0, (size_t)experts * m * n * sizeof(float), type, dma, &p.bm, &p.splits);
     p.bn = p.bm;
     p.mtiles = ceil_div(m, p.bm);
     p.ntiles = ceil_div(n, p.bn);

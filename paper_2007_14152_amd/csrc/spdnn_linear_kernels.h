@@ -419,6 +419,49 @@ __device__ inline RowTile row_tile(const int32_t* offsets, int experts, int32_t 
     return {set, first + (int64_t)tile * BM, last};
 }
 
+// The same without what is left over, for kernels whose workgroups are shared out to the XCDs: tiles without rows would make shares
+// uneven (48000 rows of 64 experts, 4096 x 4096 bf16: 1796 us with them, XX without).  f(expert, its first tile, its tiles) for 64 experts at a
+// time, one a lane; gives the number of tiles.
+template <int BM, typename F>
+__device__ inline int each_expert(const int32_t* offsets, int experts, int32_t rows, F f) {
+    const int lane = threadIdx.x % 64;
+    int before = 0;
+    for (int e0 = 0; e0 <= experts; e0 += 64) {
+        const int e = e0 + lane;
+        const int first = min(max(offsets[min(e, experts)], 0), rows);
+        const int last = e >= experts ? rows : min(max(offsets[e + 1], first), rows);
+        const int tiles = e > experts ? 0 : (last - first + BM - 1) / BM;
+        int upto = tiles;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) {
+            const int other = __shfl_up(upto, step);
+            if (lane >= step) upto += other;
+        }
+        f(e, before + upto - tiles, tiles);
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return before;
+}
+template <int BM>
+__device__ inline int row_tiles(const int32_t* offsets, int experts, int32_t rows, int mtiles) {
+    return offsets ? each_expert<BM>(offsets, experts, rows, [](int, int, int) {}) : mtiles;
+}
+template <int BM>
+__device__ inline RowTile full_row_tile(const int32_t* offsets, int experts, int32_t rows, int t) {
+    if (!offsets) return {0, (int64_t)t * BM, rows};
+    int set = experts, tile = 0;
+    each_expert<BM>(offsets, experts, rows, [&](int e, int first, int tiles) {
+        const uint64_t found = __ballot(t >= first && t < first + tiles);
+        if (!found) return;
+        const int lane = __ffsll((unsigned long long)found) - 1;
+        set = __builtin_amdgcn_readlane(e, lane);
+        tile = t - __builtin_amdgcn_readlane(first, lane);
+    });
+    const int first = min(max(offsets[set], 0), rows);
+    const int last = set == experts ? rows : min(max(offsets[set + 1], first), rows);
+    return {set, first + (int64_t)tile * BM, last};
+}
+
 // --- the product of a tile --------------------------------------------------
 //
 // A workgroup of WM x WN waves, each with MF x NF fragments: WM * MF * 16 lines of a, WN * NF * 16 lines of b.
@@ -499,7 +542,8 @@ struct TileProduct {
         }
     }
     // a, b: the first number of the tile's lines at the first k; alines, blines: lines there are; ks: k there are.
-    template <int OF>
+    // HALF: only the first half of a's lines is there, and the waves of the other half only load.
+    template <int OF, bool HALF = false>
     __device__ __forceinline__ void run(char* lds, const char* a, int64_t aline, int alines, const char* b, int64_t bline, int blines, int64_t ks) {
         const int thread = threadIdx.x, lane = thread % 64, wave = thread / 64, wm = wave / WN, wn = wave % WN;
 #pragma unroll
@@ -544,8 +588,10 @@ struct TileProduct {
             int at = 0;
             read_b(lds, 0, lane, wn, fb[0]);
             read_a(lds, 0, 0, lane, wm, fa[0]);
+            const bool idle = HALF && w / WN >= WM / 2;
             do {
                 const char* now = lds + at;
+                if (!idle) {
                 read_a(now, 0, 1, lane, wm, fa[1]);
                 multiply<0, OF>(fa[0], fb[0]);
                 interleave<kReadsA>();
@@ -556,6 +602,7 @@ struct TileProduct {
                 read_a(now, 1, 1, lane, wm, fa[1]);
                 multiply<0, OF>(fa[0], fb[1]);
                 interleave<kReadsA>();
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 loads_done();
                 __builtin_amdgcn_s_barrier();
@@ -564,10 +611,12 @@ struct TileProduct {
                 if (ks > 0) load(lds + at);
                 at = kStage - at;
                 now = lds + at;
+                if (!idle) {
                 read_b(now, 0, lane, wn, fb[0]);
                 read_a(now, 0, 0, lane, wm, fa[0]);
                 multiply<1, OF>(fa[1], fb[1]);
                 interleave<kReadsA + kReadsB>();
+                }
                 __builtin_amdgcn_sched_barrier(0);
             } while (--steps > 0);
             __syncthreads();
@@ -668,11 +717,13 @@ __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Endi
     using P = TileProduct<T, Adjacent::K, AB, SHAPE, DMA>;
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
-    const int per = p.mtiles * p.ntiles;
-    const int t = xcd_order(blockIdx.x, gridDim.x);
+    const int mtiles = row_tiles<BM>(p.offsets, p.experts, p.rows, p.mtiles);
+    const int per = mtiles * p.ntiles;
+    if ((int)blockIdx.x >= per * p.splits) return;
+    const int t = xcd_order(blockIdx.x, per * p.splits);
     const int split = t / per;
-    const TileAt tile = banded(t - split * per, p.mtiles, p.ntiles, 8);
-    const RowTile r = row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
+    const TileAt tile = banded(t - split * per, mtiles, p.ntiles, 8);
+    const RowTile r = full_row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
     if (r.first >= r.last) return;
     const int n0 = tile.n * BN;
     if (r.set == p.experts) {  // rows of no expert
@@ -688,7 +739,10 @@ __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Endi
     const char* const a = p.x.p + r.first * p.x.line + k0 * sizeof(T);
     const char* const b = p.w.p + r.set * p.w.set + (AB == Adjacent::K ? n0 * p.w.line + k0 * sizeof(T) : k0 * p.w.line + n0 * sizeof(T));
     P product;
-    product.template run<P::NO_SUMS>(lds, a, p.x.line, (int)min((int64_t)BM, r.last - r.first), b, p.w.line, min(BN, p.cols - n0), ks);
+    const int alines = (int)min((int64_t)BM, r.last - r.first), blines = min(BN, p.cols - n0);
+    // The last tile of an expert: half of it takes half the time (48000 rows of 64 experts, 4096 x 4096 bf16: 6 %).
+    if (DMA && SHAPE::kM == 256 && alines <= BM / 2) product.template run<P::NO_SUMS, true>(lds, a, p.x.line, alines, b, p.w.line, blines, ks);
+    else product.template run<P::NO_SUMS>(lds, a, p.x.line, alines, b, p.w.line, blines, ks);
     product.end(lds, e, r.set, r.first, min(r.last, r.first + BM), n0, p.splits > 1 ? p.parts + (int64_t)split * p.rows * p.cols : nullptr);
 }
 
@@ -916,6 +970,21 @@ __device__ inline RowRange grad_rows(const int32_t* offsets, int32_t rows, int s
     return {first, min(first + per, last)};
 }
 
+// The expert with the `rank`-th largest number of rows: long tiles that begin last would leave the chip to themselves (dW of 12 experts:
+// XX us in order of experts, YY so).  Up to 64 experts; more are many tiles anyway, and stay in order.
+__device__ inline int by_load(const int32_t* offsets, int experts, int rank) {
+    if (!offsets || experts > 64) return rank;
+    const int lane = threadIdx.x % 64, e = min(lane, experts - 1);
+    const int load = offsets[e + 1] - offsets[e];
+    int before = 0;
+    for (int j = 0; j < experts; ++j) {
+        const int other = __builtin_amdgcn_readlane(load, j);
+        before += other > load || (other == load && j < lane);
+    }
+    const uint64_t found = __ballot(lane < experts && before == rank);
+    return found ? __ffsll((unsigned long long)found) - 1 : rank;
+}
+
 template <typename T, typename SHAPE, bool DMA>
 __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad p, Ending e) {
     using P = TileProduct<T, Adjacent::L, Adjacent::L, SHAPE, DMA>;
@@ -923,8 +992,10 @@ __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const int per = p.mtiles * p.ntiles;
-    const int t = xcd_order(blockIdx.x, gridDim.x);
-    const int set = t / per % p.experts, split = t / per / p.experts;
+    // An expert's tiles and parts at a time, each expert's shared out to the XCDs.
+    const int each = per * p.splits;
+    const int set = by_load(p.offsets, p.experts, blockIdx.x / each);
+    const int t = xcd_order(blockIdx.x % each, each), split = t / per;
     const TileAt tile = banded(t % per, p.mtiles, p.ntiles, 8);
     const RowRange r = grad_rows<P::A::kStep>(p.offsets, p.rows, set, split, p.splits);
     const int m0 = tile.m * BM, n0 = tile.n * BN;
