@@ -222,22 +222,36 @@ struct ByDma {
                 for (int i = ks % G::kChunk; i < G::kChunk; ++i)
                     reinterpret_cast<T*>(tile + line * 128 + (ks / G::kChunk ^ (line >> 1 & 7)) * 16)[i] = (T)0.0f;
     }
-    // lines, ks: what there is of both from p on.
-    __device__ void load(const char* p, char* tile, int lines, int64_t ks, int thread, int wave) const {
+    // Loads of one step, to be asked for one chunk of every lane after the other.  lines, ks: what there is of both from p on.
+    struct Step {
+        Memory memory;
+        uint32_t at[kBases], step;
+        char* tile;
+        __device__ __forceinline__ void load(int c) const {
+            load_to_lds(memory, at[c % kBases] + c / kBases * step, tile, c * (THREADS * 16));
+        }
+    };
+    __device__ __forceinline__ Step begin_step(const char* p, char* tile, int lines, int64_t ks, int thread, int wave) const {
         const int k = (int)min(ks, (int64_t)G::kStep);  // nothing is loaded if there is none
         const uint32_t bytes = k <= 0 ? 0 : ADJ == Adjacent::K ? (lines - 1) * line + k * (uint32_t)sizeof(T) : (k - 1) * line + lines * (uint32_t)sizeof(T);
         const uint64_t base = (uint64_t)p;
-        const Memory memory = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff),
-                               __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
-        uint32_t at[kBases];
+        Step s;
+        s.memory = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff),
+                    __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+        s.step = step;
+        s.tile = tile + wave * 1024;
 #pragma unroll
-        for (int c = 0; c < kBases; ++c) at[c] = from[c];
+        for (int c = 0; c < kBases; ++c) s.at[c] = from[c];
         if (ADJ == Adjacent::K && k < G::kStep)
 #pragma unroll
             for (int c = 0; c < kBases; ++c)
-                if (G::at(c * THREADS + thread).chunk * G::kChunk >= k) at[c] += kOutside;
+                if (G::at(c * THREADS + thread).chunk * G::kChunk >= k) s.at[c] += kOutside;
+        return s;
+    }
+    __device__ __forceinline__ void load(const char* p, char* tile, int lines, int64_t ks, int thread, int wave) const {
+        const Step s = begin_step(p, tile, lines, ks, thread, wave);
 #pragma unroll
-        for (int c = 0; c < G::kChunks; ++c) load_to_lds(memory, at[c % kBases] + c / kBases * step, tile + wave * 1024, c * (THREADS * 16));
+        for (int c = 0; c < G::kChunks; ++c) s.load(c);
     }
 };
 
@@ -514,6 +528,15 @@ struct TileProduct {
 #pragma unroll
         for (int m = 0; m < kPart; ++m) a[m] = A::read(stage, (wm * MF + part * kPart + m) * 16, half, lane);
     }
+    static constexpr int kLoads = A::kChunks + B::kChunks;  // of a step
+    template <int PART, int OF>
+    __device__ __forceinline__ void multiply_line(int m, const Frag<T>& a, const Frag<T> (&b)[NF]) {
+        Frag<T> ones;
+        for (int i = 0; i < A::kChunk; ++i) ones[i] = (T)1.0f;
+        if constexpr (OF == OF_A) sums[PART * kPart + m] = mma(ones, a, sums[PART * kPart + m]);
+#pragma unroll
+        for (int n = 0; n < NF; ++n) acc[PART * kPart + m][n] = mma(b[n], a, acc[PART * kPart + m][n]);
+    }
     template <int PART, int OF>
     __device__ __forceinline__ void multiply(const Frag<T> (&a)[kPart], const Frag<T> (&b)[NF]) {
         Frag<T> ones;
@@ -592,34 +615,50 @@ struct TileProduct {
             do {
                 const char* now = lds + at;
                 if (!idle) {
-                read_a(now, 0, 1, lane, wm, fa[1]);
-                multiply<0, OF>(fa[0], fb[0]);
-                interleave<kReadsA>();
-                read_b(now, 1, lane, wn, fb[1]);
-                read_a(now, 1, 0, lane, wm, fa[0]);
-                multiply<1, OF>(fa[1], fb[0]);
-                interleave<kReadsA + kReadsB>();
-                read_a(now, 1, 1, lane, wm, fa[1]);
-                multiply<0, OF>(fa[0], fb[1]);
-                interleave<kReadsA>();
+                    read_a(now, 0, 1, lane, wm, fa[1]);
+                    multiply<0, OF>(fa[0], fb[0]);
+                    interleave<kReadsA>();
+                    read_b(now, 1, lane, wn, fb[1]);
+                    read_a(now, 1, 0, lane, wm, fa[0]);
+                    multiply<1, OF>(fa[1], fb[0]);
+                    interleave<kReadsA + kReadsB>();
+                    read_a(now, 1, 1, lane, wm, fa[1]);
+                    multiply<0, OF>(fa[0], fb[1]);
+                    interleave<kReadsA>();
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 loads_done();
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
                 if (rest % A::kChunk && steps == 2) clear(lds + kStage - at);
-                if (ks > 0) load(lds + at);
+                // (Behind the last step too, of nothing.)  Asked for one by one between products: eight at a time hold up a wave for longer
+                // than its products take (24000 x 4096 x 4096 bf16 627 us, so 612).
+                const auto sa = da.begin_step(a, lds + at, alines, ks, thread, w);
+                const auto sb = db.begin_step(b, lds + at + A::kBytes, blines, ks, thread, w);
+                ks -= A::kStep;
+                a += astep;
+                b += bstep;
                 at = kStage - at;
                 now = lds + at;
-                if (!idle) {
-                read_b(now, 0, lane, wn, fb[0]);
-                read_a(now, 0, 0, lane, wm, fa[0]);
-                multiply<1, OF>(fa[1], fb[1]);
-                interleave<kReadsA + kReadsB>();
-                }
                 __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int m = 0; m < kPart; ++m) {
+                    if (!idle) {
+#pragma unroll
+                        for (int n = m * NF / kPart; n < (m + 1) * NF / kPart; ++n) fb[0][n] = B::read(now + A::kBytes, (wn * NF + n) * 16, 0, lane);
+                        fa[0][m] = A::read(now, (wm * MF + m) * 16, 0, lane);
+                        multiply_line<1, OF>(m, fa[1][m], fb[1]);
+                    }
+#pragma unroll
+                    for (int c = m * kLoads / kPart; c < (m + 1) * kLoads / kPart; ++c) {
+                        if (c < A::kChunks) sa.load(c);
+                        else sb.load(c - A::kChunks);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             } while (--steps > 0);
-            __syncthreads();
+            loads_done();  // the loads of nothing store zeros
+            __builtin_amdgcn_s_barrier();
             return;
         }
         ByRegisters<T, AA, S::kM, S::kThreads> ra;
