@@ -693,7 +693,7 @@ struct TileProduct {
     }
     // Ends the tile by way of LDS: rows of NF * 16 sums of a wave's own, chunk c of row r at place c ^ r (its last bits).  first, last: out's rows; n0: the
     // first column; parts: where sums go that are not all there yet (rows of out's), or null.  What add has is asked for kAhead rows a
-    // lane at a time: with one workgroup on a CU nothing else hides it.
+    // lane at a time, before the rows ahead of them are ended: with one workgroup on a CU nothing else hides it.
     __device__ __forceinline__ void end(char* lds, const Ending& e, int set, int64_t first, int64_t last, int n0, float* parts) {
         constexpr int kTurn = MF < 4 ? MF : 4, kLanes = NF * 2, kRows = 64 / kLanes, kAhead = kTurn * 16 / kRows < 4 ? kTurn * 16 / kRows : 4;
         constexpr int kLine = NF * 64, kMask = NF * 4 - 1;
@@ -702,6 +702,14 @@ struct TileProduct {
         const int c = lane % kLanes * 2, col = n0 + wn * (NF * 16) + c * 4;
         Biases<T> bias;
         if (!parts) bias.load(e, set, col);
+        Added<T> added[kAhead], then[kAhead];
+        const auto fetch = [&](int line, Added<T>(&to)[kAhead]) __attribute__((always_inline)) {
+            const int64_t row0 = first + wm * MF * 16 + line + lane / kLanes;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (!parts && row0 + i * kRows < last) to[i].load(e, row0 + i * kRows, col);
+        };
+        fetch(0, added);
 #pragma unroll
         for (int m0 = 0; m0 < MF; m0 += kTurn) {
 #pragma unroll
@@ -713,10 +721,7 @@ struct TileProduct {
 #pragma unroll 1
             for (int r0 = 0; r0 < kTurn * 16; r0 += kRows * kAhead) {
                 const int64_t row0 = first + (wm * MF + m0) * 16 + r0 + lane / kLanes;
-                Added<T> added[kAhead];
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i)
-                    if (!parts && row0 + i * kRows < last) added[i].load(e, row0 + i * kRows, col);
+                if (m0 * 16 + r0 + kRows * kAhead < MF * 16) fetch(m0 * 16 + r0 + kRows * kAhead, then);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     const int r = r0 + i * kRows + lane / kLanes;
@@ -735,6 +740,8 @@ struct TileProduct {
                         end_sums<T>(e, set, row, col, sum, bias, added[i], [&](int j) { return *reinterpret_cast<const float*>(at + ((c + j / 4) ^ (r & kMask)) * 16 + j % 4 * 4); });
                     }
                 }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) added[i] = then[i];
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
