@@ -1033,7 +1033,7 @@ __device__ inline RowRange grad_rows(const int32_t* offsets, int32_t rows, int s
 __device__ inline int by_load(const int32_t* offsets, int experts, int rank) {
     if (!offsets || experts > 64) return rank;
     const int lane = threadIdx.x % 64, e = min(lane, experts - 1);
-    const int load = offsets[e + 1] - offsets[e];
+    const int load = max(offsets[e + 1], 0) - max(offsets[e], 0);
     int before = 0;
     for (int j = 0; j < experts; ++j) {
         const int other = __builtin_amdgcn_readlane(load, j);
