@@ -68,10 +68,11 @@ double cost(int b, int64_t n, double k, double longest, int32_t type) {
     const Row& r = (type == SPDNN_F32 ? k32 : k16)[b == 64 ? 0 : b == 128 ? 1 : 2];
     const int64_t full = 256 * r.per_cu, rest = n % full;
     const double rounds = n / full * r.us[r.per_cu - 1] + (rest ? r.us[(rest - 1) / 256] : 0.0);
-    return std::max(rounds * k, r.us[r.per_cu - 1] * longest) / 4096 + r.ends * ceil_div(n, full);
+    const int64_t beside = std::min<int64_t>(r.per_cu, ceil_div(std::max<int64_t>(n, 1), 256));
+    return std::max(rounds * k, r.us[beside - 1] * longest) / 4096 + r.ends * ceil_div(n, full);
 }
 // The tile and the number of parts of k with which `tiles(b)` tiles take least.  Parts are written and read once more, out_bytes a part,
-// which a join of 6 us does at 4 TB/s.  uneven: how many times the k of all on average the longest tile may have.  (777 x 1500 x 1021 floats: 110 us
+// which a join does in 9 us and at 4 TB/s.  uneven: how many times the k of all on average the longest tile may have.  (777 x 1500 x 1021 floats: 110 us
 // with tiles of 128, 40 with tiles of 64.  dW of 12 experts of 10007 rows in all, 1500 x 777 floats: 532 us with tiles of 128.)
 template <typename F>
 void choose(F tiles, int64_t steps, double uneven, size_t out_bytes, int32_t type, bool dma, int* b, int64_t* splits) {
@@ -81,7 +82,7 @@ void choose(F tiles, int64_t steps, double uneven, size_t out_bytes, int32_t typ
         if (!dma && tile != 128) continue;
         for (int64_t s = 1; s <= 64; s *= 2) {
             if (s > 1 && (steps / s < 4 || s * out_bytes > kMostParts)) break;
-            const double us = cost(tile, tiles(tile) * s, k / s, uneven * k / s, type) + (s > 1 ? 6.0 + 2.0 * s * out_bytes / 4e6 : 0.0);
+            const double us = cost(tile, tiles(tile) * s, k / s, uneven * k / s, type) + (s > 1 ? 9.0 + 2.0 * s * out_bytes / 4e6 : 0.0);
             if (us < best) {
                 best = us;
                 *b = tile;

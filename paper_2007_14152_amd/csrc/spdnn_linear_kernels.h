@@ -444,7 +444,7 @@ __device__ inline RowTile row_tile(const int32_t* offsets, int experts, int32_t 
 }
 
 // The same without what is left over, for kernels whose workgroups are shared out to the XCDs: tiles without rows would make shares
-// uneven (48000 rows of 64 experts, 4096 x 4096 bf16: 1796 us with them, XX without).  f(expert, its first tile, its tiles) for 64 experts at a
+// uneven (48000 rows of 64 experts, 4096 x 4096 bf16: 1796 us with them, 1734 without).  f(expert, its first tile, its tiles) for 64 experts at a
 // time, one a lane; gives the number of tiles.
 template <int BM, typename F>
 __device__ inline int each_expert(const int32_t* offsets, int experts, int32_t rows, F f) {
@@ -1029,7 +1029,7 @@ __device__ inline RowRange grad_rows(const int32_t* offsets, int32_t rows, int s
 }
 
 // The expert with the `rank`-th largest number of rows: long tiles that begin last would leave the chip to themselves (dW of 12 experts:
-// XX us in order of experts, YY so).  Up to 64 experts; more are many tiles anyway, and stay in order.
+// 10007 x 1500 x 777 floats, dx and dW 437 us in order of experts, 422 so).  Up to 64 experts; more are many tiles anyway, and stay in order.
 __device__ inline int by_load(const int32_t* offsets, int experts, int rank) {
     if (!offsets || experts > 64) return rank;
     const int lane = threadIdx.x % 64, e = min(lane, experts - 1);
