@@ -63,7 +63,7 @@ double cost(int b, int64_t n, double k, double longest, int32_t type) {
         int per_cu;
         double us[4], ends;
     };
-    static const Row k16[3] = {{4, {32, 35, 44, 52}, 3.5}, {2, {52, 73}, 7}, {1, {104}, 10}};
+    static const Row k16[3] = {{4, {26, 35, 44, 52}, 3.5}, {2, {49, 73}, 7}, {1, {104}, 10}};
     static const Row k32[3] = {{4, {93, 149, 209, 269}, 4}, {2, {275, 491}, 9}, {1, {966}, 18}};
     const Row& r = (type == SPDNN_F32 ? k32 : k16)[b == 64 ? 0 : b == 128 ? 1 : 2];
     const int64_t full = 256 * r.per_cu, rest = n % full;
@@ -117,6 +117,7 @@ Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t e
     p.per_split = ceil_div(steps, p.splits) * step_of(type);
     p.splits = ceil_div(k, p.per_split);
     p.parts = p.splits > 1 ? aligned((size_t)p.splits * rows * cols * sizeof(float)) : 0;
+    p.alone = type != SPDNN_F32 && tiles(p.bm, p.bn) * p.splits <= kGroupsWanted;
     return p;
 }
 Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32_t type, bool dma) {
@@ -129,6 +130,7 @@ Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32_t type
     p.mtiles = ceil_div(m, p.bm);
     p.ntiles = ceil_div(n, p.bn);
     p.parts = p.splits > 1 ? aligned((size_t)p.splits * experts * m * n * sizeof(float)) : 0;
+    p.alone = type != SPDNN_F32 && tiles(p.bm) * p.splits <= kGroupsWanted;
     return p;
 }
 int check_tiles(const Plan& p, int32_t sets) {

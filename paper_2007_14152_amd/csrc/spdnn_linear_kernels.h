@@ -489,16 +489,21 @@ __device__ inline RowTile full_row_tile(const int32_t* offsets, int experts, int
 // --- the product of a tile --------------------------------------------------
 //
 // A workgroup of WM x WN waves, each with MF x NF fragments: WM * MF * 16 lines of a, WN * NF * 16 lines of b.
-template <int MF, int NF, int WM, int WN>
+// With operands that go straight to LDS, STAGES steps of k are there or under way.
+template <int MF, int NF, int WM, int WN, int STAGES>
 struct Shape {
-    static constexpr int kMF = MF, kNF = NF, kWM = WM, kWN = WN;
+    static constexpr int kMF = MF, kNF = NF, kWM = WM, kWN = WN, kStages = STAGES;
     static constexpr int kThreads = WM * WN * 64;
     static constexpr int kM = WM * MF * 16;
     static constexpr int kN = WN * NF * 16;
 };
-using Large = Shape<8, 4, 2, 4>;   // 256 x 256
-using Middle = Shape<4, 4, 2, 2>;  // 128 x 128
-using Small = Shape<2, 2, 2, 2>;   // 64 x 64
+using Large = Shape<8, 4, 2, 4, 2>;  // 256 x 256
+// 128 x 128 and 64 x 64; where a CU has no second workgroup, with a stage more, as nothing else covers the loads' way (4096 k of
+// bf16, 256 tiles: 60.7 and 54.1 us, 39.6 and 29.8; with 512 tiles 80 and 115, 40 and 37, and with 1024 57 and 68).
+template <int STAGES>
+using Middle = Shape<4, 4, 2, 2, STAGES>;
+template <int STAGES>
+using Small = Shape<2, 2, 2, 2, STAGES>;
 
 template <typename T, Adjacent AA, Adjacent AB, typename SHAPE, bool DMA>
 struct TileProduct {
@@ -508,7 +513,8 @@ struct TileProduct {
     using B = Tile<T, AB, S::kN, S::kThreads>;
     static constexpr int kStage = A::kBytes + B::kBytes;
     static constexpr int kEndBytes = WM * WN * (MF < 4 ? MF : 4) * 16 * NF * 64;
-    static constexpr int kLds = 2 * kStage > kEndBytes ? 2 * kStage : kEndBytes;
+    static constexpr int kStages = DMA ? S::kStages : 2;
+    static constexpr int kLds = kStages * kStage > kEndBytes ? kStages * kStage : kEndBytes;
 
     Acc acc[MF][NF];
     Acc sums[MF > NF ? MF : NF];  // over k of the lines of b (OF_B) or of a (OF_A): products with ones, beside the others
@@ -610,20 +616,29 @@ struct TileProduct {
             const auto clear = [&](char* stage) __attribute__((noinline)) {
                 ByDma<T, AA, S::kM, S::kThreads>::clear(stage, rest, threadIdx.x);
                 ByDma<T, AB, S::kN, S::kThreads>::clear(stage + A::kBytes, rest, threadIdx.x);
-                loads_done();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
             };
-            load(lds);
-            loads_done();
+#pragma unroll
+            for (int i = 0; i < kStages; ++i) load(lds + i * kStage);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * kLoads) : "memory");
             __builtin_amdgcn_s_barrier();
             if (rest % A::kChunk && steps == 1) clear(lds);
-            if (ks > 0) load(lds + kStage);
             int at = 0;
             read_b(lds, 0, lane, wn, fb[0]);
             read_a(lds, 0, 0, lane, wm, fa[0]);
             const bool idle = HALF && w / WN >= WM / 2;
             do {
                 const char* now = lds + at;
+                const int then = at == (kStages - 1) * kStage ? 0 : at + kStage;
+                // What the next loads need, worked out beside products.  (Behind the last step too, of nothing.)  They are asked for one by
+                // one between products: eight at a time hold up a wave for longer than its products take (24000 x 4096 x 4096 bf16 627
+                // us, so 609).
+                const auto sa = da.begin_step(a, lds + at, alines, ks, thread, w);
+                const auto sb = db.begin_step(b, lds + at + A::kBytes, blines, ks, thread, w);
+                ks -= A::kStep;
+                a += astep;
+                b += bstep;
                 if (!idle) {
                     read_a(now, 0, 1, lane, wm, fa[1]);
                     multiply<0, OF>(fa[0], fb[0]);
@@ -637,18 +652,12 @@ struct TileProduct {
                     interleave<kReadsA>();
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                loads_done();
+                // the next stage is there, for all waves; this one is free, all of it being in registers
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
-                if (rest % A::kChunk && steps == 2) clear(lds + kStage - at);
-                // (Behind the last step too, of nothing.)  Asked for one by one between products: eight at a time hold up a wave for longer
-                // than its products take (24000 x 4096 x 4096 bf16 627 us, so 612).
-                const auto sa = da.begin_step(a, lds + at, alines, ks, thread, w);
-                const auto sb = db.begin_step(b, lds + at + A::kBytes, blines, ks, thread, w);
-                ks -= A::kStep;
-                a += astep;
-                b += bstep;
-                at = kStage - at;
+                if (rest % A::kChunk && steps == 2) clear(lds + then);
+                at = then;
                 now = lds + at;
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll

@@ -15,6 +15,7 @@ struct Plan {
     int few;       // linear_short_kernel: fragments of rows in a tile (1, 2 or 4); 0: linear_kernel
     bool narrow;   // and whether its tiles have 16 columns instead of 64
     int bm, bn;
+    bool alone;    // no CU has two workgroups
     int64_t mtiles, ntiles, splits, per_split;
     size_t parts;  // bytes
 };

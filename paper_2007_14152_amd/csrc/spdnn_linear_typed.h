@@ -20,9 +20,11 @@ void launch_stored(const Plan& c, const Product& p, const Ending& e, hipStream_t
     else if (c.few == 2) launch_few<T, ADJ, 2>(c, grid, p, e, s);
     else if (c.few == 4) launch_few<T, ADJ, 4>(c, grid, p, e, s);
     else if (c.bm == 256) linear_kernel<T, ADJ, Large, true><<<grid, 512, 0, s>>>(p, e);
-    else if (c.bm == 64) linear_kernel<T, ADJ, Small, true><<<grid, 256, 0, s>>>(p, e);
-    else if (c.dma) linear_kernel<T, ADJ, Middle, true><<<grid, 256, 0, s>>>(p, e);
-    else linear_kernel<T, ADJ, Middle, false><<<grid, 256, 0, s>>>(p, e);
+    else if (c.bm == 64 && c.alone) linear_kernel<T, ADJ, Small<3>, true><<<grid, 256, 0, s>>>(p, e);
+    else if (c.bm == 64) linear_kernel<T, ADJ, Small<2>, true><<<grid, 256, 0, s>>>(p, e);
+    else if (c.dma && c.alone) linear_kernel<T, ADJ, Middle<3>, true><<<grid, 256, 0, s>>>(p, e);
+    else if (c.dma) linear_kernel<T, ADJ, Middle<2>, true><<<grid, 256, 0, s>>>(p, e);
+    else linear_kernel<T, ADJ, Middle<2>, false><<<grid, 256, 0, s>>>(p, e);
 }
 template <typename T>
 void launch_product(const Plan& c, Adjacent adj, const Product& p, const Ending& e, hipStream_t s) {
@@ -45,9 +47,11 @@ template <typename T>
 void launch_weight_grad(const Plan& c, const WeightGrad& p, const Ending& e, hipStream_t s) {
     const dim3 grid((unsigned)(c.mtiles * c.ntiles * p.experts * c.splits));
     if (c.bm == 256) weight_grad_kernel<T, Large, true><<<grid, 512, 0, s>>>(p, e);
-    else if (c.bm == 64) weight_grad_kernel<T, Small, true><<<grid, 256, 0, s>>>(p, e);
-    else if (c.dma) weight_grad_kernel<T, Middle, true><<<grid, 256, 0, s>>>(p, e);
-    else weight_grad_kernel<T, Middle, false><<<grid, 256, 0, s>>>(p, e);
+    else if (c.bm == 64 && c.alone) weight_grad_kernel<T, Small<3>, true><<<grid, 256, 0, s>>>(p, e);
+    else if (c.bm == 64) weight_grad_kernel<T, Small<2>, true><<<grid, 256, 0, s>>>(p, e);
+    else if (c.dma && c.alone) weight_grad_kernel<T, Middle<3>, true><<<grid, 256, 0, s>>>(p, e);
+    else if (c.dma) weight_grad_kernel<T, Middle<2>, true><<<grid, 256, 0, s>>>(p, e);
+    else weight_grad_kernel<T, Middle<2>, false><<<grid, 256, 0, s>>>(p, e);
     if (c.splits > 1) {
         weight_grad_join_kernel<T><<<loop_groups((int64_t)p.experts * p.m * ((p.n - 1) / kEnd + 1)), 256, 0, s>>>(p, e);
         const int64_t n = (int64_t)p.experts * (p.d_is_a ? p.m : p.n);
