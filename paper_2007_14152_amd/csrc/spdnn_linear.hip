@@ -149,11 +149,9 @@ int most_parts(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t expe
     return SPDNN_OK;
 }
 
-// Whether an operand can go straight to LDS: rows of whole words of 4 bytes, tiles within reach of 32-bit offsets, and rows of k that do
-// not overlap.
+// Whether an operand can go straight to LDS: tiles within reach of 32-bit offsets, and rows of k that do not overlap.
 bool dma_side(const Side& s, Adjacent adj, int32_t along, int32_t type) {
-    const int size = size_of(type);
-    return (int64_t)along * size % 4 == 0 && s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size);
+    return s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size_of(type));
 }
 
 void run_product(int32_t type, Adjacent adj, Product p, Ending e, hipStream_t s) {

@@ -180,8 +180,9 @@ struct ByRegisters {
 
 // Loads of a tile straight into LDS, 16 bytes a lane.  What is not there comes as zeros, from the range check of the buffer: lines
 // beyond the last, and what lies behind the last k (Adjacent::K: a lane whose chunk does has kOutside added to its offset; of a chunk
-// that is there in part, clear() clears the rest).  Addresses may have any alignment; memory rows have whole words of 4 bytes, which is
-// what the range check goes by, a tile's lines lie within kDmaSpan bytes, and the k rows of Adjacent::L do not overlap.
+// that is there in part, clear() clears the rest).  Addresses may have any alignment; a tile's lines lie within kDmaSpan bytes, and the k
+// rows of Adjacent::L do not overlap.  The range check goes by words of 4 bytes.  Where the last memory row of a tile ends within one, the
+// range takes in the two bytes behind it if the matrix goes on there (`follows`), and otherwise patch() stores the number that is missing.
 //
 // They are written as instructions: the compiler would let the transposing LDS reads wait for all loads of this kind that are under way,
 // for it cannot tell that they go to the other stage.  Whoever reads what they have stored waits with loads_done() and a barrier first.
@@ -214,7 +215,9 @@ struct ByDma {
     static_assert(G::kChunks % kBases == 0);
     uint32_t from[kBases];
     uint32_t line, step;
-    __device__ void begin(int64_t line_bytes, int thread) {
+    bool follows;
+    __device__ void begin(int64_t line_bytes, bool goes_on, int thread) {
+        follows = goes_on;
         line = (uint32_t)line_bytes;
         step = kRows * kBases * line;
 #pragma unroll
@@ -226,9 +229,20 @@ struct ByDma {
     // Clears what the last chunk of k has behind the last k: ks of a step that is not whole.  To be called between barriers.
     __device__ static void clear(char* tile, int ks, int thread) {
         if constexpr (ADJ == Adjacent::K)
+#pragma unroll 1
             for (int line = thread; line < LINES; line += THREADS)
+#pragma unroll 1
                 for (int i = ks % G::kChunk; i < G::kChunk; ++i)
                     reinterpret_cast<T*>(tile + line * 128 + (ks / G::kChunk ^ (line >> 1 & 7)) * 16)[i] = (T)0.0f;
+    }
+    // Whether the last number of the last memory row is missing in a last step of k, and the store of it.  p: as for begin_step.
+    __device__ __forceinline__ bool misses(int lines, int k) const { return sizeof(T) == 2 && !follows && ((ADJ == Adjacent::K ? k : lines) & 1); }
+    __device__ void patch(const char* p, char* tile, int lines, int k, int thread) const {
+        if (!misses(lines, k) || thread != 0) return;
+        const int row = ADJ == Adjacent::K ? lines - 1 : k - 1, col = ADJ == Adjacent::K ? k - 1 : lines - 1;  // of memory
+        constexpr int kRow = G::kPerRow * 16;
+        const int place = ADJ == Adjacent::K ? col / G::kChunk ^ (row >> 1 & 7) : col / G::kChunk ^ G::turn(row) * G::kBlock;
+        reinterpret_cast<T*>(tile + row * kRow + place * 16)[col % G::kChunk] = reinterpret_cast<const T*>(p + (int64_t)row * line)[col];
     }
     // Loads of one step, to be asked for one chunk of every lane after the other.  lines, ks: what there is of both from p on.
     struct Step {
@@ -242,7 +256,9 @@ struct ByDma {
     };
     __device__ __forceinline__ Step begin_step(const char* p, char* tile, int lines, int64_t ks, int thread, int wave) const {
         const int k = (int)min(ks, (int64_t)G::kStep);  // nothing is loaded if there is none
-        const uint32_t bytes = k <= 0 ? 0 : ADJ == Adjacent::K ? (lines - 1) * line + k * (uint32_t)sizeof(T) : (k - 1) * line + lines * (uint32_t)sizeof(T);
+        uint32_t bytes = k <= 0 ? 0 : ADJ == Adjacent::K ? (lines - 1) * line + k * (uint32_t)sizeof(T) : (k - 1) * line + lines * (uint32_t)sizeof(T);
+        if constexpr (sizeof(T) == 2)
+            if (k > 0 && (follows || (ADJ == Adjacent::L && ks > G::kStep))) bytes += (ADJ == Adjacent::K ? k & 1 : lines & 1) * 2;
         const uint64_t base = (uint64_t)p;
         Step s;
         s.memory = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff),
@@ -517,7 +533,10 @@ struct TileProduct {
     static constexpr int kLds = kStages * kStage > kEndBytes ? kStages * kStage : kEndBytes;
 
     Acc acc[MF][NF];
-    Acc sums[MF > NF ? MF : NF];  // over k of the lines of b (OF_B) or of a (OF_A): products with ones, beside the others
+    // Sums over k of the lines of b (OF_B) or of a (OF_A), products with ones beside the others: one accumulator a fragment, for lines that
+    // are not there may hold anything, which must not meet another line's sum, not even times zero.  a's fragments are shared out to the
+    // WN waves that have the same, one of a part each.
+    Acc sums[NF > 2 ? NF : 2];
 
     enum { NO_SUMS = 0, OF_A = 1, OF_B = 2 };
     template <int OF>
@@ -545,11 +564,20 @@ struct TileProduct {
         for (int m = 0; m < kPart; ++m) a[m] = A::read(stage, (wm * MF + part * kPart + m) * 16, half, lane);
     }
     static constexpr int kLoads = A::kChunks + B::kChunks;  // of a step
-    template <int PART, int OF>
-    __device__ __forceinline__ void multiply_line(int m, const Frag<T>& a, const Frag<T> (&b)[NF]) {
+    static_assert(kPart <= WN);
+    template <int PART>
+    __device__ __forceinline__ void sum_a(const Frag<T> (&a)[kPart]) {
+        const int wn = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % WN;
+        typedef int Bits __attribute__((ext_vector_type(4)));
         Frag<T> ones;
         for (int i = 0; i < A::kChunk; ++i) ones[i] = (T)1.0f;
-        if constexpr (OF == OF_A) sums[PART * kPart + m] = mma(ones, a, sums[PART * kPart + m]);
+        Bits own = __builtin_bit_cast(Bits, a[0]) & (wn == 0 ? -1 : 0);  // (a choice between fragments would put them into memory)
+#pragma unroll
+        for (int m = 1; m < kPart; ++m) own |= __builtin_bit_cast(Bits, a[m]) & (wn == m ? -1 : 0);
+        sums[PART] = mma(ones, __builtin_bit_cast(Frag<T>, own), sums[PART]);
+    }
+    template <int PART, int OF>
+    __device__ __forceinline__ void multiply_line(int m, const Frag<T>& a, const Frag<T> (&b)[NF]) {
 #pragma unroll
         for (int n = 0; n < NF; ++n) acc[PART * kPart + m][n] = mma(b[n], a, acc[PART * kPart + m][n]);
     }
@@ -560,9 +588,7 @@ struct TileProduct {
         if constexpr (OF == OF_B && PART == 0)
 #pragma unroll
             for (int n = 0; n < NF; ++n) sums[n] = mma(b[n], ones, sums[n]);
-        if constexpr (OF == OF_A)
-#pragma unroll
-            for (int m = 0; m < kPart; ++m) sums[PART * kPart + m] = mma(ones, a[m], sums[PART * kPart + m]);
+        if constexpr (OF == OF_A) sum_a<PART>(a);
 #pragma unroll
         for (int m = 0; m < kPart; ++m)
 #pragma unroll
@@ -582,8 +608,10 @@ struct TileProduct {
     }
     // a, b: the first number of the tile's lines at the first k; alines, blines: lines there are; ks: k there are.
     // HALF: only the first half of a's lines is there, and the waves of the other half only load.
+    // afollows, bfollows: see ByDma.
     template <int OF, bool HALF = false>
-    __device__ __forceinline__ void run(char* lds, const char* a, int64_t aline, int alines, const char* b, int64_t bline, int blines, int64_t ks) {
+    __device__ __forceinline__ void run(char* lds, const char* a, int64_t aline, int alines, bool afollows, const char* b, int64_t bline, int blines, bool bfollows,
+                                        int64_t ks) {
         const int thread = threadIdx.x, lane = thread % 64, wave = thread / 64, wm = wave / WN, wn = wave % WN;
 #pragma unroll
         for (int m = 0; m < MF; ++m)
@@ -591,15 +619,15 @@ struct TileProduct {
             for (int n = 0; n < NF; ++n) acc[m][n] = Acc{0, 0, 0, 0};
         if constexpr (OF != NO_SUMS)
 #pragma unroll
-            for (int i = 0; i < (OF == OF_A ? MF : NF); ++i) sums[i] = Acc{0, 0, 0, 0};
+            for (int i = 0; i < (OF == OF_A ? 2 : NF); ++i) sums[i] = Acc{0, 0, 0, 0};
         const int64_t astep = AA == Adjacent::K ? 128 : aline * A::kStep;
         const int64_t bstep = AB == Adjacent::K ? 128 : bline * B::kStep;
         if constexpr (DMA) {
             const int w = __builtin_amdgcn_readfirstlane(wave);
             ByDma<T, AA, S::kM, S::kThreads> da;
             ByDma<T, AB, S::kN, S::kThreads> db;
-            da.begin(aline, thread);
-            db.begin(bline, thread);
+            da.begin(aline, afollows, thread);
+            db.begin(bline, bfollows, thread);
             const auto load = [&](char* to) {
                 da.load(a, to, alines, ks, thread, w);
                 db.load(b, to + A::kBytes, blines, ks, thread, w);
@@ -611,11 +639,18 @@ struct TileProduct {
             // Four parts a step: while the products of one run, what the next needs is read.  The reads of the last part are those of the next
             // step's first (behind the last step, of what stands there, which nothing uses).
             Frag<T> fa[2][kPart], fb[2][NF];
-            int64_t steps = (ks + A::kStep - 1) / A::kStep;
-            const int rest = AA == Adjacent::K || AB == Adjacent::K ? (int)(ks % A::kStep) : 0;  // k of the last step, if it has a chunk in part
-            const auto clear = [&](char* stage) __attribute__((noinline)) {
-                ByDma<T, AA, S::kM, S::kThreads>::clear(stage, rest, threadIdx.x);
-                ByDma<T, AB, S::kN, S::kThreads>::clear(stage + A::kBytes, rest, threadIdx.x);
+            int steps = ((int)ks + A::kStep - 1) / A::kStep;
+            // What the range check leaves to be done in the last step's stage.  a and b stand kStages steps behind it then.
+            const auto mend = [&](char* stage) __attribute__((always_inline)) {
+                const int rest = (int)ks & (A::kStep - 1), tail = rest ? rest : A::kStep;  // k of the last step
+                const bool partial = (AA == Adjacent::K || AB == Adjacent::K) && rest % A::kChunk;
+                if (!partial && !da.misses(alines, tail) && !db.misses(blines, tail)) return;
+                if (partial) {
+                    ByDma<T, AA, S::kM, S::kThreads>::clear(stage, rest, threadIdx.x);
+                    ByDma<T, AB, S::kN, S::kThreads>::clear(stage + A::kBytes, rest, threadIdx.x);
+                }
+                da.patch(a - kStages * astep, stage, alines, tail, threadIdx.x);
+                db.patch(b - kStages * bstep, stage + A::kBytes, blines, tail, threadIdx.x);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
             };
@@ -623,7 +658,7 @@ struct TileProduct {
             for (int i = 0; i < kStages; ++i) load(lds + i * kStage);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * kLoads) : "memory");
             __builtin_amdgcn_s_barrier();
-            if (rest % A::kChunk && steps == 1) clear(lds);
+            if (steps == 1) mend(lds);
             int at = 0;
             read_b(lds, 0, lane, wn, fb[0]);
             read_a(lds, 0, 0, lane, wm, fa[0]);
@@ -656,10 +691,11 @@ struct TileProduct {
                 asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
-                if (rest % A::kChunk && steps == 2) clear(lds + then);
+                if (steps == 2) mend(lds + then);
                 at = then;
                 now = lds + at;
                 __builtin_amdgcn_sched_barrier(0);
+                if constexpr (OF == OF_A) sum_a<1>(fa[1]);
 #pragma unroll
                 for (int m = 0; m < kPart; ++m) {
                     if (!idle) {
@@ -777,6 +813,13 @@ struct Product {
     float* parts;
 };
 
+// Whether memory of the matrix lies behind the last number of rows up to `row` of x; behind W's of expert `set` up to column `col` and k `k`.
+__device__ inline bool x_follows(const Product& p, int64_t row) { return row < p.rows && p.x.line > 0; }
+template <Adjacent AB>
+__device__ inline bool w_follows(const Product& p, int set, int col, int64_t k) {
+    return (col < p.cols && (AB == Adjacent::L || p.w.line > 0)) || (AB == Adjacent::L && k < p.width) || (set + 1 < p.experts && p.w.set > 0);
+}
+
 template <typename T, Adjacent AB, typename SHAPE, bool DMA>
 __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Ending e) {
     using P = TileProduct<T, Adjacent::K, AB, SHAPE, DMA>;
@@ -806,8 +849,9 @@ __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Endi
     P product;
     const int alines = (int)min((int64_t)BM, r.last - r.first), blines = min(BN, p.cols - n0);
     // The last tile of an expert: half of it takes half the time (48000 rows of 64 experts, 4096 x 4096 bf16: 6 %).
-    if (DMA && SHAPE::kM == 256 && alines <= BM / 2) product.template run<P::NO_SUMS, true>(lds, a, p.x.line, alines, b, p.w.line, blines, ks);
-    else product.template run<P::NO_SUMS>(lds, a, p.x.line, alines, b, p.w.line, blines, ks);
+    const bool afollows = x_follows(p, r.first + alines), bfollows = w_follows<AB>(p, r.set, n0 + blines, k0 + ks);
+    if (DMA && SHAPE::kM == 256 && alines <= BM / 2) product.template run<P::NO_SUMS, true>(lds, a, p.x.line, alines, afollows, b, p.w.line, blines, bfollows, ks);
+    else product.template run<P::NO_SUMS>(lds, a, p.x.line, alines, afollows, b, p.w.line, blines, bfollows, ks);
     product.end(lds, e, r.set, r.first, min(r.last, r.first + BM), n0, p.splits > 1 ? p.parts + (int64_t)split * p.rows * p.cols : nullptr);
 }
 
@@ -847,8 +891,8 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
     const int64_t astep = KW * 128, bstep = AB == Adjacent::K ? KW * 128 : p.w.line * A::kStep * KW;
     ByDma<T, Adjacent::K, R * 16, 64> da;
     ByDma<T, AB, BN, 64> db;
-    da.begin(p.x.line, lane);
-    db.begin(p.w.line, lane);
+    da.begin(p.x.line, x_follows(p, r.first + alines), lane);
+    db.begin(p.w.line, w_follows<AB>(p, r.set, n0 + blines, min((int64_t)p.width, (split + 1) * p.per_split)), lane);
     char* const own = lds + wave * kOwn;
     const auto load = [&](int stage) {
         da.load(a, own + stage * kStage, alines, ks, lane, 0);
@@ -863,17 +907,25 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
 #pragma unroll
         for (int n = 0; n < NF; ++n) acc[m][n] = Acc{0, 0, 0, 0};
     int64_t steps = ks > 0 ? (ks - 1) / (KW * A::kStep) + 1 : 0;
-    const int64_t last = ks - (steps - 1) * (KW * A::kStep);  // k of this wave's last step
+    const int64_t last = ks - (steps - 1) * (KW * A::kStep);  // k from this wave's last step on
     const int rest = last < A::kStep ? (int)last : 0;
+    const int tail = (int)min(last, (int64_t)A::kStep);
+    const bool mend = last <= A::kStep && (rest % A::kChunk || da.misses(alines, tail) || db.misses(blines, tail));
+    const char* const alast = a + (steps - 1) * astep;
+    const char* const blast = b + (steps - 1) * bstep;
 #pragma unroll
     for (int i = 0; i < D; ++i) load(i);
     int stage = 0;
     for (; steps > 0; --steps) {
         constexpr int kLater = (D - 1) * (A::kChunks + B::kChunks);  // loads that were asked for behind this stage's
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLater) : "memory");
-        if (steps == 1 && rest % A::kChunk) {
-            da.clear(own + stage * kStage, rest, lane);
-            db.clear(own + stage * kStage + A::kBytes, rest, lane);
+        if (steps == 1 && mend) {
+            if (rest % A::kChunk) {
+                da.clear(own + stage * kStage, rest, lane);
+                db.clear(own + stage * kStage + A::kBytes, rest, lane);
+            }
+            da.patch(alast, own + stage * kStage, alines, tail, lane);
+            db.patch(blast, own + stage * kStage + A::kBytes, blines, tail, lane);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
         Frag<T> fa[2][R], fb[2][NF];
@@ -1070,7 +1122,9 @@ __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad
     const char* const b = p.b.p + r.first * p.b.line + n0 * sizeof(T);
     P product;
     const auto run = [&](auto of) __attribute__((always_inline)) {
-        product.template run<decltype(of)::value>(lds, a, p.a.line, min(BM, p.m - m0), b, p.b.line, min(BN, p.n - n0), r.last - r.first);
+        const int alines = min(BM, p.m - m0), blines = min(BN, p.n - n0);
+        const bool more = r.last < p.rows;
+        product.template run<decltype(of)::value>(lds, a, p.a.line, alines, more || m0 + alines < p.m, b, p.b.line, blines, more || n0 + blines < p.n, r.last - r.first);
     };
     // The sums of d's columns: the workgroups of the first tiles along W's other side multiply d with ones besides.  (A pass over d of its
     // own took 225 us for 8000 x 16384 bf16, beside 920 for the product.)
@@ -1091,9 +1145,9 @@ __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad
                 for (int q = 0; q < 4; ++q) put(n0 + (wn * NF + n) * 16 + lane / 4 + q, p.n, product.sums[n][q]);
     } else if (p.dbias && p.d_is_a && tile.n == 0) {
         run(std::integral_constant<int, P::OF_A>{});
-        if (wn == 0 && lane < 16)
+        if (wn < MF / 2 && lane < 16)
 #pragma unroll
-            for (int m = 0; m < MF; ++m) put(m0 + (wm * MF + m) * 16 + lane, p.m, product.sums[m][0]);
+            for (int part = 0; part < 2; ++part) put(m0 + (wm * MF + part * (MF / 2) + wn) * 16 + lane, p.m, product.sums[part][0]);
     } else {
         run(std::integral_constant<int, P::NO_SUMS>{});
     }
