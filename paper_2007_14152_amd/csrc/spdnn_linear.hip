@@ -99,7 +99,8 @@ Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t e
     const int64_t steps = ceil_div(k, step_of(type));
     const auto tiles = [&](int bm, int bn) { return (grouped ? rows / bm + sets : ceil_div(rows, bm)) * ceil_div(cols, bn); };  // that have rows
     const int64_t each = ceil_div(rows, sets);
-    if (dma && each <= (grouped ? 48 : 128)) {
+    // (Few rows: W's bytes are what counts.  In 32 bits the matrix instructions do, from 32 rows on.)
+    if (dma && each <= (type == SPDNN_F32 ? 32 : grouped ? 48 : 128)) {
         p.few = each <= (grouped ? 8 : 16) ? 1 : each <= (grouped ? 20 : 32) ? 2 : 4;
         p.bm = 16 * p.few;
         // Tiles of 16 columns where those of 64 leave CUs idle; but columns of adjacent k, or k that are not many: 32 bytes of a row of
@@ -112,7 +113,7 @@ Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t e
         choose([&](int b) { return tiles(b, b); }, steps, 1.0, (size_t)rows * cols * sizeof(float), type, dma, &p.bm, &p.splits);
         p.bn = p.bm;
     }
-    p.mtiles = grouped ? rows / p.bm + experts + 1 : ceil_div(rows, p.bm);
+    p.mtiles = grouped ? std::min<int64_t>(rows, rows / p.bm + experts + 1) : ceil_div(rows, p.bm);
     p.ntiles = ceil_div(cols, p.bn);
     p.per_split = ceil_div(steps, p.splits) * step_of(type);
     p.splits = ceil_div(k, p.per_split);

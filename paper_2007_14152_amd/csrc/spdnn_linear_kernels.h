@@ -387,23 +387,6 @@ __device__ __forceinline__ void end_sums(const Ending& e, int set, int64_t row, 
         }
     }
 }
-// For sums that a lane has in registers.
-template <typename T>
-__device__ __forceinline__ void join_end(const Ending& e, int set, int64_t row, int col, float (&sum)[kEnd]) {
-    Biases<T> bias;
-    Added<T> added;
-    bias.load(e, set, col);
-    added.load(e, row, col);
-    float kept[kEnd];
-#pragma unroll
-    for (int i = 0; i < kEnd; ++i) kept[i] = sum[i];
-    end_sums<T>(e, set, row, col, sum, bias, added, [&](int j) {
-        float one = 0;
-#pragma unroll
-        for (int i = 0; i < kEnd; ++i) one = i == j ? kept[i] : one;
-        return one;
-    });
-}
 // Zeros, for rows of no expert.
 template <typename T>
 __device__ inline void end_zeros(const Ending& e, int64_t row, int col) {
@@ -459,7 +442,7 @@ __device__ inline RowTile row_tile(const int32_t* offsets, int experts, int32_t 
     return {set, first + (int64_t)tile * BM, last};
 }
 
-// The same without what is left over, for kernels whose workgroups are shared out to the XCDs: tiles without rows would make shares
+// The same without what is left over (tiles beyond the last have no rows), for kernels whose workgroups are shared out to the XCDs: tiles without rows would make shares
 // uneven (48000 rows of 64 experts, 4096 x 4096 bf16: 1796 us with them, 1734 without).  f(expert, its first tile, its tiles) for 64 experts at a
 // time, one a lane; gives the number of tiles.
 template <int BM, typename F>
@@ -489,7 +472,7 @@ __device__ inline int row_tiles(const int32_t* offsets, int experts, int32_t row
 template <int BM>
 __device__ inline RowTile full_row_tile(const int32_t* offsets, int experts, int32_t rows, int t) {
     if (!offsets) return {0, (int64_t)t * BM, rows};
-    int set = experts, tile = 0;
+    int set = -1, tile = 0;
     each_expert<BM>(offsets, experts, rows, [&](int e, int first, int tiles) {
         const uint64_t found = __ballot(t >= first && t < first + tiles);
         if (!found) return;
@@ -497,6 +480,7 @@ __device__ inline RowTile full_row_tile(const int32_t* offsets, int experts, int
         set = __builtin_amdgcn_readlane(e, lane);
         tile = t - __builtin_amdgcn_readlane(first, lane);
     });
+    if (set < 0) return {0, rows, rows};
     const int first = min(max(offsets[set], 0), rows);
     const int last = set == experts ? rows : min(max(offsets[set + 1], first), rows);
     return {set, first + (int64_t)tile * BM, last};
@@ -871,7 +855,8 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
     const int t = xcd_order(blockIdx.x, gridDim.x);
     const int split = t / per;
     const TileAt tile = banded(t - split * per, p.mtiles, p.ntiles, 8);
-    const RowTile r = row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
+    // Of less rows than experts, only tiles with rows; of more, without a look at all experts first.
+    const RowTile r = p.rows < p.experts ? full_row_tile<BM>(p.offsets, p.experts, p.rows, tile.m) : row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
     if (r.first >= r.last) return;
     const int n0 = tile.n * BN;
     if (r.set == p.experts) {  // rows of no expert
@@ -989,16 +974,26 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
     }
 }
 
-// Parts of sums added up, split by split.
+// Parts of a sum added up in order, eight of them under way.  (64 parts of 256 x 42 sums: one after the other 61 us.)
+__device__ __forceinline__ float sum_parts(const float* from, int64_t stride, int splits) {
+    float sum = 0;
+    int s = 0;
+    for (; s + 8 <= splits; s += 8) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = from[(s + i) * stride];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[i];
+    }
+    for (; s < splits; ++s) sum += from[s * stride];
+    return sum;
+}
 template <typename T>
 __global__ __launch_bounds__(256) void linear_join_kernel(Product p, Ending e) {
-    const int vecs = (p.cols - 1) / kEnd + 1;
-    const int64_t items = (int64_t)p.rows * vecs;
-    for (int64_t i0 = (int64_t)blockIdx.x * 256; i0 < items; i0 += (int64_t)gridDim.x * 256) {
-        const int64_t i = i0 + threadIdx.x;
-        if (i >= items) continue;
-        const int64_t row = i / vecs;
-        const int col = (int)(i - row * vecs) * kEnd;
+    const int64_t items = (int64_t)p.rows * p.cols;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / p.cols;
+        const int col = (int)(i - row * p.cols);
         int set = 0;
         if (p.offsets) {  // the last expert that begins at the row or before
             int lo = 0, hi = p.experts + 1;
@@ -1009,18 +1004,19 @@ __global__ __launch_bounds__(256) void linear_join_kernel(Product p, Ending e) {
             }
             set = lo;
         }
+        const bool f32 = sizeof(T) == 4 || e.out_f32;
         if (set == p.experts) {
-            end_zeros<T>(e, row, col);
+            for (char* to : {e.out, e.pre})
+                if (to) {
+                    char* const line = to + row * (to == e.out ? e.out_line : e.pre_line);
+                    if (f32) reinterpret_cast<float*>(line)[col] = 0.0f;
+                    else reinterpret_cast<T*>(line)[col] = (T)0.0f;
+                }
             continue;
         }
-        float sum[kEnd] = {};
-        for (int s = 0; s < p.splits; ++s) {
-            const float* const from = p.parts + ((int64_t)s * p.rows + row) * p.cols + col;
-#pragma unroll
-            for (int j = 0; j < kEnd; ++j)
-                if (col + j < p.cols) sum[j] += from[j];
-        }
-        join_end<T>(e, set, row, col, sum);
+        const float sum = sum_parts(p.parts + i, items, p.splits);
+        if (f32) end_one<T, float>(e, set, row, col, sum);
+        else end_one<T, T>(e, set, row, col, sum);
     }
 }
 
@@ -1156,19 +1152,12 @@ __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad
 
 template <typename T>
 __global__ __launch_bounds__(256) void weight_grad_join_kernel(WeightGrad p, Ending e) {
-    const int vecs = (p.n - 1) / kEnd + 1;
-    const int64_t lines = (int64_t)p.experts * p.m, items = lines * vecs;
+    const int64_t items = (int64_t)p.experts * p.m * p.n;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
-        const int64_t line = i / vecs;
-        const int col = (int)(i - line * vecs) * kEnd;
-        float sum[kEnd] = {};
-        for (int s = 0; s < p.splits; ++s) {
-            const float* const from = p.parts + (s * lines + line) * p.n + col;
-#pragma unroll
-            for (int j = 0; j < kEnd; ++j)
-                if (col + j < p.n) sum[j] += from[j];
-        }
-        join_end<T>(e, (int)(line / p.m), line % p.m, col, sum);
+        const int64_t line = i / p.n;
+        const float sum = sum_parts(p.parts + i, items, p.splits);
+        if (sizeof(T) == 4 || e.out_f32) end_one<T, float>(e, (int)(line / p.m), line % p.m, (int)(i - line * p.n), sum);
+        else end_one<T, T>(e, (int)(line / p.m), line % p.m, (int)(i - line * p.n), sum);
     }
 }
 
@@ -1196,8 +1185,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void bias_grad_join_kernel(const float* parts, int32_t splits, int64_t n, void* dbias, bool f32) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
-    float sum = 0;
-    for (int s = 0; s < splits; ++s) sum += parts[s * n + i];
+    const float sum = sum_parts(parts + i, n, splits);
     if (f32) ((float*)dbias)[i] = sum;
     else ((T*)dbias)[i] = rounded<T>(sum);
 }

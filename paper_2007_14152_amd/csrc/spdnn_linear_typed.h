@@ -30,7 +30,7 @@ template <typename T>
 void launch_product(const Plan& c, Adjacent adj, const Product& p, const Ending& e, hipStream_t s) {
     if (adj == Adjacent::K) launch_stored<T, Adjacent::K>(c, p, e, s);
     else launch_stored<T, Adjacent::L>(c, p, e, s);
-    if (c.splits > 1) linear_join_kernel<T><<<loop_groups((int64_t)p.rows * ((p.cols - 1) / kEnd + 1)), 256, 0, s>>>(p, e);
+    if (c.splits > 1) linear_join_kernel<T><<<loop_groups((int64_t)p.rows * p.cols), 256, 0, s>>>(p, e);
 }
 
 template <typename T>
@@ -53,7 +53,7 @@ void launch_weight_grad(const Plan& c, const WeightGrad& p, const Ending& e, hip
     else if (c.dma) weight_grad_kernel<T, Middle<2>, true><<<grid, 256, 0, s>>>(p, e);
     else weight_grad_kernel<T, Middle<2>, false><<<grid, 256, 0, s>>>(p, e);
     if (c.splits > 1) {
-        weight_grad_join_kernel<T><<<loop_groups((int64_t)p.experts * p.m * ((p.n - 1) / kEnd + 1)), 256, 0, s>>>(p, e);
+        weight_grad_join_kernel<T><<<loop_groups((int64_t)p.experts * p.m * p.n), 256, 0, s>>>(p, e);
         const int64_t n = (int64_t)p.experts * (p.d_is_a ? p.m : p.n);
         if (p.dbias) bias_grad_join_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(p.bias_parts, c.splits, n, p.dbias, p.bias_f32);
     }
