@@ -336,6 +336,7 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         p.dbias = dbias;
         p.bias_f32 = grad_type == SPDNN_F32;
         p.d_is_a = transposed != 0;
+        p.sorted = offsets && experts <= 64 && rows / experts >= 256;
         Ending e{};
         e.out = (char*)dweight;
         e.out_line = dweight_stride * size_of(grad_type);

@@ -361,30 +361,45 @@ __device__ inline void end_one(const Ending& e, int set, int64_t row, int col, f
     if (e.add) y += (float)reinterpret_cast<const O*>(e.add + row * e.add_line)[col];
     reinterpret_cast<O*>(e.out + set * e.out_set + row * e.out_line)[col] = rounded<O>(y);
 }
+// out, pre: where the eight go.
 template <typename T, typename O>
-__device__ __forceinline__ void end_eight(const Ending& e, int set, int64_t row, int col, float (&y)[kEnd], const Biases<T>& bias, const Added<T>& added) {
+__device__ __forceinline__ void end_eight(const Ending& e, char* out, char* pre, float (&y)[kEnd], const Biases<T>& bias, const Added<T>& added) {
+    if (e.bias)
 #pragma unroll
-    for (int i = 0; i < kEnd; ++i) y[i] += bias.b[i];
-    if (e.pre) store_vec<kEnd, O>(reinterpret_cast<O*>(e.pre + row * e.pre_line) + col, rounded_vec<O, kEnd>(y), false);
+        for (int i = 0; i < kEnd; ++i) y[i] += bias.b[i];
+    if (e.pre) store_vec<kEnd, O>(reinterpret_cast<O*>(pre), rounded_vec<O, kEnd>(y), false);
     if (e.act != SPDNN_ACT_NONE)
 #pragma unroll
         for (int i = 0; i < kEnd; ++i) y[i] = activated<sizeof(O) == 4>(y[i], e.act);
     if (e.add) added.template add_to<O>(y);
-    store_vec<kEnd, O>(reinterpret_cast<O*>(e.out + set * e.out_set + row * e.out_line) + col, rounded_vec<O, kEnd>(y), false);
+    store_vec<kEnd, O>(reinterpret_cast<O*>(out), rounded_vec<O, kEnd>(y), false);
 }
-// one(i): the sum of column col + i, wanted where the row has less than eight.
+// Where column `col` of row `row` is in out and in pre.
+template <typename T>
+struct Places {
+    char *out, *pre;
+    __device__ __forceinline__ Places(const Ending& e, int set, int64_t row, int col) {
+        const int size = sizeof(T) == 4 || e.out_f32 ? 4 : 2;
+        out = e.out + set * e.out_set + row * e.out_line + (int64_t)col * size;
+        pre = e.pre + row * e.pre_line + (int64_t)col * size;
+    }
+    __device__ __forceinline__ void down(const Ending& e, int rows) {
+        out += rows * e.out_line;
+        pre += rows * e.pre_line;
+    }
+};
+template <typename T>
+__device__ __forceinline__ void end_sums(const Ending& e, const Places<T>& at, float (&sum)[kEnd], const Biases<T>& bias, const Added<T>& added) {
+    if (sizeof(T) == 2 && e.out_f32) end_eight<T, float>(e, at.out, at.pre, sum, bias, added);
+    else end_eight<T, T>(e, at.out, at.pre, sum, bias, added);
+}
+// The columns from `col` to the row's end, where they are less than eight; one(i): the sum of column col + i.
 template <typename T, typename F>
-__device__ __forceinline__ void end_sums(const Ending& e, int set, int64_t row, int col, float (&sum)[kEnd], const Biases<T>& bias, const Added<T>& added, F one) {
-    const bool f32 = sizeof(T) == 2 && e.out_f32;
-    if (col + kEnd <= e.cols) {
-        if (f32) end_eight<T, float>(e, set, row, col, sum, bias, added);
-        else end_eight<T, T>(e, set, row, col, sum, bias, added);
-    } else {
+__device__ __forceinline__ void end_rest(const Ending& e, int set, int64_t row, int col, F one) {
 #pragma unroll 1
-        for (int i = 0; col + i < e.cols; ++i) {
-            if (f32) end_one<T, float>(e, set, row, col + i, one(i));
-            else end_one<T, T>(e, set, row, col + i, one(i));
-        }
+    for (int i = 0; col + i < e.cols; ++i) {
+        if (sizeof(T) == 2 && e.out_f32) end_one<T, float>(e, set, row, col + i, one(i));
+        else end_one<T, T>(e, set, row, col + i, one(i));
     }
 }
 // Zeros, for rows of no expert.
@@ -741,6 +756,7 @@ struct TileProduct {
         const int c = lane % kLanes * 2, col = n0 + wn * (NF * 16) + c * 4;
         Biases<T> bias;
         if (!parts) bias.load(e, set, col);
+        Places<T> places(e, set, first + wm * MF * 16 + lane / kLanes, col);
         Added<T> added[kAhead], then[kAhead];
         const auto fetch = [&](int line, Added<T>(&to)[kAhead]) __attribute__((always_inline)) {
             const int64_t row0 = first + wm * MF * 16 + line + lane / kLanes;
@@ -765,6 +781,8 @@ struct TileProduct {
                 for (int i = 0; i < kAhead; ++i) {
                     const int r = r0 + i * kRows + lane / kLanes;
                     const int64_t row = row0 + i * kRows;
+                    const Places<T> here = places;
+                    places.down(e, kRows);
                     if (row >= last || col >= e.cols) continue;
                     const char* const at = own + r * kLine;
                     const Acc lo = *reinterpret_cast<const Acc*>(at + (c ^ (r & kMask)) * 16);
@@ -775,12 +793,22 @@ struct TileProduct {
 #pragma unroll
                         for (int j = 0; j < kEnd; ++j)
                             if (col + j < e.cols) to[j] = sum[j];
-                    } else {
-                        end_sums<T>(e, set, row, col, sum, bias, added[i], [&](int j) { return *reinterpret_cast<const float*>(at + ((c + j / 4) ^ (r & kMask)) * 16 + j % 4 * 4); });
+                    } else if (col + kEnd <= e.cols) {
+                        end_sums<T>(e, here, sum, bias, added[i]);
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) added[i] = then[i];
+            }
+            // A row's last columns, less than eight, by a lane for each row (by the lane that has them above 64 experts' 4764 x 79 took 173 us,
+            // where 80 columns take 66).
+            const int base = n0 + wn * (NF * 16), rest = base + (e.cols - base) / kEnd * kEnd;
+            if (!parts && base < e.cols && rest < e.cols && rest < base + NF * 16) {
+                const int64_t row = first + (wm * MF + m0) * 16 + lane;
+                if (lane < kTurn * 16 && row < last)
+                    end_rest<T>(e, set, row, rest, [&](int j) {
+                        return *reinterpret_cast<const float*>(own + lane * kLine + (((rest - base + j) / 4) ^ (lane & kMask)) * 16 + (rest - base + j) % 4 * 4);
+                    });
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
@@ -959,12 +987,15 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
             Added<T> added;
             bias.load(e, r.set, col);
             added.load(e, row, col);
-            end_sums<T>(e, r.set, row, col, sum, bias, added, [&](int j) {
-                float one = 0;
+            if (col + kEnd <= e.cols)
+                end_sums<T>(e, Places<T>(e, r.set, row, col), sum, bias, added);
+            else
+                end_rest<T>(e, r.set, row, col, [&](int j) {
+                    float one = 0;
 #pragma unroll
-                for (int w = 0; w < KW; ++w) one += *reinterpret_cast<const float*>(lds + w * kOwn + line * (NF * 64) + ((c + j / 4) ^ (line % (NF * 4))) * 16 + j % 4 * 4);
-                return one;
-            });
+                    for (int w = 0; w < KW; ++w) one += *reinterpret_cast<const float*>(lds + w * kOwn + line * (NF * 64) + ((c + j / 4) ^ (line % (NF * 4))) * 16 + j % 4 * 4);
+                    return one;
+                });
         } else {
             float* const to = p.parts + ((int64_t)split * p.rows + row) * p.cols + col;
 #pragma unroll
@@ -1066,6 +1097,7 @@ struct WeightGrad {
     void* dbias;  // null: not asked for here
     bool bias_f32;
     bool d_is_a;
+    bool sorted;  // long experts first
 };
 
 // Rows of expert `set` that split `split` adds.
@@ -1086,9 +1118,10 @@ __device__ inline RowRange grad_rows(const int32_t* offsets, int32_t rows, int s
 }
 
 // The expert with the `rank`-th largest number of rows: long tiles that begin last would leave the chip to themselves (dW of 12 experts:
-// 10007 x 1500 x 777 floats, dx and dW 437 us in order of experts, 422 so).  Up to 64 experts; more are many tiles anyway, and stay in order.
-__device__ inline int by_load(const int32_t* offsets, int experts, int rank) {
-    if (!offsets || experts > 64) return rank;
+// 10007 x 1500 x 777 floats, dx and dW 437 us in order of experts, 422 so).  Up to 64 experts; more are many tiles anyway, and stay
+// in order, as do small ones (the order takes 6 us: 64 experts with a row each, 4764 x 80 96 us and 67).
+__device__ inline int by_load(const int32_t* offsets, int experts, int rank, bool sorted) {
+    if (!sorted) return rank;
     const int lane = threadIdx.x % 64, e = min(lane, experts - 1);
     const int load = max(offsets[e + 1], 0) - max(offsets[e], 0);
     int before = 0;
@@ -1109,7 +1142,7 @@ __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad
     const int per = p.mtiles * p.ntiles;
     // An expert's tiles and parts at a time, each expert's shared out to the XCDs.
     const int each = per * p.splits;
-    const int set = by_load(p.offsets, p.experts, blockIdx.x / each);
+    const int set = by_load(p.offsets, p.experts, blockIdx.x / each, p.sorted);
     const int t = xcd_order(blockIdx.x % each, each), split = t / per;
     const TileAt tile = banded(t % per, p.mtiles, p.ntiles, 8);
     const RowRange r = grad_rows<P::A::kStep>(p.offsets, p.rows, set, split, p.splits);
