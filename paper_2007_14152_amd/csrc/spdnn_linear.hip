@@ -16,7 +16,8 @@ namespace {
 using namespace spdnn;
 
 constexpr int64_t kMostGroups = 1 << 20;
-constexpr int64_t kMostTiles = 1 << 30;  // of a launch
+// Tiles of a launch: HIP takes less than 2^32 threads, of which tiles of 64 and 128 have 256, others up to 512.
+int64_t most_tiles(int b) { return (b == 64 || b == 128 ? 1 << 24 : 1 << 23) - 1; }
 
 int step_of(int32_t type) { return type == SPDNN_F32 ? 32 : 64; }
 size_t aligned(size_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
@@ -82,6 +83,7 @@ void choose(F tiles, int64_t steps, double uneven, size_t out_bytes, int32_t typ
         if (!dma && tile != 128) continue;
         for (int64_t s = 1; s <= 64; s *= 2) {
             if (s > 1 && (steps / s < 4 || s * out_bytes > kMostParts)) break;
+            if (best < 1e300 && tiles(tile) * s > most_tiles(tile)) break;
             const double us = cost(tile, tiles(tile) * s, k / s, uneven * k / s, type) + (s > 1 ? 9.0 + 2.0 * s * out_bytes / 4e6 : 0.0);
             if (us < best) {
                 best = us;
@@ -100,7 +102,7 @@ Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t e
     const auto tiles = [&](int bm, int bn) { return (grouped ? rows / bm + sets : ceil_div(rows, bm)) * ceil_div(cols, bn); };  // that have rows
     const int64_t each = ceil_div(rows, sets);
     // (Few rows: W's bytes are what counts.  In 32 bits the matrix instructions do, from 32 rows on.)
-    if (dma && each <= (type == SPDNN_F32 ? 32 : grouped ? 48 : 128)) {
+    if (dma && each <= (type == SPDNN_F32 ? 32 : grouped ? 48 : 128) && tiles(16, 64) <= most_tiles(0)) {
         p.few = each <= (grouped ? 8 : 16) ? 1 : each <= (grouped ? 20 : 32) ? 2 : 4;
         p.bm = 16 * p.few;
         // Tiles of 16 columns where those of 64 leave CUs idle; but columns of adjacent k, or k that are not many: 32 bytes of a row of
@@ -135,7 +137,7 @@ Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32_t type
     return p;
 }
 int check_tiles(const Plan& p, int32_t sets) {
-    if ((double)p.mtiles * p.ntiles * p.splits * sets > (double)kMostTiles) return fail(SPDNN_EINVAL, "sizes too large: more than 2^30 tiles");
+    if ((double)p.mtiles * p.ntiles * p.splits * sets > (double)most_tiles(p.few ? 0 : p.bm)) return fail(SPDNN_EINVAL, "sizes too large: too many tiles");
     return SPDNN_OK;
 }
 // The most work memory that any alignment asks for.

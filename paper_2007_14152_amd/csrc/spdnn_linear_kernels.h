@@ -108,7 +108,7 @@ struct Tile {
     static constexpr int kBlock = sizeof(T) == 2 ? 2 : 4;                    // chunks of 16 numbers
     static constexpr int kBlocks = LINES / 16;
 
-    __device__ static int turn(int k) {  // f(k)
+    __device__ static int turn(int k) {  // f(k) of Adjacent::L
         const int f = sizeof(T) == 2 ? (k & 3) | (k >> 3 & 1) << 2 : k >> 2 & 3;
         return f & (kBlocks >= 8 ? 7 : kBlocks >= 4 ? 3 : kBlocks >= 2 ? 1 : 0);
     }
@@ -503,6 +503,11 @@ __device__ inline RowTile full_row_tile(const int32_t* offsets, int experts, int
 
 // --- the product of a tile --------------------------------------------------
 //
+// Bound by the matrix instructions and, for tiles of 256, by the power that they may take: 8192 x 8192 x 8192 bf16 1330 TFLOP/s with k
+// adjacent in both operands, 1400 else (products alone, on what registers hold, 2000; the library's best 1530, 1220 and 1080 for the
+// three layouts), floats 146 to 149 (154).  Neither 160 KB of stages with half the step, nor four waves of 128 x 128, nor one barrier for
+// fewer products gave more.  A CU's tile of 256 x 256 reads 12 KB of LDS for 32 instructions of a wave, three quarters of the rate.
+//
 // A workgroup of WM x WN waves, each with MF x NF fragments: WM * MF * 16 lines of a, WN * NF * 16 lines of b.
 // With operands that go straight to LDS, STAGES steps of k are there or under way.
 template <int MF, int NF, int WM, int WN, int STAGES>
@@ -638,7 +643,7 @@ struct TileProduct {
             // Four parts a step: while the products of one run, what the next needs is read.  The reads of the last part are those of the next
             // step's first (behind the last step, of what stands there, which nothing uses).
             Frag<T> fa[2][kPart], fb[2][NF];
-            int steps = ((int)ks + A::kStep - 1) / A::kStep;
+            int steps = (int)((ks + A::kStep - 1) / A::kStep);
             // What the range check leaves to be done in the last step's stage.  a and b stand kStages steps behind it then.
             const auto mend = [&](char* stage) __attribute__((always_inline)) {
                 const int rest = (int)ks & (A::kStep - 1), tail = rest ? rest : A::kStep;  // k of the last step
@@ -745,9 +750,9 @@ struct TileProduct {
             next = t;
         }
     }
-    // Ends the tile by way of LDS: rows of NF * 16 sums of a wave's own, chunk c of row r at place c ^ r (its last bits).  first, last: out's rows; n0: the
-    // first column; parts: where sums go that are not all there yet (rows of out's), or null.  What add has is asked for kAhead rows a
-    // lane at a time, before the rows ahead of them are ended: with one workgroup on a CU nothing else hides it.
+    // Ends the tile by way of LDS: rows of NF * 16 sums of a wave's own, chunk c of row r at place c ^ r (its last bits).  first, last:
+    // out's rows; n0: the first column; parts: where sums go that are not all there yet (rows of out's), or null.  What add has is asked
+    // for kAhead rows a lane at a time, before the rows ahead of them are ended: with one workgroup on a CU nothing else hides it.
     __device__ __forceinline__ void end(char* lds, const Ending& e, int set, int64_t first, int64_t last, int n0, float* parts) {
         constexpr int kTurn = MF < 4 ? MF : 4, kLanes = NF * 2, kRows = 64 / kLanes, kAhead = kTurn * 16 / kRows < 4 ? kTurn * 16 / kRows : 4;
         constexpr int kLine = NF * 64, kMask = NF * 4 - 1;
@@ -883,8 +888,8 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
     const int t = xcd_order(blockIdx.x, gridDim.x);
     const int split = t / per;
     const TileAt tile = banded(t - split * per, p.mtiles, p.ntiles, 8);
-    // Of less rows than experts, only tiles with rows; of more, without a look at all experts first.
-    const RowTile r = p.rows < p.experts ? full_row_tile<BM>(p.offsets, p.experts, p.rows, tile.m) : row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
+    // Where a tile for each row is less than row_tile() needs, only tiles with rows; else without a look at all experts first.
+    const RowTile r = p.mtiles <= p.rows / BM + p.experts ? full_row_tile<BM>(p.offsets, p.experts, p.rows, tile.m) : row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
     if (r.first >= r.last) return;
     const int n0 = tile.n * BN;
     if (r.set == p.experts) {  // rows of no expert
@@ -1200,19 +1205,24 @@ template <typename T>
 __global__ __launch_bounds__(256) void bias_grad_kernel(const T* d, int64_t d_stride, const int32_t* offsets, int32_t rows, int32_t cols, int32_t splits,
                                                         float* parts, void* dbias, bool f32) {
     __shared__ float sums[4][64];
-    const int set = blockIdx.y, split = blockIdx.z, col = blockIdx.x * 64 + threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int set = blockIdx.y, split = blockIdx.z, wave = threadIdx.x / 64;
     const RowRange r = grad_rows<1>(offsets, rows, set, split, splits);
-    float sum = 0;
-    if (col < cols)
-        for (int64_t row = r.first + wave; row < r.last; row += 4) sum += (float)d[row * d_stride + col];
-    sums[wave][threadIdx.x % 64] = sum;
-    __syncthreads();
-    if (wave || col >= cols) return;
-    for (int w = 1; w < 4; ++w) sum += sums[w][threadIdx.x];
-    const int64_t at = (int64_t)set * cols + col;
-    if (splits > 1) parts[split * ((int64_t)gridDim.y * cols) + at] = sum;
-    else if (f32) ((float*)dbias)[at] = sum;
-    else ((T*)dbias)[at] = rounded<T>(sum);
+    for (int block = blockIdx.x; block <= (cols - 1) / 64; block += gridDim.x) {
+        const int col = block * 64 + threadIdx.x % 64;
+        float sum = 0;
+        if (col < cols)
+            for (int64_t row = r.first + wave; row < r.last; row += 4) sum += (float)d[row * d_stride + col];
+        sums[wave][threadIdx.x % 64] = sum;
+        __syncthreads();
+        if (wave == 0 && col < cols) {
+            for (int w = 1; w < 4; ++w) sum += sums[w][threadIdx.x];
+            const int64_t at = (int64_t)set * cols + col;
+            if (splits > 1) parts[split * ((int64_t)gridDim.y * cols) + at] = sum;
+            else if (f32) ((float*)dbias)[at] = sum;
+            else ((T*)dbias)[at] = rounded<T>(sum);
+        }
+        __syncthreads();
+    }
 }
 template <typename T>
 __global__ __launch_bounds__(256) void bias_grad_join_kernel(const float* parts, int32_t splits, int64_t n, void* dbias, bool f32) {

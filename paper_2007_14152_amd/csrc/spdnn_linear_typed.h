@@ -62,7 +62,7 @@ void launch_weight_grad(const Plan& c, const WeightGrad& p, const Ending& e, hip
 template <typename T>
 void launch_bias_grad(const void* d, int64_t d_stride, const int32_t* offsets, int32_t rows, int32_t cols, int32_t experts, int32_t splits, float* parts,
                       void* dbias, bool f32, hipStream_t s) {
-    const dim3 grid((unsigned)((cols - 1) / 64 + 1), (unsigned)experts, (unsigned)splits);
+    const dim3 grid((unsigned)std::min((cols - 1) / 64 + 1, 1 << 22), (unsigned)experts, (unsigned)splits);
     bias_grad_kernel<T><<<grid, 256, 0, s>>>((const T*)d, d_stride, offsets, rows, cols, splits, parts, dbias, f32);
     const int64_t n = (int64_t)experts * cols;
     if (splits > 1) bias_grad_join_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(parts, splits, n, dbias, f32);

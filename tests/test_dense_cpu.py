@@ -88,6 +88,14 @@ def test_work_memory():
     for bad in [(-1, 8, 8, 0, 1, 0), (1, 0, 8, 0, 1, 0), (1, 8, 0, 0, 1, 0), (1, 8, 8, 0, 0, 0), (1, 8, 8, 0, 1025, 0), (1, 8, 8, 0, 1, 3)]:
         assert L.spdnn_linear_bytes(*bad, ctypes.byref(size)) == sp.SPDNN_EINVAL
         assert L.spdnn_linear_grad_bytes(*bad, 0, 0, 0, ctypes.byref(size)) == sp.SPDNN_EINVAL
+    # A launch takes less than 2^32 threads: more tiles are refused, long and thin outputs within it are not.
+    for big in [(2 ** 31 - 1, 1, 1, 0, 1, 1), (1 << 20, 8, 1 << 24, 0, 1, 1), (1000, 8, 1 << 30, 0, 1, 0)]:
+        assert L.spdnn_linear_bytes(*big, ctypes.byref(size)) == sp.SPDNN_EINVAL and "tiles" in sp.spdnn_last_error()
+    assert L.spdnn_linear_grad_bytes(8, 1 << 24, 1 << 14, 1, 256, 1, 1, 0, 0, ctypes.byref(size)) == sp.SPDNN_EINVAL
+    for type in (0, 1, 2):
+        ask("spdnn_linear_bytes", (1 << 30) - 1, 64, 64, 0, 1, type)
+        ask("spdnn_linear_bytes", (1 << 29) - 1, 4096, 1, 1, 1024, type)
+        ask("spdnn_linear_grad_bytes", 100, (1 << 29) - 1, 1, 0, 1, type, type, 0, 1)  # (dx: 2^22 tiles of 128 x 128; 1000 rows are 2^25)
 
 
 class Shape:

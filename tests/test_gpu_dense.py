@@ -176,6 +176,25 @@ def test_grouped_exact(sp, rows, experts, width, cols, dropped, dtype, transpose
             equal(got, want_grad, what)
 
 
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("rows,experts", [(1, 1), (2, 2), (3, 2), (15, 16), (16, 16), (17, 16), (18, 16), (64, 64), (68, 64), (69, 64), (256, 256), (272, 256),
+                                          (273, 256), (274, 256), (290, 256), (1024, 1024), (1090, 1024), (1100, 1024)])
+def test_about_as_many_rows_as_experts(sp, rows, experts, dtype):
+    """Every row in a tile of its own or all in one, whatever the tiles are counted by; out of memory that held something else."""
+    g = torch.Generator().manual_seed(rows + experts)
+    x, w, dout = whole(g, (rows, 24), dtype), whole(g, (experts, 24, 40), dtype), whole(g, (rows, 40), dtype)
+    at = torch.arange(experts + 1)
+    for offsets in (at.clamp(max=rows), at.clamp(max=rows - 1), (at - experts + rows).clamp(0, rows) * at.sign(), at.sign() * rows, at // experts * rows, at * 0,
+                    loads(1, rows, experts)):
+        offsets = offsets.to(torch.int32)
+        want, grads = ref.linear(x, w, offsets=offsets)[0], ref.linear_grad(dout, x, w, offsets=offsets)[0]
+        off = offsets.to(DEV)
+        torch.full((rows, 40), float("nan"), dtype=dtype, device=DEV)
+        equal(sp.grouped_linear(x.to(DEV), off, w.to(DEV)), want)
+        for what, a, b in zip(("dx", "dweight", "dbias"), sp.grouped_linear_grad(dout.to(DEV), x.to(DEV), off, w.to(DEV), dtype=F32), grads):
+            equal(a, b, what)
+
+
 @pytest.mark.parametrize("name", ref.ACTS)
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (F16, F16), (BF16, F32)])
 @pytest.mark.parametrize("rows,width,cols", [(1, 300, 77), (37, 128, 64), (200, 520, 264)])
