@@ -185,7 +185,7 @@ struct ByRegisters {
 // range takes in the two bytes behind it if the matrix goes on there (`follows`), and otherwise patch() stores the number that is missing.
 //
 // They are written as instructions: the compiler would let the transposing LDS reads wait for all loads of this kind that are under way,
-// for it cannot tell that they go to the other stage.  Whoever reads what they have stored waits with loads_done() and a barrier first.
+// for it cannot tell that they go to the other stage.  Whoever reads what they have stored waits for its count (or all, loads_done()) and at a barrier first.
 constexpr uint32_t kOutside = 1u << 31;
 using Memory __attribute__((ext_vector_type(4))) = int;  // address, bytes, format: the same for all lanes
 // past: leaves nothing in the caches.
@@ -431,82 +431,74 @@ __device__ inline TileAt banded(int t, int mtiles, int ntiles, int band) {
     return {b * band + in % high, in / high};
 }
 
-// Rows of x by expert, in tiles of BM rows that begin with an expert's first: tile t is the (t - start(e))th of the last expert e
-// whose start(e) = offsets[e] / BM + e is not beyond t.  (An expert of n rows at offset o needs at most (o + n) / BM + 1 - o / BM
-// tiles, so that starts leave room; what is left over has no rows.)  What stands behind the last expert's rows is counted as one more,
-// `experts`.  Every lane of a wave gets the same.  Offsets that do not ascend within 0 .. rows give wrong rows, but none outside.
+// Rows of x by expert, in tiles of BM rows that begin with an expert's first; what stands behind the last expert's rows is one more,
+// `experts`.  Only tiles with rows are counted: others would make the XCDs' shares uneven (48000 rows of 64 experts, 4096 x 4096 bf16: 1796 us
+// with them, 1734 without; 256 rows of 256 experts, 4096 x 1024: 291 and 238).  Every wave counts for itself, a lane experts / 64 + 1 experts side by
+// side.  Offsets that do not ascend within 0 .. rows give wrong rows, but none outside.
 struct RowTile {
     int set;
     int64_t first, last;  // rows; none if first >= last
 };
 template <int BM>
-__device__ inline RowTile row_tile(const int32_t* offsets, int experts, int32_t rows, int t) {
-    if (!offsets) return {0, (int64_t)t * BM, rows};
-    const int lane = threadIdx.x % 64;
-    int before = 0;
-    for (int e0 = 0; e0 <= experts; e0 += 64) {
-        const int e = e0 + lane;
-        const bool in = e <= experts && min(max(offsets[min(e, experts)], 0), rows) / BM + e <= t;
-        before += __popcll(__ballot(in));
-    }
-    const int set = max(before - 1, 0);
-    const int first = min(max(offsets[set], 0), rows);
-    const int last = set == experts ? rows : min(max(offsets[set + 1], first), rows);
-    const int tile = t - (first / BM + set);
-    if (tile < 0) return {set, last, last};
-    return {set, first + (int64_t)tile * BM, last};
-}
+struct RowTiles {
+    const int32_t* offsets;
+    int experts, rows, each;
+    int first, own;  // this lane's tiles
+    int all;
 
-// The same without what is left over (tiles beyond the last have no rows), for kernels whose workgroups are shared out to the XCDs: tiles without rows would make shares
-// uneven (48000 rows of 64 experts, 4096 x 4096 bf16: 1796 us with them, 1734 without).  f(expert, its first tile, its tiles) for 64 experts at a
-// time, one a lane; gives the number of tiles.
-template <int BM, typename F>
-__device__ inline int each_expert(const int32_t* offsets, int experts, int32_t rows, F f) {
-    const int lane = threadIdx.x % 64;
-    int before = 0;
-    for (int e0 = 0; e0 <= experts; e0 += 64) {
-        const int e = e0 + lane;
-        const int first = min(max(offsets[min(e, experts)], 0), rows);
-        const int last = e >= experts ? rows : min(max(offsets[e + 1], first), rows);
-        const int tiles = e > experts ? 0 : (last - first + BM - 1) / BM;
-        int upto = tiles;
+    __device__ __forceinline__ int expert_first(int e) const { return min(max(offsets[min(e, experts)], 0), rows); }
+    __device__ __forceinline__ int expert_last(int e, int from) const { return e >= experts ? rows : min(max(offsets[e + 1], from), rows); }
+    __device__ __forceinline__ int expert_tiles(int e) const {
+        const int from = expert_first(e), to = expert_last(e, from);
+        return e > experts || to <= from ? 0 : (to - from - 1) / BM + 1;
+    }
+    // Sums over this lane and those before it.
+    __device__ __forceinline__ static int upto(int x) {
+        const int lane = threadIdx.x % 64;
 #pragma unroll
         for (int step = 1; step < 64; step *= 2) {
-            const int other = __shfl_up(upto, step);
-            if (lane >= step) upto += other;
+            const int other = __shfl_up(x, step);
+            if (lane >= step) x += other;
         }
-        f(e, before + upto - tiles, tiles);
-        before += __builtin_amdgcn_readlane(upto, 63);
+        return x;
     }
-    return before;
-}
-template <int BM>
-__device__ inline int row_tiles(const int32_t* offsets, int experts, int32_t rows, int mtiles) {
-    return offsets ? each_expert<BM>(offsets, experts, rows, [](int, int, int) {}) : mtiles;
-}
-template <int BM>
-__device__ inline RowTile full_row_tile(const int32_t* offsets, int experts, int32_t rows, int t) {
-    if (!offsets) return {0, (int64_t)t * BM, rows};
-    int set = -1, tile = 0;
-    each_expert<BM>(offsets, experts, rows, [&](int e, int first, int tiles) {
-        const uint64_t found = __ballot(t >= first && t < first + tiles);
-        if (!found) return;
+    // others: tiles where there are no offsets.
+    __device__ __forceinline__ RowTiles(const int32_t* o, int e, int32_t r, int others) : offsets(o), experts(e), rows(r), each(e / 64 + 1), first(0), own(0), all(others) {
+        if (!offsets) return;
+        const int lane = threadIdx.x % 64;
+#pragma unroll 4
+        for (int i = 0; i < each; ++i) own += expert_tiles(lane * each + i);
+        const int until = upto(own);
+        first = until - own;
+        all = __builtin_amdgcn_readlane(until, 63);
+    }
+    __device__ __forceinline__ RowTile tile(int t) const {
+        if (!offsets) return {0, (int64_t)t * BM, rows};
+        const uint64_t found = __ballot(t >= first && t < first + own);
+        if (!found) return {0, rows, rows};
         const int lane = __ffsll((unsigned long long)found) - 1;
-        set = __builtin_amdgcn_readlane(e, lane);
-        tile = t - __builtin_amdgcn_readlane(first, lane);
-    });
-    if (set < 0) return {0, rows, rows};
-    const int first = min(max(offsets[set], 0), rows);
-    const int last = set == experts ? rows : min(max(offsets[set + 1], first), rows);
-    return {set, first + (int64_t)tile * BM, last};
-}
+        int set = lane * each, in = t - __builtin_amdgcn_readlane(first, lane);
+        if (each > 1) {
+            const int mine = (int)(threadIdx.x % 64) < each ? expert_tiles(set + (int)(threadIdx.x % 64)) : 0;
+            const int until = upto(mine);
+            const uint64_t which = __ballot(in >= until - mine && in < until);
+            if (!which) return {0, rows, rows};
+            const int at = __ffsll((unsigned long long)which) - 1;
+            set += at;
+            in -= __builtin_amdgcn_readlane(until - mine, at);
+        }
+        const int from = expert_first(set);
+        return {set, from + (int64_t)in * BM, expert_last(set, from)};
+    }
+};
 
 // --- the product of a tile --------------------------------------------------
 //
 // Bound by the matrix instructions and, for tiles of 256, by the power that they may take: 8192 x 8192 x 8192 bf16 1330 TFLOP/s with k
 // adjacent in both operands, 1400 else (products alone, on what registers hold, 2000; the library's best 1530, 1220 and 1080 for the
 // three layouts), floats 146 to 149 (154).  Neither 160 KB of stages with half the step, nor four waves of 128 x 128, nor one barrier for
-// fewer products gave more.  A CU's tile of 256 x 256 reads 12 KB of LDS for 32 instructions of a wave, three quarters of the rate.
+// fewer products gave more.  A wave of a tile of 256 x 256 reads 12 KB of LDS for 32 instructions: three quarters of what LDS gives in that
+// time; smaller tiles read more for each product, and are taken where there are few tiles or little k (choose() of spdnn_linear.hip).
 //
 // A workgroup of WM x WN waves, each with MF x NF fragments: WM * MF * 16 lines of a, WN * NF * 16 lines of b.
 // With operands that go straight to LDS, STAGES steps of k are there or under way.
@@ -837,18 +829,20 @@ __device__ inline bool w_follows(const Product& p, int set, int col, int64_t k) 
     return (col < p.cols && (AB == Adjacent::L || p.w.line > 0)) || (AB == Adjacent::L && k < p.width) || (set + 1 < p.experts && p.w.set > 0);
 }
 
+// out = act(x W + b) + add, a tile for each workgroup.  24000 x 4096 x 4096 bf16 667 us with gelu and a residual (1.2 PFLOP/s), 609 without
+// both; 48000 rows of 64 experts of 4096 x 4096 1.70 ms (0.95: an expert's last tile, and W that changes, cost what is missing).
 template <typename T, Adjacent AB, typename SHAPE, bool DMA>
 __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Ending e) {
     using P = TileProduct<T, Adjacent::K, AB, SHAPE, DMA>;
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
-    const int mtiles = row_tiles<BM>(p.offsets, p.experts, p.rows, p.mtiles);
-    const int per = mtiles * p.ntiles;
+    const RowTiles<BM> tiles(p.offsets, p.experts, p.rows, p.mtiles);
+    const int mtiles = tiles.all, per = mtiles * p.ntiles;
     if ((int)blockIdx.x >= per * p.splits) return;
     const int t = xcd_order(blockIdx.x, per * p.splits);
     const int split = t / per;
     const TileAt tile = banded(t - split * per, mtiles, p.ntiles, 8);
-    const RowTile r = full_row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
+    const RowTile r = tiles.tile(tile.m);
     if (r.first >= r.last) return;
     const int n0 = tile.n * BN;
     if (r.set == p.experts) {  // rows of no expert
@@ -884,12 +878,13 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
     static_assert(kSums <= kOwn);
     constexpr int BM = R * 16, BN = NF * 16;
     __shared__ __align__(16) char lds[KW * kOwn];
-    const int per = p.mtiles * p.ntiles;
-    const int t = xcd_order(blockIdx.x, gridDim.x);
+    const RowTiles<BM> tiles(p.offsets, p.experts, p.rows, p.mtiles);
+    const int mtiles = tiles.all, per = mtiles * p.ntiles;
+    if ((int)blockIdx.x >= per * p.splits) return;
+    const int t = xcd_order(blockIdx.x, per * p.splits);
     const int split = t / per;
-    const TileAt tile = banded(t - split * per, p.mtiles, p.ntiles, 8);
-    // Where a tile for each row is less than row_tile() needs, only tiles with rows; else without a look at all experts first.
-    const RowTile r = p.mtiles <= p.rows / BM + p.experts ? full_row_tile<BM>(p.offsets, p.experts, p.rows, tile.m) : row_tile<BM>(p.offsets, p.experts, p.rows, tile.m);
+    const TileAt tile = banded(t - split * per, mtiles, p.ntiles, 8);
+    const RowTile r = tiles.tile(tile.m);
     if (r.first >= r.last) return;
     const int n0 = tile.n * BN;
     if (r.set == p.experts) {  // rows of no expert
@@ -1059,7 +1054,8 @@ __global__ __launch_bounds__(256) void linear_join_kernel(Product p, Ending e) {
 // --- gradients --------------------------------------------------------------
 
 // d[r] = dout[r] * act'(pre[r]) in the rows' type, rows of no expert left out: what both products of the gradient take.  The matrix
-// instructions take 16 bits a number: this is where the slope's product is rounded to them.
+// instructions take 16 bits a number: this is where the slope's product is rounded to them.  Bound by memory: 8000 x 16384 bf16 133 us (5.9 TB/s);
+// formed in the products' loads instead, dout and pre would both be read there, by every tile beside another.
 template <typename T, typename D>
 __global__ __launch_bounds__(256) void slope_kernel(const D* dout, int64_t dout_stride, const D* pre, int64_t pre_stride, int act, int32_t rows,
                                                     int32_t cols, const int32_t* offsets, int32_t experts, T* d, int64_t d_stride) {
@@ -1138,6 +1134,8 @@ __device__ inline int by_load(const int32_t* offsets, int experts, int rank, boo
     return found ? __ffsll((unsigned long long)found) - 1 : rank;
 }
 
+// A tile of dW, k being the rows: both operands have k as their stored rows, which the transposing reads of LDS turn, and nothing is transposed in memory.
+// 8192 x 8192 x 8192 bf16 1416 TFLOP/s (the library's best for this layout 1080); 12 experts of 10007 x 1500 x 777 floats with dx 415 us.
 template <typename T, typename SHAPE, bool DMA>
 __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad p, Ending e) {
     using P = TileProduct<T, Adjacent::L, Adjacent::L, SHAPE, DMA>;
@@ -1200,7 +1198,7 @@ __global__ __launch_bounds__(256) void weight_grad_join_kernel(WeightGrad p, End
 }
 
 // dbias[e][c] = sum over the rows of expert e of d[r][c]: a workgroup has 64 columns; its four waves add every fourth row, and
-// their sums are added in order.
+// their sums are added in order.  (Only where dW is not asked for.)
 template <typename T>
 __global__ __launch_bounds__(256) void bias_grad_kernel(const T* d, int64_t d_stride, const int32_t* offsets, int32_t rows, int32_t cols, int32_t splits,
                                                         float* parts, void* dbias, bool f32) {

@@ -48,9 +48,9 @@ bool with_row_of(int32_t width, F f) {
     });
 }
 
-// Threads that take rows in turn, a few to every lane of the chip.
+// Threads that take rows in turn: as many as the chip's 256 CUs hold.
 constexpr int64_t kNormThreads = 2048 * 256;
-// Workgroups that add columns: each leaves a part.
+// Workgroups that add columns, each of which leaves a part: two a CU.  60000 x 1024 bf16: 256 107 us, 512 98, 768 102, 1024 111, 2048 113.
 constexpr int64_t kParts = 512;
 int64_t parts_of(int32_t rows) { return std::min<int64_t>(rows, kParts); }
 

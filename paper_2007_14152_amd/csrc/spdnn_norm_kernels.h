@@ -69,7 +69,9 @@ struct Norm {
 
 // out[t] = (x[t] - mean) * rstd * weight + bias.  A team of G lanes (a wave, or the workgroup) has a row, U vectors a lane, in
 // registers: it is read once, and the variance is that of the differences from the mean, which does not cancel.  (WHOLE: V divides the
-// width, and no vector has numbers of the one before it.)  A team takes rows in turn, with the next row under way and the parameters in registers.
+// width, and no vector has numbers of the one before it.)  A team takes rows in turn, with the next row under way and the parameters in
+// registers.  Bound by memory: 24000 x 4096 bf16 73 us (5.4 TB/s; stores that stay in the caches 78; a wave for every row, which reads the
+// parameters for it, 116).
 template <typename T, typename O, int V, bool WHOLE, int U, int G, int THREADS>
 __global__ __launch_bounds__(THREADS) void layer_norm_kernel(Norm p, const T* __restrict__ x, int64_t x_stride, O* __restrict__ out, int64_t out_stride) {
     __shared__ float lds[G > 64 ? 2 * (G / 64) : 1];
@@ -182,7 +184,8 @@ struct NormGrad {
 
 // With h = (x - mean) * rstd and g = dout * weight: dx = rstd * (g - mean(g) - h * mean(g * h)) + add, and for a part of the rows
 // the sums of dout * h and of dout, column by column.  A team takes rows in turn and keeps its columns' sums in registers; the teams
-// of a workgroup are added in order through LDS.
+// of a workgroup are added in order through LDS.  60000 x 1024 bf16 with add 98 us (5.0 TB/s) with the join, 78 of which what is read and
+// written asks for.
 template <typename T, int V, bool WHOLE, int U, int G, int THREADS>
 __global__ __launch_bounds__(THREADS) void layer_norm_grad_kernel(NormGrad p, const T* __restrict__ dout, int64_t dout_stride, const T* __restrict__ x,
                                                                   int64_t x_stride, const T* __restrict__ add, int64_t add_stride, T* __restrict__ dx,

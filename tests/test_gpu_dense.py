@@ -178,7 +178,9 @@ def test_grouped_exact(sp, rows, experts, width, cols, dropped, dtype, transpose
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
 @pytest.mark.parametrize("rows,experts", [(1, 1), (2, 2), (3, 2), (15, 16), (16, 16), (17, 16), (18, 16), (64, 64), (68, 64), (69, 64), (256, 256), (272, 256),
-                                          (273, 256), (274, 256), (290, 256), (1024, 1024), (1090, 1024), (1100, 1024)])
+                                          (273, 256), (274, 256), (290, 256), (1024, 1024), (1090, 1024), (1100, 1024),
+                                          # and experts about as many as a wave has lanes
+                                          (100, 63), (130, 65), (127, 127), (500, 128), (9000, 63), (9000, 64), (20000, 130)])
 def test_about_as_many_rows_as_experts(sp, rows, experts, dtype):
     """Every row in a tile of its own or all in one, whatever the tiles are counted by; out of memory that held something else."""
     g = torch.Generator().manual_seed(rows + experts)
