@@ -462,7 +462,7 @@ struct RowTiles {
         }
         return x;
     }
-    // others: tiles where there are no offsets.
+    // others: tiles of the launch, which are all where there are no offsets.
     __device__ __forceinline__ RowTiles(const int32_t* o, int e, int32_t r, int others) : offsets(o), experts(e), rows(r), each(e / 64 + 1), first(0), own(0), all(others) {
         if (!offsets) return;
         const int lane = threadIdx.x % 64;
@@ -470,7 +470,7 @@ struct RowTiles {
         for (int i = 0; i < each; ++i) own += expert_tiles(lane * each + i);
         const int until = upto(own);
         first = until - own;
-        all = __builtin_amdgcn_readlane(until, 63);
+        all = min(max(__builtin_amdgcn_readlane(until, 63), 0), others);  // (of wrong offsets more)
     }
     __device__ __forceinline__ RowTile tile(int t) const {
         if (!offsets) return {0, (int64_t)t * BM, rows};
@@ -829,7 +829,7 @@ __device__ inline bool w_follows(const Product& p, int set, int col, int64_t k) 
     return (col < p.cols && (AB == Adjacent::L || p.w.line > 0)) || (AB == Adjacent::L && k < p.width) || (set + 1 < p.experts && p.w.set > 0);
 }
 
-// out = act(x W + b) + add, a tile for each workgroup.  24000 x 4096 x 4096 bf16 667 us with gelu and a residual (1.2 PFLOP/s), 609 without
+// out = act(x W + b) + add, a tile for each workgroup.  24000 x 4096 x 4096 bf16 672 us with a bias and a residual (1.2 PFLOP/s), 609 without
 // both; 48000 rows of 64 experts of 4096 x 4096 1.70 ms (0.95: an expert's last tile, and W that changes, cost what is missing).
 template <typename T, Adjacent AB, typename SHAPE, bool DMA>
 __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Ending e) {
