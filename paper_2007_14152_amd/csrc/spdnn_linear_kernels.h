@@ -472,23 +472,38 @@ struct RowTiles {
         first = until - own;
         all = min(max(__builtin_amdgcn_readlane(until, 63), 0), others);  // (of wrong offsets more)
     }
-    __device__ __forceinline__ RowTile tile(int t) const {
-        if (!offsets) return {0, (int64_t)t * BM, rows};
-        const uint64_t found = __ballot(t >= first && t < first + own);
-        if (!found) return {0, rows, rows};
-        const int lane = __ffsll((unsigned long long)found) - 1;
-        int set = lane * each, in = t - __builtin_amdgcn_readlane(first, lane);
-        if (each > 1) {
-            const int mine = (int)(threadIdx.x % 64) < each ? expert_tiles(set + (int)(threadIdx.x % 64)) : 0;
-            const int until = upto(mine);
-            const uint64_t which = __ballot(in >= until - mine && in < until);
-            if (!which) return {0, rows, rows};
-            const int at = __ffsll((unsigned long long)which) - 1;
-            set += at;
-            in -= __builtin_amdgcn_readlane(until - mine, at);
+    // Tile t of all * ntiles, and its columns'.  Bands of eight tiles of rows, so that an XCD's workgroups share W's columns and x's
+    // rows in its L2; EACH: bands that end with an expert's rows, so that they share one W (48000 rows of 64 experts, 4096 x 4096 bf16: 1684
+    // us, so 1580 to 1610).  For few rows, where no W is shared, bands over experts are better by up to 15 %.
+    template <bool EACH>
+    __device__ __forceinline__ RowTile tile(int t, int ntiles, int* n) const {
+        TileAt at = banded(t, all, ntiles, 8);
+        int set = 0, begin = 0, count = all, from = 0, to = rows;
+        if (offsets) {
+            const int m = EACH ? t / ntiles : at.m;
+            const uint64_t found = __ballot(m >= first && m < first + own);
+            if (!found) return {0, rows, rows};
+            const int lane = __ffsll((unsigned long long)found) - 1;
+            set = lane * each;
+            begin = __builtin_amdgcn_readlane(first, lane);
+            count = __builtin_amdgcn_readlane(own, lane);
+            if (each > 1) {
+                const int mine = (int)(threadIdx.x % 64) < each ? expert_tiles(set + (int)(threadIdx.x % 64)) : 0;
+                const int until = begin + upto(mine);
+                const uint64_t which = __ballot(m >= until - mine && m < until);
+                if (!which) return {0, rows, rows};
+                const int next = __ffsll((unsigned long long)which) - 1;
+                set += next;
+                count = __builtin_amdgcn_readlane(mine, next);
+                begin = __builtin_amdgcn_readlane(until, next) - count;
+            }
+            from = expert_first(set);
+            to = expert_last(set, from);
+            if (EACH) at = banded(t - begin * ntiles, count, ntiles, 8);
+            else at.m -= begin;
         }
-        const int from = expert_first(set);
-        return {set, from + (int64_t)in * BM, expert_last(set, from)};
+        *n = at.n;
+        return {set, from + (int64_t)at.m * BM, to};
     }
 };
 
@@ -830,21 +845,21 @@ __device__ inline bool w_follows(const Product& p, int set, int col, int64_t k) 
 }
 
 // out = act(x W + b) + add, a tile for each workgroup.  24000 x 4096 x 4096 bf16 672 us with a bias and a residual (1.2 PFLOP/s), 609 without
-// both; 48000 rows of 64 experts of 4096 x 4096 1.70 ms (0.95: an expert's last tile, and W that changes, cost what is missing).
+// both; 48000 rows of 64 experts of 4096 x 4096 1.6 ms (1.0: an expert's last tile, and W that changes, cost what is missing).
 template <typename T, Adjacent AB, typename SHAPE, bool DMA>
 __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Ending e) {
     using P = TileProduct<T, Adjacent::K, AB, SHAPE, DMA>;
     __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const RowTiles<BM> tiles(p.offsets, p.experts, p.rows, p.mtiles);
-    const int mtiles = tiles.all, per = mtiles * p.ntiles;
+    const int per = tiles.all * p.ntiles;
     if ((int)blockIdx.x >= per * p.splits) return;
     const int t = xcd_order(blockIdx.x, per * p.splits);
     const int split = t / per;
-    const TileAt tile = banded(t - split * per, mtiles, p.ntiles, 8);
-    const RowTile r = tiles.tile(tile.m);
+    int ntile = 0;
+    const RowTile r = tiles.template tile<true>(t - split * per, p.ntiles, &ntile);
     if (r.first >= r.last) return;
-    const int n0 = tile.n * BN;
+    const int n0 = ntile * BN;
     if (r.set == p.experts) {  // rows of no expert
         if (split == 0 && p.splits == 1)
             for (int64_t row = r.first + threadIdx.x / (BN / kEnd); row < min(r.last, r.first + BM); row += blockDim.x / (BN / kEnd)) {
@@ -879,14 +894,14 @@ __global__ __launch_bounds__(KW * 64) void linear_short_kernel(Product p, Ending
     constexpr int BM = R * 16, BN = NF * 16;
     __shared__ __align__(16) char lds[KW * kOwn];
     const RowTiles<BM> tiles(p.offsets, p.experts, p.rows, p.mtiles);
-    const int mtiles = tiles.all, per = mtiles * p.ntiles;
+    const int per = tiles.all * p.ntiles;
     if ((int)blockIdx.x >= per * p.splits) return;
     const int t = xcd_order(blockIdx.x, per * p.splits);
     const int split = t / per;
-    const TileAt tile = banded(t - split * per, mtiles, p.ntiles, 8);
-    const RowTile r = tiles.tile(tile.m);
+    int ntile = 0;
+    const RowTile r = tiles.template tile<false>(t - split * per, p.ntiles, &ntile);
     if (r.first >= r.last) return;
-    const int n0 = tile.n * BN;
+    const int n0 = ntile * BN;
     if (r.set == p.experts) {  // rows of no expert
         if (split == 0 && p.splits == 1)
             for (int64_t row = r.first + threadIdx.x / (BN / kEnd); row < min(r.last, r.first + BM); row += KW * 64 / (BN / kEnd)) {
