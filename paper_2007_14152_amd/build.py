@@ -32,7 +32,7 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
 
 
 # (and kernels of the dense products: what is read back from scratch waits for all loads to LDS that are under way)
-NO_SCRATCH_KERNELS = ["fused_row2_kernel", "fused_pair_kernel", "13linear_kernel", "linear_short_kernel", "weight_grad_kernel"]
+NO_SCRATCH_KERNELS = ["fused_row2_kernel", "fused_pair_kernel", "13linear_kernel", "linear_short_kernel", "weight_grad_kernel", "grads_kernel"]
 # Kernels that count LDS addresses from the start of the workgroup's LDS: all of it must be dynamic.
 LDS_FROM_ZERO_KERNELS = ["resident_kernel", "fused_flat_kernel", "few_kernel", "strided_kernel"]
 # Bytes of scratch per lane that these may spill: outside the arithmetic, at what was measured with them.  (Spills are

@@ -157,14 +157,14 @@ bool dma_side(const Side& s, Adjacent adj, int32_t along, int32_t type) {
     return s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size_of(type));
 }
 
-void run_product(int32_t type, Adjacent adj, Product p, Ending e, hipStream_t s) {
+Plan plan_of(int32_t type, Adjacent adj, Product& p) {
     const bool dma = dma_side(p.x, Adjacent::K, p.width, type) && dma_side(p.w, adj, adj == Adjacent::K ? p.width : p.cols, type);
     const Plan c = plan_product(p.rows, p.width, p.cols, p.offsets != nullptr, p.experts, type, dma, adj);
     p.mtiles = (int32_t)c.mtiles;
     p.ntiles = (int32_t)c.ntiles;
     p.splits = (int32_t)c.splits;
     p.per_split = c.per_split;
-    with_type(type, [&](auto tt) { launch_product<decltype(tt)>(c, adj, p, e, s); });
+    return c;
 }
 
 // Work memory of the gradients: d in the rows' type where dout is not that already, and parts, which the three steps use in turn.
@@ -249,7 +249,9 @@ int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64
     e.cols = cols;
     e.act = act;
     e.out_f32 = out_type == SPDNN_F32;
-    run_product(type, transposed ? Adjacent::K : Adjacent::L, p, e, (hipStream_t)hip_stream);
+    const Adjacent adj = transposed ? Adjacent::K : Adjacent::L;
+    const Plan c = plan_of(type, adj, p);
+    with_type(type, [&](auto tt) { launch_product<decltype(tt)>(c, adj, p, e, (hipStream_t)hip_stream); });
     return launched();
 }
 
@@ -300,8 +302,13 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
                                        d_stride, s);
         });
     }
-    if (dx && rows > 0) {
-        Product p{};
+    const bool has_x = dx && rows > 0;
+    const Adjacent adj = transposed ? Adjacent::L : Adjacent::K;
+    Product px{};
+    Ending ex{};
+    Plan cx{};
+    if (has_x) {
+        Product& p = px;
         p.x = {(const char*)d, d_stride * size, 0};
         p.w = {(const char*)weight, weight_stride * size, expert_stride * size};
         p.offsets = offsets;
@@ -310,14 +317,17 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         p.cols = width;
         p.experts = experts;
         p.parts = parts;
-        Ending e{};
+        Ending& e = ex;
         e.out = (char*)dx;
         e.out_line = dx_stride * size;
         e.cols = width;
         e.act = SPDNN_ACT_NONE;
         e.out_f32 = type == SPDNN_F32;
-        run_product(type, transposed ? Adjacent::L : Adjacent::K, p, e, s);
+        cx = plan_of(type, adj, p);
     }
+    const auto run_x = [&] {
+        if (has_x) with_type(type, [&](auto tt) { launch_product<decltype(tt)>(cx, adj, px, ex, s); });
+    };
     if (dweight) {
         const Side sx{(const char*)x, x_stride * size, 0}, sd{(const char*)d, d_stride * size, 0};
         WeightGrad p{};
@@ -346,8 +356,17 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         e.cols = p.n;
         e.act = SPDNN_ACT_NONE;
         e.out_f32 = grad_type == SPDNN_F32;
-        with_type(type, [&](auto tt) { launch_weight_grad<decltype(tt)>(c, p, e, s); });
-    } else if (dbias) {
+        const auto small = [](const Plan& q) { return q.dma && !q.few && q.bm == 64 && q.splits == 1; };
+        if (has_x && small(cx) && small(c) && cx.mtiles * cx.ntiles + c.mtiles * c.ntiles * experts + 8 <= most_tiles(64)) {
+            with_type(type, [&](auto tt) { launch_grads<decltype(tt)>(cx, adj, px, ex, c, p, e, s); });
+        } else {
+            run_x();
+            with_type(type, [&](auto tt) { launch_weight_grad<decltype(tt)>(c, p, e, s); });
+        }
+        return launched();
+    }
+    run_x();
+    if (dbias) {
         with_type(type, [&](auto tt) {
             launch_bias_grad<decltype(tt)>(d, d_stride, offsets, rows, cols, experts, (int32_t)w.bias_splits, parts, dbias, grad_type == SPDNN_F32, s);
         });

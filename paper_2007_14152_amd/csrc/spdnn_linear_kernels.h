@@ -847,14 +847,13 @@ __device__ inline bool w_follows(const Product& p, int set, int col, int64_t k) 
 // out = act(x W + b) + add, a tile for each workgroup.  24000 x 4096 x 4096 bf16 672 us with a bias and a residual (1.2 PFLOP/s), 609 without
 // both; 48000 rows of 64 experts of 4096 x 4096 1.6 ms (1.0: an expert's last tile, and W that changes, cost what is missing).
 template <typename T, Adjacent AB, typename SHAPE, bool DMA>
-__global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Ending e) {
+__device__ __forceinline__ void linear_tile(char* lds, const Product& p, const Ending& e, int bid) {
     using P = TileProduct<T, Adjacent::K, AB, SHAPE, DMA>;
-    __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const RowTiles<BM> tiles(p.offsets, p.experts, p.rows, p.mtiles);
     const int per = tiles.all * p.ntiles;
-    if ((int)blockIdx.x >= per * p.splits) return;
-    const int t = xcd_order(blockIdx.x, per * p.splits);
+    if (bid >= per * p.splits) return;
+    const int t = xcd_order(bid, per * p.splits);
     const int split = t / per;
     int ntile = 0;
     const RowTile r = tiles.template tile<true>(t - split * per, p.ntiles, &ntile);
@@ -879,6 +878,11 @@ __global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Endi
     if (DMA && SHAPE::kM == 256 && alines <= BM / 2) product.template run<P::NO_SUMS, true>(lds, a, p.x.line, alines, afollows, b, p.w.line, blines, bfollows, ks);
     else product.template run<P::NO_SUMS>(lds, a, p.x.line, alines, afollows, b, p.w.line, blines, bfollows, ks);
     product.end(lds, e, r.set, r.first, min(r.last, r.first + BM), n0, p.splits > 1 ? p.parts + (int64_t)split * p.rows * p.cols : nullptr);
+}
+template <typename T, Adjacent AB, typename SHAPE, bool DMA>
+__global__ __launch_bounds__(SHAPE::kThreads) void linear_kernel(Product p, Ending e) {
+    __shared__ __align__(16) char lds[TileProduct<T, Adjacent::K, AB, SHAPE, DMA>::kLds];
+    linear_tile<T, AB, SHAPE, DMA>(lds, p, e, blockIdx.x);
 }
 
 // The same for few rows (R * 16 of a tile), where the weights' bytes are what counts.  Every wave has all of the tile (NF * 16 columns) and
@@ -1152,16 +1156,15 @@ __device__ inline int by_load(const int32_t* offsets, int experts, int rank, boo
 // A tile of dW, k being the rows: both operands have k as their stored rows, which the transposing reads of LDS turn, and nothing is transposed in memory.
 // 8192 x 8192 x 8192 bf16 1416 TFLOP/s (the library's best for this layout 1080); 12 experts of 10007 x 1500 x 777 floats with dx 415 us.
 template <typename T, typename SHAPE, bool DMA>
-__global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad p, Ending e) {
+__device__ __forceinline__ void weight_grad_tile(char* lds, const WeightGrad& p, const Ending& e, int bid) {
     using P = TileProduct<T, Adjacent::L, Adjacent::L, SHAPE, DMA>;
     constexpr int MF = P::MF, NF = P::NF, WN = P::WN;
-    __shared__ __align__(16) char lds[P::kLds];
     constexpr int BM = P::S::kM, BN = P::S::kN;
     const int per = p.mtiles * p.ntiles;
     // An expert's tiles and parts at a time, each expert's shared out to the XCDs.
     const int each = per * p.splits;
-    const int set = by_load(p.offsets, p.experts, blockIdx.x / each, p.sorted);
-    const int t = xcd_order(blockIdx.x % each, each), split = t / per;
+    const int set = by_load(p.offsets, p.experts, bid / each, p.sorted);
+    const int t = xcd_order(bid % each, each), split = t / per;
     const TileAt tile = banded(t % per, p.mtiles, p.ntiles, 8);
     const RowRange r = grad_rows<P::A::kStep>(p.offsets, p.rows, set, split, p.splits);
     const int m0 = tile.m * BM, n0 = tile.n * BN;
@@ -1199,6 +1202,23 @@ __global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad
         run(std::integral_constant<int, P::NO_SUMS>{});
     }
     product.end(lds, e, set, m0, min(p.m, m0 + BM), n0, p.splits > 1 ? p.parts + ((int64_t)split * p.experts + set) * p.m * p.n : nullptr);
+}
+template <typename T, typename SHAPE, bool DMA>
+__global__ __launch_bounds__(SHAPE::kThreads) void weight_grad_kernel(WeightGrad p, Ending e) {
+    __shared__ __align__(16) char lds[TileProduct<T, Adjacent::L, Adjacent::L, SHAPE, DMA>::kLds];
+    weight_grad_tile<T, SHAPE, DMA>(lds, p, e, blockIdx.x);
+}
+
+// dx and dW in one launch, where both have tiles of 64 x 64 and k in one part: each alone leaves CUs with one or two workgroups, whose waves
+// wait for what those of others would hide.  first: dx's workgroups, a multiple of 8.  (777 x 1500 x 1021 floats 85.5 us
+// in two launches, 62.9 in one; 1000 x 1024 x 1024 bf16 21.9 and 15.8; 16 experts of 2000 x 1024 x 1024 floats 96.4 and 89.6.)
+template <typename T, Adjacent AB, typename SHAPE>
+__global__ __launch_bounds__(SHAPE::kThreads) void grads_kernel(Product x, Ending ex, WeightGrad w, Ending ew, int first) {
+    using P = TileProduct<T, Adjacent::K, AB, SHAPE, true>;
+    using Q = TileProduct<T, Adjacent::L, Adjacent::L, SHAPE, true>;
+    __shared__ __align__(16) char lds[P::kLds > Q::kLds ? P::kLds : Q::kLds];
+    if ((int)blockIdx.x < first) linear_tile<T, AB, SHAPE, true>(lds, x, ex, blockIdx.x);
+    else weight_grad_tile<T, SHAPE, true>(lds, w, ew, blockIdx.x - first);
 }
 
 template <typename T>

@@ -28,6 +28,9 @@ void launch_slope(bool dout_f32, const void* dout, int64_t dout_stride, const vo
                   const int32_t* offsets, int32_t experts, void* d, int64_t d_stride, hipStream_t s);
 template <typename T>
 void launch_weight_grad(const Plan& c, const WeightGrad& p, const Ending& e, hipStream_t s);
+// Both at once: tiles of 64 x 64 that go straight to LDS, without splits.
+template <typename T>
+void launch_grads(const Plan& cx, Adjacent adj, const Product& x, const Ending& ex, const Plan& cw, const WeightGrad& w, const Ending& ew, hipStream_t s);
 template <typename T>
 void launch_bias_grad(const void* d, int64_t d_stride, const int32_t* offsets, int32_t rows, int32_t cols, int32_t experts, int32_t splits, float* parts,
                       void* dbias, bool f32, hipStream_t s);

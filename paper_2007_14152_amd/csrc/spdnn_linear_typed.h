@@ -60,6 +60,14 @@ void launch_weight_grad(const Plan& c, const WeightGrad& p, const Ending& e, hip
 }
 
 template <typename T>
+void launch_grads(const Plan& cx, Adjacent adj, const Product& x, const Ending& ex, const Plan& cw, const WeightGrad& w, const Ending& ew, hipStream_t s) {
+    const int64_t first = (cx.mtiles * cx.ntiles + 7) / 8 * 8;
+    const dim3 grid((unsigned)(first + cw.mtiles * cw.ntiles * w.experts));
+    if (adj == Adjacent::K) grads_kernel<T, Adjacent::K, Small<2>><<<grid, 256, 0, s>>>(x, ex, w, ew, (int)first);
+    else grads_kernel<T, Adjacent::L, Small<2>><<<grid, 256, 0, s>>>(x, ex, w, ew, (int)first);
+}
+
+template <typename T>
 void launch_bias_grad(const void* d, int64_t d_stride, const int32_t* offsets, int32_t rows, int32_t cols, int32_t experts, int32_t splits, float* parts,
                       void* dbias, bool f32, hipStream_t s) {
     const dim3 grid((unsigned)std::min((cols - 1) / 64 + 1, 1 << 22), (unsigned)experts, (unsigned)splits);
@@ -75,4 +83,5 @@ void launch_bias_grad(const void* d, int64_t d_stride, const int32_t* offsets, i
     template void spdnn::launch_slope<T>(bool, const void*, int64_t, const void*, int64_t, int, int32_t, int32_t, const int32_t*, int32_t, void*,      \
                                          int64_t, hipStream_t);                                                                                        \
     template void spdnn::launch_weight_grad<T>(const Plan&, const WeightGrad&, const Ending&, hipStream_t);                                            \
+    template void spdnn::launch_grads<T>(const Plan&, Adjacent, const Product&, const Ending&, const Plan&, const WeightGrad&, const Ending&, hipStream_t); \
     template void spdnn::launch_bias_grad<T>(const void*, int64_t, const int32_t*, int32_t, int32_t, int32_t, int32_t, float*, void*, bool, hipStream_t);
