@@ -397,7 +397,8 @@ enum { SPDNN_ACT_NONE = 0, SPDNN_ACT_RELU = 1, SPDNN_ACT_CLIP = 2, SPDNN_ACT_GEL
  *               elements between experts' matrices.
  *   bias      : experts x cols numbers of bias_type (type or SPDNN_F32), or NULL.
  *   act       : SPDNN_ACT_NONE y, RELU max(y, 0), CLIP min(max(y, 0), 32), GELU y (1 + erf(y / sqrt 2)) / 2,
- *               SILU y / (1 + exp(-y)); a NaN stays one.  It is taken of the sum in 32 bits.
+ *               SILU y / (1 + exp(-y)); infinities have the limits (0 at -inf, slopes 0 and 1), a NaN stays
+ *               one.  It is taken of the sum in 32 bits.
  *   add       : a residual, or NULL.
  *   pre       : if not NULL, receives x[t] W + b (rounded to out_type), what spdnn_linear_grad starts from.
  * 1 <= experts <= SPDNN_MAX_EXPERTS, 1 <= width, cols <= 2^30; an out (or dW of all experts) of 2^24 tiles of 128 x 128 or more is

@@ -55,6 +55,8 @@ __device__ inline float act_tail(float a, float bell) {
 }
 // |x|, but 64 at the most, where bell and the tail are 0: an infinity has the limits, gelu 0 and x, slopes 0 and 1.  A NaN stays one.
 __device__ inline float act_size(float x) { return fabsf(x) > 64.0f ? 64.0f : fabsf(x); }
+// What a sigmoid is multiplied with: within the range where it is neither 0 nor 1 in 32 bits, so that infinities have their limits here too.
+__device__ inline float act_within(float x) { return x < -128.0f ? -128.0f : x > 128.0f ? 128.0f : x; }
 // A NaN stays one.
 template <bool EXACT>
 __device__ __forceinline__ float activated(float x, int act) {
@@ -65,7 +67,10 @@ __device__ __forceinline__ float activated(float x, int act) {
             const float a = act_size(x);
             return (x < 0.0f ? 0.0f : x) - a * act_tail<EXACT>(a, EXACT ? 0.0f : act_exp<EXACT>(-0.5f * a * a));
         }
-        case SPDNN_ACT_SILU: return EXACT ? x / (1.0f + expf(-x)) : x * __builtin_amdgcn_rcpf(1.0f + act_exp<EXACT>(-x));
+        case SPDNN_ACT_SILU: {
+            const float y = x < -128.0f ? -128.0f : x;
+            return EXACT ? y / (1.0f + expf(-y)) : y * __builtin_amdgcn_rcpf(1.0f + act_exp<EXACT>(-y));
+        }
     }
     return x;
 }
@@ -81,7 +86,7 @@ __device__ inline float act_slope(float x, int act) {
         }
         case SPDNN_ACT_SILU: {
             const float s = EXACT ? 1.0f / (1.0f + expf(-x)) : __builtin_amdgcn_rcpf(1.0f + act_exp<EXACT>(-x));
-            return s + x * s * (1.0f - s);
+            return s + act_within(x) * s * (1.0f - s);
         }
     }
     return 1.0f;

@@ -84,12 +84,26 @@ def test_the_slope_of_gelu_keeps_its_digits(sp, dtype, cols):
         ref.assert_within(got, want.numpy(), off.numpy(), dtype, "slope")
 
 
+# sigmoids: exp is off by 4 U, its argument by 2 U |x| (16 bits: a product and its factor); sum, quotient and products by 6 U.
+@pytest.mark.parametrize("dtype", ref.TYPES)
+def test_silu_keeps_its_digits(sp, dtype):
+    """x / (1 + exp(-x)) and its slope relative to their terms, down to where exp(x) leaves the normal numbers of 32 bits (and silu becomes 0)."""
+    x = arguments(dtype, -87.0, 87.0)
+    z = x.double()
+    s, o = torch.sigmoid(z), torch.sigmoid(-z)
+    rel = (2 * z.abs() + 10) * U
+    for got in activated(sp, x, "silu", 9):
+        ref.assert_within(got, (z * s).numpy(), ((z * s).abs() * rel).numpy(), dtype, "silu")
+    for got in slopes(sp, x, "silu", 9):
+        ref.assert_within(got, (s * (1 + z * o)).numpy(), (s * rel + 2 * (z * s * o).abs() * rel + 4 * U * s).numpy(), dtype, "slope")
+
+
 def ends(dtype):
     big = {F32: 1e38, BF16: 1e38, F16: 65504.0}[dtype]
     return torch.tensor([-INF, -big, -100.0, 100.0, big, INF, NAN], dtype=dtype)
 
 
-ENDS = ["gelu"]
+ENDS = ["gelu", "silu"]
 
 
 @pytest.mark.parametrize("act", ENDS)
@@ -110,5 +124,5 @@ def test_gradients_where_pre_leaves_16_bits(sp, act):
     x, w = torch.full((5, 300), -1.0, dtype=F16, device=DEV), torch.full((300, 24), 300.0, dtype=F16, device=DEV)
     out, pre = sp.linear(x, w, act=act, pre=True)
     assert not out.any() and bool((pre == -INF).all())
-    for g in sp.linear_grad(torch.ones_like(out), x, w, pre=pre, act=act):
-        assert not g.any()
+    for grad in sp.linear_grad(torch.ones_like(out), x, w, pre=pre, act=act):
+        assert not grad.any()
