@@ -415,7 +415,8 @@ int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64
  * dx[t] = d[t] W^T, of type; dW_e = sum over e's rows of x[t]^T d[t], stored as W is (transposed or not); db_e = sum over e's rows of
  * d[t].  Any of dx, dweight and dbias may be NULL: it is not computed then, and x (only dweight needs it) and weight (only
  * dx) are not read.
- *   dout_type : of dout and pre, type or SPDNN_F32.  d is rounded to type for the products, where it is not dout itself.
+ *   dout_type : of dout and pre, type or SPDNN_F32.  d is rounded to type for dx and dW, where it is not dout itself (so one beyond
+ *               65504 is infinite there with SPDNN_F16); db sums it as it is in 32 bits.
  *   grad_type : of dweight and dbias, type or SPDNN_F32.
  * dx is zero in the rows of no expert, dweight and dbias for experts without rows.  Slopes: RELU 0 up to 0, CLIP 0 up to 0 and from 32 on. */
 int spdnn_linear_grad_bytes(int32_t rows, int32_t width, int32_t cols, int32_t grouped, int32_t experts, int32_t type,

@@ -173,6 +173,8 @@ struct GradWork {
     int64_t d_stride;  // elements
     size_t d, bytes;
     int64_t bias_splits;
+    int64_t slope_rows;   // of a workgroup that adds up d's columns beside
+    int32_t slope_lanes;  // that have a row's columns, eight each
 };
 int grad_work(int32_t rows, int32_t width, int32_t cols, bool grouped, int32_t experts, int32_t type, int32_t dout_type, int32_t act, bool transposed,
               GradWork* w) {
@@ -187,6 +189,15 @@ int grad_work(int32_t rows, int32_t width, int32_t cols, bool grouped, int32_t e
         CHECK(check_tiles(p, experts));
         parts = std::max(parts, p.parts + (p.splits > 1 ? aligned((size_t)p.splits * experts * cols * sizeof(float)) : 0));
     }
+    // Chunks of rows: up to four workgroups a CU and 256 chunks, whose parts are added up; a row to eight for each team as long as CUs are idle, but
+    // no more than two experts' on average, which a chunk takes one after the other.
+    w->slope_lanes = 64;
+    while (w->slope_lanes > 1 && w->slope_lanes / 2 * 8 >= cols) w->slope_lanes /= 2;
+    const int64_t teams = 256 / w->slope_lanes, blocks = ceil_div(cols, w->slope_lanes * 8);
+    const int64_t least = std::min(std::max(teams, std::min(8 * teams, ceil_div(rows * blocks, 256))), std::max<int64_t>(1, 2 * ceil_div(rows, experts)));
+    w->slope_rows = std::max({least, ceil_div(rows * blocks, 1024), ceil_div(rows, 256)});
+    w->slope_rows = std::min<int64_t>(w->slope_rows, INT32_MAX);
+    if (w->own_d && type != SPDNN_F32) parts = std::max(parts, aligned((size_t)(ceil_div(rows, w->slope_rows) + experts) * cols * sizeof(float)));
     if (w->bias_splits > 1) parts = std::max(parts, aligned((size_t)w->bias_splits * experts * cols * sizeof(float)));
     w->bytes = w->d + parts;
     return SPDNN_OK;
@@ -294,10 +305,19 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
     float* const parts = (float*)((char*)work + w.d);
     const void* d = dout;
     int64_t d_stride = dout_stride;
+    // dbias of 16-bit rows is the sum of d as it is in 32 bits.
+    const bool sums = w.own_d && rows > 0 && dbias && type != SPDNN_F32;
+    void* const bias_left = sums ? nullptr : dbias;
+    if (sums) {
+        with_type(type, [&](auto tt) {
+            launch_slope_sums<decltype(tt)>(dout_type == SPDNN_F32, dout, dout_stride, act == SPDNN_ACT_NONE ? nullptr : pre, pre_stride, act, rows, cols, offsets, experts,
+                                            dx || dweight ? work : nullptr, w.d_stride, (int32_t)w.slope_rows, w.slope_lanes, parts, dbias, grad_type == SPDNN_F32, s);
+        });
+    }
     if (w.own_d && rows > 0) {
         d = work;
         d_stride = w.d_stride;
-        with_type(type, [&](auto tt) {
+        if (!sums) with_type(type, [&](auto tt) {
             launch_slope<decltype(tt)>(dout_type == SPDNN_F32, dout, dout_stride, act == SPDNN_ACT_NONE ? nullptr : pre, pre_stride, act, rows, cols, offsets, experts, work,
                                        d_stride, s);
         });
@@ -345,7 +365,7 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         p.ntiles = (int32_t)c.ntiles;
         p.splits = (int32_t)c.splits;
         p.bias_parts = (float*)((char*)parts + c.parts);
-        p.dbias = dbias;
+        p.dbias = bias_left;
         p.bias_f32 = grad_type == SPDNN_F32;
         p.d_is_a = transposed != 0;
         p.sorted = offsets && experts <= 64 && rows / experts >= 256;
@@ -366,9 +386,9 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         return launched();
     }
     run_x();
-    if (dbias) {
+    if (bias_left) {
         with_type(type, [&](auto tt) {
-            launch_bias_grad<decltype(tt)>(d, d_stride, offsets, rows, cols, experts, (int32_t)w.bias_splits, parts, dbias, grad_type == SPDNN_F32, s);
+            launch_bias_grad<decltype(tt)>(d, d_stride, offsets, rows, cols, experts, (int32_t)w.bias_splits, parts, bias_left, grad_type == SPDNN_F32, s);
         });
     }
     return launched();

@@ -1050,22 +1050,23 @@ __device__ __forceinline__ float sum_parts(const float* from, int64_t stride, in
     for (; s < splits; ++s) sum += from[s * stride];
     return sum;
 }
+// The last of `sets` experts that begins at the row or before, or the first.
+__device__ inline int set_of(const int32_t* offsets, int sets, int64_t row) {
+    int lo = 0, hi = sets;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (offsets[mid] <= row) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
 template <typename T>
 __global__ __launch_bounds__(256) void linear_join_kernel(Product p, Ending e) {
     const int64_t items = (int64_t)p.rows * p.cols;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / p.cols;
         const int col = (int)(i - row * p.cols);
-        int set = 0;
-        if (p.offsets) {  // the last expert that begins at the row or before
-            int lo = 0, hi = p.experts + 1;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (p.offsets[mid] <= row) lo = mid;
-                else hi = mid;
-            }
-            set = lo;
-        }
+        const int set = p.offsets ? set_of(p.offsets, p.experts + 1, row) : 0;
         const bool f32 = sizeof(T) == 4 || e.out_f32;
         if (set == p.experts) {
             for (char* to : {e.out, e.pre})
@@ -1117,21 +1118,6 @@ __global__ __launch_bounds__(256) void slope_kernel(const D* dout, int64_t dout_
     }
 }
 
-// dW[e] = sum over the rows of expert e of a[r] b[r]^T, a and b being x and d, or d and x where W is stored the other way round.  Sums
-// of long batches are split: parts [split][expert][line of a][line of b].
-struct WeightGrad {
-    Side a, b;
-    const int32_t* offsets;
-    int32_t rows, m, n, experts;
-    int32_t mtiles, ntiles, splits;
-    float* parts;
-    float* bias_parts;
-    void* dbias;  // null: not asked for here
-    bool bias_f32;
-    bool d_is_a;
-    bool sorted;  // long experts first
-};
-
 // Rows of expert `set` that split `split` adds.
 struct RowRange {
     int64_t first, last;
@@ -1148,6 +1134,116 @@ __device__ inline RowRange grad_rows(const int32_t* offsets, int32_t rows, int s
     first = min(first + per * split, last);
     return {first, min(first + per, last)};
 }
+
+// The same with dbias[e] = sum over the rows of expert e of d[r], taken of d before it is rounded: 16 bits a number are for the matrix
+// instructions, which dbias does not need.  A workgroup has `each` rows, of which teams of `lanes` lanes (a power of two, up to 64) take one after
+// the other, eight columns a lane; where an expert's rows end the teams are added in order.  Parts [chunk of rows + expert][column]: chunks and
+// experts that have rows in common go up together, so no two pairs meet in one.  d: null where only dbias is asked for.  Bound by memory:
+// 8000 x 16384 bf16, gelu, 162 us and 5 for the parts, beside which dW without these sums takes 121 instead of 145 (256 k); without d 117.
+template <typename T, typename D>
+__global__ __launch_bounds__(256) void slope_sums_kernel(const D* dout, int64_t dout_stride, const D* pre, int64_t pre_stride, int act, int32_t rows,
+                                                         int32_t cols, const int32_t* offsets, int32_t experts, T* d, int64_t d_stride, int32_t each,
+                                                         int32_t lanes, float* parts) {
+    constexpr int V = 8, AHEAD = 4;
+    __shared__ float lds[V][256];
+    const int teams = 256 / lanes, lane = threadIdx.x % lanes, team = threadIdx.x / lanes;
+    const int col0 = blockIdx.x * lanes * V, col = col0 + lane * V, here = min(V, cols - col);
+    const int64_t used = offsets ? min(max(offsets[experts], 0), rows) : rows;
+    const int64_t end = min((int64_t)(blockIdx.y + 1) * each, used);
+    int64_t first = (int64_t)blockIdx.y * each;
+    while (first < end) {
+        int set = 0;
+        int64_t last = end;
+        if (offsets) {
+            set = set_of(offsets, experts, first);
+            last = min(max((int64_t)offsets[set + 1], first + 1), end);
+        }
+        float sum[V] = {};
+        if (here == V) {
+            for (int64_t row = first + team; row < last; row += teams * AHEAD) {
+                Pack<D, V> x[AHEAD], z[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (row + teams * u >= last) continue;
+                    x[u] = load_vec<V>(dout + (row + teams * u) * dout_stride + col);
+                    if (pre) z[u] = load_vec<V>(pre + (row + teams * u) * pre_stride + col);
+                }
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (row + teams * u >= last) continue;
+                    float y[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        y[j] = (float)x[u][j];
+                        if (pre) y[j] *= act_slope<false>((float)z[u][j], act);
+                        sum[j] += y[j];
+                    }
+                    if (d) store_vec<V, T>(d + (row + teams * u) * d_stride + col, rounded_vec<T, V>(y), false);
+                }
+            }
+        } else {
+            for (int64_t row = first + team; row < last; row += teams)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    if (j >= here) continue;
+                    float y = (float)dout[row * dout_stride + col + j];
+                    if (pre) y *= act_slope<false>((float)pre[row * pre_stride + col + j], act);
+                    sum[j] += y;
+                    if (d) d[row * d_stride + col + j] = rounded<T>(y);
+                }
+        }
+        __syncthreads();  // what the last expert's sums left has been read
+#pragma unroll
+        for (int j = 0; j < V; ++j) lds[j][threadIdx.x] = sum[j];
+        __syncthreads();
+        const int64_t at = ((int64_t)blockIdx.y + set) * cols;
+        for (int c = threadIdx.x; c < min(lanes * V, cols - col0); c += 256) {
+            float all = 0;
+            for (int t = 0; t < teams; ++t) all += lds[c % V][t * lanes + c / V];
+            parts[at + col0 + c] = all;
+        }
+        first = last;
+    }
+}
+// The parts added up: a workgroup has 64 columns of an expert, its four waves every fourth part, added in order.
+template <typename T>
+__global__ __launch_bounds__(256) void slope_join_kernel(const float* parts, int32_t rows, int32_t cols, const int32_t* offsets, int32_t experts,
+                                                         int32_t each, void* dbias, bool f32) {
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int blocks = (cols - 1) / 64 + 1;
+    for (int64_t b = blockIdx.x; b < (int64_t)experts * blocks; b += gridDim.x) {
+        const int set = (int)(b / blocks), col = (int)(b - (int64_t)set * blocks) * 64 + lane;
+        const RowRange r = grad_rows<1>(offsets, rows, set, 0, 1);
+        const int chunk = (int)(r.first / each) + wave, chunks = r.last > r.first ? (int)((r.last - 1) / each) + 1 : 0;
+        float sum = 0;
+        if (col < cols && chunk < chunks) sum = sum_parts(parts + ((int64_t)chunk + set) * cols + col, 4 * (int64_t)cols, (chunks - chunk + 3) / 4);
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && col < cols) {
+            for (int w = 1; w < 4; ++w) sum += sums[w][lane];
+            const int64_t at = (int64_t)set * cols + col;
+            if (f32) ((float*)dbias)[at] = sum;
+            else ((T*)dbias)[at] = rounded<T>(sum);
+        }
+        __syncthreads();
+    }
+}
+
+// dW[e] = sum over the rows of expert e of a[r] b[r]^T, a and b being x and d, or d and x where W is stored the other way round.  Sums
+// of long batches are split: parts [split][expert][line of a][line of b].
+struct WeightGrad {
+    Side a, b;
+    const int32_t* offsets;
+    int32_t rows, m, n, experts;
+    int32_t mtiles, ntiles, splits;
+    float* parts;
+    float* bias_parts;
+    void* dbias;  // null: not asked for here
+    bool bias_f32;
+    bool d_is_a;
+    bool sorted;  // long experts first
+};
 
 // The expert with the `rank`-th largest number of rows: long tiles that begin last would leave the chip to themselves (dW of 12 experts:
 // 10007 x 1500 x 777 floats, dx and dW 437 us in order of experts, 422 so).  Up to 64 experts; more are many tiles anyway, and stay
@@ -1188,7 +1284,7 @@ __device__ __forceinline__ void weight_grad_tile(char* lds, const WeightGrad& p,
         const bool more = r.last < p.rows;
         product.template run<decltype(of)::value>(lds, a, p.a.line, alines, more || m0 + alines < p.m, b, p.b.line, blines, more || n0 + blines < p.n, r.last - r.first);
     };
-    // The sums of d's columns: the workgroups of the first tiles along W's other side multiply d with ones besides.  (A pass over d of its
+    // The sums of d's columns (where d is not rounded here, or of 32 bits): the workgroups of the first tiles along W's other side multiply d with ones besides.  (A pass over d of its
     // own took 225 us for 8000 x 16384 bf16, beside 920 for the product.)
     const auto put = [&](int col, int cols, float sum) {
         if (col >= cols) return;

@@ -44,6 +44,18 @@ void launch_slope(bool dout_f32, const void* dout, int64_t dout_stride, const vo
 }
 
 template <typename T>
+void launch_slope_sums(bool dout_f32, const void* dout, int64_t dout_stride, const void* pre, int64_t pre_stride, int act, int32_t rows, int32_t cols,
+                       const int32_t* offsets, int32_t experts, void* d, int64_t d_stride, int32_t each, int32_t lanes, float* parts, void* dbias, bool f32, hipStream_t s) {
+    const dim3 grid((unsigned)((cols - 1) / (lanes * 8) + 1), (unsigned)((rows - 1) / each + 1));
+    if (dout_f32)
+        slope_sums_kernel<T, float><<<grid, 256, 0, s>>>((const float*)dout, dout_stride, (const float*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)d, d_stride, each, lanes, parts);
+    else
+        slope_sums_kernel<T, T><<<grid, 256, 0, s>>>((const T*)dout, dout_stride, (const T*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)d, d_stride, each, lanes, parts);
+    const int64_t blocks = (int64_t)experts * ((cols - 1) / 64 + 1);
+    slope_join_kernel<T><<<(unsigned)std::min(blocks, kMostLoopGroups), 256, 0, s>>>(parts, rows, cols, offsets, experts, each, dbias, f32);
+}
+
+template <typename T>
 void launch_weight_grad(const Plan& c, const WeightGrad& p, const Ending& e, hipStream_t s) {
     const dim3 grid((unsigned)(c.mtiles * c.ntiles * p.experts * c.splits));
     if (c.bm == 256) weight_grad_kernel<T, Large, true><<<grid, 512, 0, s>>>(p, e);
@@ -82,6 +94,8 @@ void launch_bias_grad(const void* d, int64_t d_stride, const int32_t* offsets, i
     template void spdnn::launch_product<T>(const Plan&, Adjacent, const Product&, const Ending&, hipStream_t);                                         \
     template void spdnn::launch_slope<T>(bool, const void*, int64_t, const void*, int64_t, int, int32_t, int32_t, const int32_t*, int32_t, void*,      \
                                          int64_t, hipStream_t);                                                                                        \
+    template void spdnn::launch_slope_sums<T>(bool, const void*, int64_t, const void*, int64_t, int, int32_t, int32_t, const int32_t*, int32_t, void*, \
+                                              int64_t, int32_t, int32_t, float*, void*, bool, hipStream_t);                                            \
     template void spdnn::launch_weight_grad<T>(const Plan&, const WeightGrad&, const Ending&, hipStream_t);                                            \
     template void spdnn::launch_grads<T>(const Plan&, Adjacent, const Product&, const Ending&, const Plan&, const WeightGrad&, const Ending&, hipStream_t); \
     template void spdnn::launch_bias_grad<T>(const void*, int64_t, const int32_t*, int32_t, int32_t, int32_t, int32_t, float*, void*, bool, hipStream_t);

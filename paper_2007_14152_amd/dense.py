@@ -164,7 +164,8 @@ def linear_grad(dout, x, weight, pre=None, act=None, dtype=None, for_x=True, for
 
     dout: [rows, out] of x's type or float32; act as it was there, pre as linear gave it (of dout's type), needed with an act.  dx is
     of x's type; dweight and dbias are of dtype (x's, or float32), dweight is stored as weight is.  dout times the activation's slope
-    is rounded to x's type before the products.  What for_x, for_weight and for_bias leave out is None."""
+    is rounded to x's type for dx and dweight (in float16 what lies beyond 65504 is infinite there); dbias sums it in 32 bits.
+    What for_x, for_weight and for_bias leave out is None."""
     return _backward("linear_grad", dout, x, None, weight, pre, act, dtype, for_x, for_weight, for_bias)
 
 

@@ -126,3 +126,44 @@ def test_gradients_where_pre_leaves_16_bits(sp, act):
     assert not out.any() and bool((pre == -INF).all())
     for grad in sp.linear_grad(torch.ones_like(out), x, w, pre=pre, act=act):
         assert not grad.any()
+
+
+# one column to several workgroups of 512, one row to several chunks; experts that begin within a chunk, with one row and with none
+SUMS = [(1, 1, None), (3, 9, None), (17, 40, None), (1000, 513, None), (5000, 1100, None), (40, 24, [0, 1, 1, 2, 16, 17, 33, 40]), (700, 30, [0, 0, 700]),
+        (900, 520, [0, 100, 100, 101, 640, 880]), (2000, 16, list(range(0, 1001)) + [1999])]
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dtype,wide,act", [(BF16, False, "gelu"), (BF16, True, None), (F16, True, "silu"), (F16, False, "clip"), (F32, False, "gelu")])
+@pytest.mark.parametrize("rows,cols,at", SUMS, ids=lambda v: "-".join(map(str, v[:7])) if isinstance(v, list) else str(v))
+def test_dbias_is_a_sum_of_32_bits(sp, rows, cols, at, dtype, wide, act, transposed):
+    """dbias sums dout * act'(pre) as it is before it is rounded to 16 bits for the products."""
+    g = torch.Generator().manual_seed(rows + cols)
+    width, sets = 24, () if at is None else (len(at) - 1,)
+    kind = F32 if wide else dtype
+    x, dout, pre = torch.randn(rows, width, generator=g).to(dtype), torch.randn(rows, cols, generator=g).to(kind), (2 * torch.randn(rows, cols, generator=g)).to(kind)
+    w = torch.randn(sets + ((cols, width) if transposed else (width, cols)), generator=g).to(dtype)
+    d, z = dout.double(), pre.double()
+    s = ref.slope(z, act)
+    d, off = d * s, d.abs() * ref.slope_off(z, act) + U * (d * s).abs()
+    want, room = [], []
+    for a, b in [(0, rows)] if at is None else list(zip(at, at[1:])):
+        want.append(d[a:b].sum(0))
+        room.append(off[a:b].sum(0) + 2 * (b - a + 1) * U * (d[a:b].abs() + off[a:b]).sum(0))
+    if at is not None:
+        dout[at[-1]:], pre[at[-1]:] = NAN, NAN
+    want, room = torch.stack(want).view(sets + (cols,)), torch.stack(room).view(sets + (cols,))
+    w = w.to(DEV).transpose(-1, -2) if transposed else w.to(DEV)
+    args = (dout.to(DEV), x.to(DEV)) + (() if at is None else (torch.tensor(at, dtype=torch.int32, device=DEV),)) + (w,)
+    call = sp.linear_grad if at is None else sp.grouped_linear_grad
+    every = call(*args, pre=pre.to(DEV), act=act, dtype=F32)
+    ref.assert_within(every[2], want.numpy(), room.numpy(), F32, "dbias")
+    assert torch.equal(call(*args, pre=pre.to(DEV), act=act, dtype=F32, for_x=False, for_weight=False)[2], every[2]) or dtype == F32
+    ref.assert_within(call(*args, pre=pre.to(DEV), act=act, dtype=dtype, for_x=False)[2], want.numpy(), room.numpy(), dtype, "dbias of x's type")
+
+
+def test_dbias_of_numbers_beyond_16_bits(sp):
+    """A dout of floats that float16 does not hold."""
+    dout = torch.full((40, 16), 1e5, device=DEV)
+    db = sp.linear_grad(dout, torch.ones(40, 8, dtype=F16, device=DEV), torch.ones(8, 16, dtype=F16, device=DEV), dtype=F32, for_x=False, for_weight=False)[2]
+    assert torch.equal(db.cpu(), torch.full((16,), 4e6))
