@@ -22,6 +22,16 @@ int check_param(int32_t param_type, int32_t type) {
     return SPDNN_OK;
 }
 
+// Threads that take rows in turn: as many as the chip's 256 CUs hold.
+constexpr int64_t kNormThreads = 2048 * 256;
+// Workgroups that add columns, each of which leaves a part: two a CU.  60000 x 1024 bf16: 256 107 us, 512 98, 768 102, 1024 111, 2048 113.
+constexpr int64_t kParts = 512;
+// And where registers do not hold a row (the workgroups have 256 columns each).
+constexpr int64_t kLongParts = 16;
+// The most parts for any type: rows of more columns than this no type's registers hold.
+constexpr int32_t kHeldVecs = 4096, kHeldWidth = kHeldVecs * 8;
+int64_t most_parts(int32_t rows, int32_t width) { return std::min(static_cast<int64_t>(rows), width > kHeldWidth ? kLongParts : kParts); }
+
 // f(U, G, threads) for a row that registers hold: so many vectors a lane, lanes of a team and of a workgroup; false for longer ones.
 template <int V, typename F>
 bool with_row(int32_t width, F f) {
@@ -33,7 +43,7 @@ bool with_row(int32_t width, F f) {
     else if (vecs <= 512) SPDNN_ROW(2, 256, 256);
     else if (vecs <= 1024) SPDNN_ROW(4, 256, 256);
     else if (vecs <= 2048) SPDNN_ROW(2, 1024, 1024);
-    else if (vecs <= 4096) SPDNN_ROW(4, 1024, 1024);
+    else if (vecs <= kHeldVecs) SPDNN_ROW(4, 1024, 1024);
     else return false;
 #undef SPDNN_ROW
     return true;
@@ -47,12 +57,6 @@ bool with_row_of(int32_t width, F f) {
         else f(std::integral_constant<int, V>{}, std::false_type{}, u, g, threads);
     });
 }
-
-// Threads that take rows in turn: as many as the chip's 256 CUs hold.
-constexpr int64_t kNormThreads = 2048 * 256;
-// Workgroups that add columns, each of which leaves a part: two a CU.  60000 x 1024 bf16: 256 107 us, 512 98, 768 102, 1024 111, 2048 113.
-constexpr int64_t kParts = 512;
-int64_t parts_of(int32_t rows) { return std::min<int64_t>(rows, kParts); }
 
 }  // namespace
 
@@ -95,7 +99,7 @@ int spdnn_layer_norm_grad_bytes(int32_t rows, int32_t width, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
     if (rows < 0) return fail(SPDNN_EINVAL, "rows < 0");
     CHECK(check_width(width));
-    *bytes = ((size_t)parts_of(rows) * 2 * (size_t)width * sizeof(float) + kAlign - 1) / kAlign * kAlign;
+    *bytes = ((size_t)most_parts(rows, width) * 2 * (size_t)width * sizeof(float) + kAlign - 1) / kAlign * kAlign;
     return SPDNN_OK;
 }
 
@@ -119,7 +123,7 @@ int spdnn_layer_norm_grad(const void* dout, int32_t type, int64_t dout_stride, c
         CHECK(check_work(work, work_bytes, need));
     }
     const hipStream_t s = (hipStream_t)hip_stream;
-    const int64_t most = parts_of(rows);
+    const int64_t most = most_parts(rows, width);
     const NormGrad p{rows, width, (const float2*)stats, weight, param_type == SPDNN_F32, sums ? (float*)work : nullptr, (int64_t)rows * width * size_of(type) >= kPastBytes};
     with_type(type, [&](auto tt) {
         using T = decltype(tt);
@@ -133,7 +137,7 @@ int spdnn_layer_norm_grad(const void* dout, int32_t type, int64_t dout_stride, c
             if (!held) {
                 layer_norm_grad_long_kernel<T><<<dim3((unsigned)std::min<int64_t>(rows, kMostGroups)), 1024, 0, s>>>(p, (const T*)dout, dout_stride, (const T*)x, x_stride, (const T*)add, add_stride, (T*)dx, dx_stride);
                 if (sums) {
-                    parts = std::min<int64_t>(rows, 16);
+                    parts = std::min<int64_t>(rows, kLongParts);
                     layer_norm_columns_kernel<T><<<dim3((unsigned)std::min((width - 1) / 256 + 1, 65536), (unsigned)parts), 256, 0, s>>>(p, (const T*)dout, dout_stride, (const T*)x, x_stride);
                 }
             }

@@ -98,6 +98,17 @@ def test_work_memory():
         ask("spdnn_linear_grad_bytes", 100, (1 << 29) - 1, 1, 0, 1, type, type, 0, 1)  # (dx: 2^22 tiles of 128 x 128; 1000 rows are 2^25)
 
 
+def test_work_memory_of_long_rows():
+    """Rows that registers do not hold in any type leave 16 parts, whatever their number: no more memory than that is asked for."""
+    size = ctypes.c_size_t()
+    for rows, width in [(600, 1 << 20), (4096, 65536), (600, 40000), (9, 32769), (2 ** 31 - 1, 1 << 30)]:
+        assert sp.lib().spdnn_layer_norm_grad_bytes(rows, width, ctypes.byref(size)) == sp.SPDNN_OK
+        assert 0 <= size.value - min(rows, 16) * 2 * width * 4 < 256
+    for rows, width in [(600, 16385), (4096, 32768), (9, 32768)]:
+        assert sp.lib().spdnn_layer_norm_grad_bytes(rows, width, ctypes.byref(size)) == sp.SPDNN_OK
+        assert 0 <= size.value - min(rows, 512) * 2 * width * 4 < 256
+
+
 class Shape:
     """A tensor without memory that says that it lies on the GPU."""
 
