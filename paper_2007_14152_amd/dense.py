@@ -36,7 +36,7 @@ def _weight(t, x, sets):
     if cols > _MOST or sets and size[0] > _MOST:
         _fits("weight", *size)
     stride, step = t.stride()[-2:]
-    transposed = stride == 1 and (step != 1 or cols == 1)
+    transposed = (stride == 1 or width == 1) and (step != 1 or cols == 1)
     if transposed:
         line = step if cols > 1 else max(step, width)
     elif step == 1 or cols == 1:

@@ -212,3 +212,15 @@ def test_how_weights_are_stored():
     assert stored(S(8, 1), x)[0] is True  # a column: its rows are adjacent
     assert stored(S(1, 4), S(3, 1))[0] in (False, True)
     assert stored(Shape(like=torch.empty(8, 4, device="meta").expand(5, 8, 4)), x) == (False, 4, 0)
+
+
+def test_a_weight_of_one_row():
+    """One row has adjacent rows, whatever lies between its columns."""
+    x = S(3, 1)
+    one = Shape(like=torch.empty(6, 4, 5, device="meta")[:1, :, 2])
+    assert one.stride() == (20, 5)
+    assert dense._weight(one, x, False) == (1, 1, 4, True, 5, 0)
+    many = Shape(like=torch.empty(2, 6, 4, 5, device="meta")[:, :1, :, 2])
+    assert dense._weight(many, x, True) == (2, 1, 4, True, 5, 120)
+    assert dense._weight(S(1, 4), x, False) == (1, 1, 4, False, 4, 0)
+    assert dense._weight(Shape(like=torch.empty(1, 1, device="meta").expand(1, 4)), x, False)[3:5] == (True, 0)  # one number for all columns

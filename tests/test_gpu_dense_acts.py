@@ -167,3 +167,15 @@ def test_dbias_of_numbers_beyond_16_bits(sp):
     dout = torch.full((40, 16), 1e5, device=DEV)
     db = sp.linear_grad(dout, torch.ones(40, 8, dtype=F16, device=DEV), torch.ones(8, 16, dtype=F16, device=DEV), dtype=F32, for_x=False, for_weight=False)[2]
     assert torch.equal(db.cpu(), torch.full((16,), 4e6))
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+def test_weights_of_one_row(sp, dtype):
+    """A row whose columns lie apart, and one number for all columns."""
+    g = torch.Generator().manual_seed(1)
+    x, w = torch.randint(-3, 4, (70, 1), generator=g).to(dtype), torch.randint(-3, 4, (6, 130, 5), generator=g).to(dtype)
+    for weight in (w.to(DEV)[:1, :, 2], w.to(DEV)[:1, :1, 2].expand(1, 130)):
+        want = x.double() @ weight.cpu().double()
+        assert torch.equal(sp.linear(x.to(DEV), weight).cpu().double(), want)
+        dx, dw, db = sp.linear_grad(want.to(dtype).to(DEV), x.to(DEV), weight, dtype=F32)
+        assert torch.equal(dw.cpu().double(), x.double().t() @ want) and torch.equal(dx.cpu(), (want @ weight.cpu().double().t()).to(dtype))
