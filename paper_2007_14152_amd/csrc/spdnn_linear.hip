@@ -152,8 +152,10 @@ int most_parts(int32_t rows, int32_t k, int32_t cols, bool grouped, int32_t expe
     return SPDNN_OK;
 }
 
-// Whether an operand can go straight to LDS: tiles within reach of 32-bit offsets, and rows of k that do not overlap.
+// Whether an operand can go straight to LDS: tiles within reach of 32-bit offsets, rows of k that do not overlap.  And lines that are all one row
+// in memory have to end with a word: the range check leaves out half a word for every one of them, and only the last line's is stored.
 bool dma_side(const Side& s, Adjacent adj, int32_t along, int32_t type) {
+    if (adj == Adjacent::K && s.line == 0 && (int64_t)along * size_of(type) % 4 != 0) return false;
     return s.line <= kDmaSpan / 256 - 256 && (adj == Adjacent::K || s.line >= (int64_t)along * size_of(type));
 }
 
