@@ -20,7 +20,7 @@ HEADERS = [os.path.join(CSRC, "spdnn_kernels.h"), os.path.join(CSRC, "spdnn_orde
            os.path.join(CSRC, "spdnn_profile.h"),
            os.path.join(CSRC, "spdnn_error.h"), os.path.join(CSRC, "spdnn_rows_kernels.h"),
            os.path.join(CSRC, "spdnn_check.h"), os.path.join(CSRC, "spdnn_vec.h"), os.path.join(CSRC, "spdnn_linear_kernels.h"),
-           os.path.join(CSRC, "spdnn_linear_launch.h"), os.path.join(CSRC, "spdnn_linear_typed.h"), os.path.join(CSRC, "spdnn_norm_kernels.h"),
+           os.path.join(CSRC, "spdnn_linear_plan.h"), os.path.join(CSRC, "spdnn_linear_launch.h"), os.path.join(CSRC, "spdnn_linear_typed.h"), os.path.join(CSRC, "spdnn_norm_kernels.h"),
            os.path.join(os.path.dirname(_HERE), "include", "spdnn.h")]
 # host build of the connection-ordering routine, for tests of the set-up logic without a GPU
 ORDER_HOST_LIB = os.path.join(CSRC, "libspdnn_order_host.so")

@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "../../include/spdnn.h"
+#include "spdnn_linear_plan.h"
 #include "spdnn_vec.h"
 
 #pragma clang fp contract(off)
@@ -101,7 +102,6 @@ __device__ inline float act_slope(float x, int act) {
 //                 operands of a gradient of W)              block ^ f(k)
 // so that the lanes that read a fragment together meet all banks.  The second form is turned round on the way to registers: for 16
 // bits by the transposing LDS read (16 lanes give 4 rows of 16 numbers, lane i gets column i), floats are read one by one.
-enum class Adjacent { K, L };
 
 struct Side {
     const char* p;

@@ -2,23 +2,12 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cstdint>
 
 #include "spdnn_linear_kernels.h"
+#include "spdnn_linear_plan.h"
 
 namespace spdnn {
-
-// How a product is cut: into tiles of bm x bn, and of k (a multiple of a step each).
-struct Plan {
-    bool dma;      // operands go straight to LDS
-    int few;       // linear_short_kernel: fragments of rows in a tile (1, 2 or 4); 0: linear_kernel
-    bool narrow;   // and whether its tiles have 16 columns instead of 64
-    int bm, bn;
-    bool alone;    // no CU has two workgroups
-    int64_t mtiles, ntiles, splits, per_split;
-    size_t parts;  // bytes
-};
 
 template <typename T>
 void launch_product(const Plan& c, Adjacent adj, const Product& p, const Ending& e, hipStream_t s);

@@ -1,8 +1,9 @@
 // Host build of the connection-ordering routine (spdnn_order.h), of the tile
-// layout functions (spdnn_layout.h) and of other host logic (spdnn_cut.h, spdnn_profile.h), so that
+// layout functions (spdnn_layout.h) and of other host logic (spdnn_cut.h, spdnn_profile.h, spdnn_linear_plan.h), so that
 // it can be tested without a GPU.  Not used by the inference path.
 #include "spdnn_cut.h"
 #include "spdnn_layout.h"
+#include "spdnn_linear_plan.h"
 #include "spdnn_order.h"
 #include "spdnn_profile.h"
 
@@ -120,5 +121,17 @@ void spdnn_take_host_counts_host(const int32_t* runs, int n, const int* host_cou
 }
 uint32_t spdnn_res_code_host(uint32_t slot, int planes_log2) { return spdnn::res_code(slot, planes_log2); }
 uint32_t spdnn_res_slot_host(uint32_t code, int planes_log2) { return spdnn::res_slot(code, planes_log2); }
+
+// How a dense product is cut (spdnn_linear_plan.h): {few, narrow, bm, bn, alone, splits, mtiles, ntiles}.  grad: of W, m x n from `rows` rows.
+static void put_plan(const spdnn::Plan& p, int64_t* out) {
+    const int64_t all[8] = {p.few, p.narrow, p.bm, p.bn, p.alone, p.splits, p.mtiles, p.ntiles};
+    std::copy(all, all + 8, out);
+}
+void spdnn_linear_plan_host(int rows, int k, int cols, int grouped, int experts, int type, int dma, int k_adjacent, int64_t* out) {
+    put_plan(spdnn::plan_product(rows, k, cols, grouped, experts, type, dma, k_adjacent ? spdnn::Adjacent::K : spdnn::Adjacent::L), out);
+}
+void spdnn_weight_grad_plan_host(int rows, int m, int n, int experts, int type, int dma, int64_t* out) {
+    put_plan(spdnn::plan_grad(rows, m, n, experts, type, dma), out);
+}
 
 }  // extern "C"

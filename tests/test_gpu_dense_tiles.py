@@ -1,0 +1,168 @@
+"""Every kernel and tile of the dense products (dense_plans.py) against products in 64 bits: small whole numbers, whose sums are exact, and
+activations and a residual behind them."""
+import pytest
+import torch
+
+import dense_plans as plans
+import dense_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, F16 = ref.TYPES
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def sp():
+    import paper_2007_14152_amd as package
+    return package
+
+
+@pytest.fixture(autouse=True)
+def say(request):
+    print(request.node.name, flush=True)
+
+
+def whole(g, shape, dtype, most=2):
+    return torch.randint(-most, most + 1, shape, generator=g, device=DEV).to(dtype)
+
+
+def seeded(n):
+    return torch.Generator(DEV).manual_seed(n)
+
+
+def stored(w, transposed):
+    return w.transpose(-1, -2).contiguous().transpose(-1, -2) if transposed else w
+
+
+def equal(got, want, what):
+    want = want.to(got.dtype)
+    assert got.shape == want.shape and torch.equal(got, want), (what, int((got != want).sum()), (got != want).nonzero()[:4].tolist())
+
+
+def near(got, want, off, what):
+    """On the GPU what ref.assert_within does."""
+    room = off * (1 + ref.OUT_U[got.dtype]) + ref.OUT_U[got.dtype] * want.abs() + ref.SMALLEST[got.dtype]
+    bad = ~((got.double() - want).abs() <= room)
+    assert not bool(bad.any()), (what, int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+def batches(loads):
+    at = [0]
+    for n in loads:
+        at.append(at[-1] + n)
+    return at
+
+
+def product(x, w, at):
+    """x W in 64 bits; at: where experts begin, or None."""
+    if at is None:
+        return x.double() @ w.double()
+    out = torch.zeros(x.shape[0], w.shape[-1], dtype=torch.float64, device=DEV)
+    for e, (a, b) in enumerate(zip(at, at[1:])):
+        out[a:b] = x[a:b].double() @ w[e].double()
+    return out
+
+
+def spread(bias, at, rows):
+    """Every row's bias; 0 behind the last expert."""
+    if at is None:
+        return bias.double().expand(rows, -1)
+    out = torch.zeros(rows, bias.shape[-1], dtype=torch.float64, device=DEV)
+    for e, (a, b) in enumerate(zip(at, at[1:])):
+        out[a:b] = bias[e].double()
+    return out
+
+
+def check_product(sp, rows, k, cols, at, dtype, transposed):
+    g = seeded(rows + k + cols)
+    sets, used = (() if at is None else (len(at) - 1,)), rows if at is None else at[-1]
+    x, w, add = whole(g, (rows, k), dtype), whole(g, sets + (k, cols), dtype), whole(g, (rows, cols), dtype, 9)
+    bias = whole(g, sets + (cols,), dtype, 9)
+    z = product(x, w, at)
+    inside = torch.ones(rows, 1, dtype=torch.float64, device=DEV)
+    inside[used:] = 0
+    x[used:], add[used:] = NAN, NAN
+    wd = stored(w, transposed)
+    off = None if at is None else torch.tensor(at, dtype=torch.int32, device=DEV)
+
+    def call(**more):
+        return sp.linear(x, wd, **more) if at is None else sp.grouped_linear(x, off, wd, **more)
+
+    equal(call(dtype=F32), z, "plain, to 32 bits")
+    y = z + spread(bias, at, rows)
+    rest = torch.where(inside > 0, add.double(), 0.0)
+    got, pre = call(bias=bias, act="clip", add=add, pre=True)
+    equal(pre, y, "pre")
+    equal(got, (y.clamp(0, 32) + rest) * inside, "clip and a residual")
+    equal(call(bias=bias.float(), act="relu"), y.clamp(min=0), "relu")
+    # gelu and silu of numbers about 1: sums times a power of two are exact too
+    scale = 2.0 ** -round(torch.tensor(2.0 * k ** 0.5).log2().item())
+    x.mul_(scale)
+    for act in ("gelu", "silu"):
+        out = call(act=act, add=add)
+        want = ref.act(z * scale, act)
+        near(out, (want + rest) * inside, (ref.act_off(z * scale, act) + ref.U * (want + rest).abs()) * inside, act)
+
+
+def check_grads(sp, rows, width, cols, at, dtype, transposed):
+    """dW and db, alone and beside dx."""
+    g = seeded(rows + width + cols)
+    sets, used = (() if at is None else (len(at) - 1,)), rows if at is None else at[-1]
+    x, w, dout = whole(g, (rows, width), dtype), whole(g, sets + (width, cols), dtype), whole(g, (rows, cols), dtype)
+    want_dx = product(dout, w.transpose(-1, -2), at)
+    dw, db = torch.zeros(sets + (width, cols), dtype=torch.float64, device=DEV), torch.zeros(sets + (cols,), dtype=torch.float64, device=DEV)
+    for e, (a, b) in enumerate([(0, rows)] if at is None else zip(at, at[1:])):
+        here = Ellipsis if at is None else e
+        dw[here] = x[a:b].double().t().contiguous() @ dout[a:b].double()
+        db[here] = dout[a:b].double().sum(0)
+    x[used:], dout[used:] = NAN, NAN
+    wd = stored(w, transposed)
+    off = None if at is None else torch.tensor(at, dtype=torch.int32, device=DEV)
+
+    def call(**more):
+        return sp.linear_grad(dout, x, wd, dtype=F32, **more) if at is None else sp.grouped_linear_grad(dout, x, off, wd, dtype=F32, **more)
+
+    for what, got, want in zip(("dx", "dweight", "dbias"), call(), (want_dx, dw, db)):
+        equal(got, want, what)
+    equal(call(for_x=False, for_bias=False)[1], dw, "dweight alone")
+    equal(call(for_weight=False, for_bias=False)[0], want_dx, "dx alone")
+    equal(call(for_x=False, for_weight=False)[2], db, "dbias alone")
+
+
+KINDS = [(dtype, transposed) for dtype in ref.TYPES for transposed in (False, True)]
+
+
+def cases(of_16, of_32):
+    return [pytest.param(dtype, transposed, *case[1:], id="%s-%s-%s-%d" % (case[0], str(dtype)[6:], "t" if transposed else "n", i))
+            for dtype, transposed in KINDS for i, case in enumerate(of_32 if dtype == F32 else of_16)]
+
+
+NO_NAME = [("few",) + c for c in plans.FEW]
+NO_NAME_GROUPED = [("few",) + c for c in plans.FEW_GROUPED]
+
+
+@pytest.mark.parametrize("dtype,transposed,rows,k,cols", cases(plans.PRODUCTS_16 + NO_NAME, plans.PRODUCTS_32 + NO_NAME))
+def test_products(sp, dtype, transposed, rows, k, cols):
+    check_product(sp, rows, k, cols, None, dtype, transposed)
+
+
+@pytest.mark.parametrize("dtype,transposed,loads,dropped,k,cols", cases(plans.GROUPED_16 + NO_NAME_GROUPED, plans.GROUPED_32 + NO_NAME_GROUPED))
+def test_grouped_products(sp, dtype, transposed, loads, dropped, k, cols):
+    check_product(sp, sum(loads) + dropped, k, cols, batches(loads), dtype, transposed)
+
+
+@pytest.mark.parametrize("dtype,transposed,rows,width,cols", cases(plans.GRADS_16, plans.GRADS_32))
+def test_gradients(sp, dtype, transposed, rows, width, cols):
+    check_grads(sp, rows, width, cols, None, dtype, transposed)
+
+
+@pytest.mark.parametrize("dtype,transposed,loads,dropped,width,cols", cases(plans.GROUPED_GRADS_16, plans.GROUPED_GRADS_32))
+def test_grouped_gradients(sp, dtype, transposed, loads, dropped, width, cols):
+    check_grads(sp, sum(loads) + dropped, width, cols, batches(loads), dtype, transposed)
+
+
+@pytest.mark.parametrize("dtype,transposed,loads,dropped,cols,width", cases([c for c in plans.GROUPED_16 if "/s" not in c[0]], plans.GROUPED_32[-1:]))
+def test_dx_in_the_tiles_of_grouped_products(sp, dtype, transposed, loads, dropped, cols, width):
+    """The forward sizes as gradients: dx = d W^T with as many rows, columns and k."""
+    check_grads(sp, sum(loads) + dropped, width, cols, batches(loads), dtype, transposed)
