@@ -480,9 +480,10 @@ struct RowTiles {
         const int lane = threadIdx.x % 64;
 #pragma unroll 4
         for (int i = 0; i < each; ++i) own += expert_tiles(lane * each + i);
+        own = min(own, others);  // (of wrong offsets more, whose sums would pass 32 bits)
         const int until = upto(own);
         first = until - own;
-        all = min(max(__builtin_amdgcn_readlane(until, 63), 0), others);  // (of wrong offsets more)
+        all = min(__builtin_amdgcn_readlane(until, 63), others);
     }
     // Tile t of all * ntiles, and its columns'.  Bands of eight tiles of rows, so that an XCD's workgroups share W's columns and x's
     // rows in its L2; EACH: bands that end with an expert's rows, so that they share one W (48000 rows of 64 experts, 4096 x 4096 bf16: 1684
