@@ -401,9 +401,10 @@ enum { SPDNN_ACT_NONE = 0, SPDNN_ACT_RELU = 1, SPDNN_ACT_CLIP = 2, SPDNN_ACT_GEL
  *               one.  It is taken of the sum in 32 bits.
  *   add       : a residual, or NULL.
  *   pre       : if not NULL, receives x[t] W + b (rounded to out_type), what spdnn_linear_grad starts from.
- * 1 <= experts <= SPDNN_MAX_EXPERTS, 1 <= width, cols <= 2^30; an out (or dW of all experts) of 2^24 tiles of 128 x 128 or more is
- * refused, which only very few rows or columns reach before memory ends.  work: device memory, 256-byte aligned, >= spdnn_linear_bytes
- * (grouped: whether offsets are given); contents scratch. */
+ * 1 <= experts <= SPDNN_MAX_EXPERTS, 1 <= width, cols <= 2^30.  An out (or dx, or dW of all experts) of 2^24 tiles of 128 x 128 or more is
+ * refused; grouped rows count as rows / 128 + experts + 1 tiles, but no more than one a row.  Only very few rows or columns, or very many columns
+ * for experts of few rows, reach that before memory ends.  work: device memory, 256-byte aligned, >= spdnn_linear_bytes (grouped: whether offsets
+ * are given); contents scratch. */
 int spdnn_linear_bytes(int32_t rows, int32_t width, int32_t cols, int32_t grouped, int32_t experts, int32_t type, size_t* bytes);
 int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64_t x_stride, const int32_t* offsets,
                  int32_t experts, const void* weight, int32_t transposed, int64_t weight_stride, int64_t expert_stride,

@@ -53,15 +53,18 @@ inline double cost(int b, int64_t n, double k, double longest, int32_t type) {
 // The tile and the number of parts of k with which `tiles(b)` tiles take least.  Parts are written and read once more, out_bytes a part,
 // which a join does in 9 us and at 4 TB/s.  uneven: how many times the k of all on average the longest tile may have.  (777 x 1500 x 1021 floats: 110 us
 // with tiles of 128, 40 with tiles of 64.  dW of 12 experts of 10007 rows in all, 1500 x 777 floats: 532 us with tiles of 128.)
-template <typename F>
-inline void choose(F tiles, int64_t steps, double uneven, size_t out_bytes, int32_t type, bool dma, int* b, int64_t* splits) {
+// launched: workgroups of a part, which are no fewer (all of them take part in the limit of a launch).
+template <typename F, typename G>
+inline void choose(F tiles, G launched, int64_t steps, double uneven, size_t out_bytes, int32_t type, bool dma, int* b, int64_t* splits) {
     const double k = (double)steps * step_of(type);
     double best = 1e300;
+    *b = 128;  // (too many for every tile: refused)
+    *splits = 1;
     for (const int tile : {256, 128, 64}) {
         if (!dma && tile != 128) continue;
         for (int64_t s = 1; s <= 64; s *= 2) {
             if (s > 1 && (steps / s < 4 || s * out_bytes > kMostParts)) break;
-            if (best < 1e300 && tiles(tile) * s > most_tiles(tile)) break;
+            if (launched(tile) * s > most_tiles(tile)) break;
             const double us = cost(tile, tiles(tile) * s, k / s, uneven * k / s, type) + (s > 1 ? 9.0 + 2.0 * s * out_bytes / 4e6 : 0.0);
             if (us < best) {
                 best = us;
@@ -78,9 +81,10 @@ inline Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, in
     const int64_t sets = grouped ? std::max<int64_t>(1, std::min(experts, rows)) : 1;
     const int64_t steps = ceil_div(k, step_of(type));
     const auto tiles = [&](int bm, int bn) { return (grouped ? rows / bm + sets : ceil_div(rows, bm)) * ceil_div(cols, bn); };  // that have rows
+    const auto mtiles = [&](int bm) { return grouped ? std::min<int64_t>(rows, rows / bm + experts + 1) : ceil_div(rows, bm); };
     const int64_t each = ceil_div(rows, sets);
     // (Few rows: W's bytes are what counts.  In 32 bits the matrix instructions do, from 32 rows on.)
-    if (dma && each <= (type == SPDNN_F32 ? 32 : grouped ? 48 : 128) && tiles(16, 64) <= most_tiles(0)) {
+    if (dma && each <= (type == SPDNN_F32 ? 32 : grouped ? 48 : 128) && mtiles(16) * ceil_div(cols, 64) <= most_tiles(0)) {
         p.few = each <= (grouped ? 8 : 16) ? 1 : each <= (grouped ? 20 : 32) ? 2 : 4;
         p.bm = 16 * p.few;
         // Tiles of 16 columns where those of 64 leave CUs idle; but columns of adjacent k, or k that are not many: 32 bytes of a row of
@@ -90,10 +94,10 @@ inline Plan plan_product(int32_t rows, int32_t k, int32_t cols, bool grouped, in
         p.bn = p.narrow ? 16 : 64;
         p.splits = std::max<int64_t>(1, std::min(kGroupsWanted / std::max<int64_t>(tiles(p.bm, p.bn), 1), steps / 32));
     } else {
-        choose([&](int b) { return tiles(b, b); }, steps, 1.0, (size_t)rows * cols * sizeof(float), type, dma, &p.bm, &p.splits);
+        choose([&](int b) { return tiles(b, b); }, [&](int b) { return mtiles(b) * ceil_div(cols, b); }, steps, 1.0, (size_t)rows * cols * sizeof(float), type, dma, &p.bm, &p.splits);
         p.bn = p.bm;
     }
-    p.mtiles = grouped ? std::min<int64_t>(rows, rows / p.bm + experts + 1) : ceil_div(rows, p.bm);
+    p.mtiles = mtiles(p.bm);
     p.ntiles = ceil_div(cols, p.bn);
     p.per_split = ceil_div(steps, p.splits) * step_of(type);
     p.splits = ceil_div(k, p.per_split);
@@ -106,7 +110,7 @@ inline Plan plan_grad(int32_t rows, int32_t m, int32_t n, int32_t experts, int32
     p.dma = dma;
     const auto tiles = [&](int b) { return ceil_div(m, b) * ceil_div(n, b) * experts; };
     const int64_t steps = std::max<int64_t>(1, ceil_div(ceil_div(rows, experts), step_of(type)));
-    choose(tiles, steps, experts > 1 ? 3.0 : 1.0, (size_t)experts * m * n * sizeof(float), type, dma, &p.bm, &p.splits);
+    choose(tiles, tiles, steps, experts > 1 ? 3.0 : 1.0, (size_t)experts * m * n * sizeof(float), type, dma, &p.bm, &p.splits);
     p.bn = p.bm;
     p.mtiles = ceil_div(m, p.bm);
     p.ntiles = ceil_div(n, p.bn);

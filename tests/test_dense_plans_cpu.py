@@ -1,8 +1,12 @@
 """The sizes that the GPU tests of the dense products run come to every kernel and tile there is, so that no change of the rule that chooses
 them leaves one without a test."""
+import ctypes
+import random
+
 import pytest
 
 import dense_plans as plans
+import paper_2007_14152_amd as sp
 
 TILES_16 = {"64.2", "64.3", "128.2", "128.3", "256"}
 TILES_32 = {"64.2", "128.2", "256"}
@@ -44,3 +48,25 @@ def test_few_rows(float32, k_adjacent):
     assert {"few%d%s" % (r, n) for r in (1, 2, 4) for n in ("", "n", "n/s")} <= grouped
     # (one matrix of floats takes tiles of 64 from 33 rows on; 64 columns and k in parts go together only where columns are adjacent)
     assert {"few%d%s" % (r, n) for r in ((1, 2) if float32 else (1, 2, 4)) for n in ("", "n", "n/s" if k_adjacent else "/s")} <= one
+
+
+def most(rng, log2):
+    return min(int(2 ** rng.uniform(0, log2)) + rng.randint(0, 2), 2 ** log2 - (log2 == 31))
+
+
+def test_what_is_too_large_is_what_the_header_says():
+    """2^24 tiles of 128 x 128 are refused, fewer are not, whatever tiles the sizes come to."""
+    rng, size, refused = random.Random(5), ctypes.c_size_t(), 0
+    cases = [(1024, 8, n, 1024) for n in ((1 << 21) - 128, (1 << 21) - 127, 1 << 21)] + [(r, 8, 1 << 20, 1024) for r in (900, 2047, 2048, 40000, 131072 * 8)]
+    while len(cases) < 4000:
+        case = most(rng, 31), most(rng, 30), most(rng, 30), rng.choice([None, 1, 2, 7, 64, 1000, 1024])
+        if case[0] * case[2] < 2 ** 45 and case[1] * case[2] * (case[3] or 1) < 2 ** 45:
+            cases.append(case)
+    for rows, k, cols, experts in cases:
+        lines = (rows + 127) // 128 if experts is None else min(rows, rows // 128 + experts + 1)
+        tiles = lines * ((cols + 127) // 128)
+        for type in (0, 1):
+            got = sp.lib().spdnn_linear_bytes(rows, k, cols, experts is not None, experts or 1, type, ctypes.byref(size))
+            assert (got != sp.SPDNN_OK) == (tiles >= 2 ** 24), (rows, k, cols, experts, type, tiles)
+            refused += got != sp.SPDNN_OK
+    assert 50 < refused < 7000

@@ -166,3 +166,17 @@ def test_grouped_gradients(sp, dtype, transposed, loads, dropped, width, cols):
 def test_dx_in_the_tiles_of_grouped_products(sp, dtype, transposed, loads, dropped, cols, width):
     """The forward sizes as gradients: dx = d W^T with as many rows, columns and k."""
     check_grads(sp, sum(loads) + dropped, width, cols, batches(loads), dtype, transposed)
+
+
+def test_about_as_many_tiles_as_a_launch_takes(sp):
+    """An expert for every row, and nearly 2^24 tiles of 128 x 128."""
+    n, cols = 1024, (1 << 21) - 128
+    x = (torch.arange(n, device=DEV) % 5 - 2).to(BF16).view(n, 1)
+    w = (torch.arange(cols, device=DEV) % 7 - 3).to(BF16).view(1, 1, cols).expand(n, 1, cols)
+    at = torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    out = sp.grouped_linear(x, at, w)
+    assert torch.equal(out, x * w[0])
+    at[1:] += 1  # two rows for the first expert, none for the last but one
+    at.clamp_(max=n)
+    out = sp.grouped_linear(x, at, w, act="relu")
+    assert torch.equal(out, (x * w[0]).clamp_(min=0))
