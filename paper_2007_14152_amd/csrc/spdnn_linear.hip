@@ -41,9 +41,8 @@ int check_matrix(const char* what, const void* p, int32_t type, int32_t width, i
     }
     return SPDNN_OK;
 }
-int check_output(const char* what, const void* p, int32_t out_type, int32_t type) {
+int check_output(const char* what, int32_t out_type, int32_t type) {
     if (out_type != type && out_type != SPDNN_F32) return fail(SPDNN_EINVAL, "%s is of x's type or SPDNN_F32", what);
-    (void)p;
     return SPDNN_OK;
 }
 
@@ -141,12 +140,12 @@ int spdnn_linear(const void* x, int32_t type, int32_t rows, int32_t width, int64
     CHECK(check_act(act));
     CHECK(check_rows("x", x, type, rows, width, x_stride, kRead));
     CHECK(check_matrix("weight", weight, type, width, cols, transposed, weight_stride, experts, expert_stride, kRead));
-    CHECK(check_output("out", out, out_type, type));
+    CHECK(check_output("out", out_type, type));
     CHECK(check_rows("out", out, out_type, rows, cols, out_stride, kWritten));
     if (pre) CHECK(check_rows("pre", pre, out_type, rows, cols, pre_stride, kWritten));
     if (add) CHECK(check_rows("add", add, out_type, rows, cols, add_stride, kRead));
     if (bias) {
-        CHECK(check_output("bias", bias, bias_type, type));
+        CHECK(check_output("bias", bias_type, type));
         CHECK(check_array("bias", bias, 0, size_of(bias_type)));
     }
     CHECK(check_work(work, work_bytes, need));
@@ -183,7 +182,7 @@ int spdnn_linear_grad_bytes(int32_t rows, int32_t width, int32_t cols, int32_t g
                             int32_t transposed, size_t* bytes) {
     if (!bytes) return fail(SPDNN_EINVAL, "bytes is NULL");
     CHECK(check_sizes(rows, width, cols, experts, type));
-    CHECK(check_output("dout", nullptr, dout_type, type));
+    CHECK(check_output("dout", dout_type, type));
     CHECK(check_act(act));
     GradWork w;
     CHECK(grad_work(rows, width, cols, grouped != 0, experts, type, dout_type, act, transposed != 0, &w));
@@ -208,7 +207,7 @@ int spdnn_linear_grad(const void* dout, int32_t dout_type, int64_t dout_stride, 
         CHECK(check_rows("x", x, type, rows, width, x_stride, kRead));
         CHECK(check_matrix("dweight", dweight, grad_type, width, cols, transposed, dweight_stride, experts, dexpert_stride, kWritten));
     }
-    if (dweight || dbias) CHECK(check_output("dweight, dbias", nullptr, grad_type, type));
+    if (dweight || dbias) CHECK(check_output("dweight, dbias", grad_type, type));
     if (dbias) CHECK(check_array("dbias", dbias, 0, size_of(grad_type)));
     CHECK(check_work(work, work_bytes, need));
     const hipStream_t s = (hipStream_t)hip_stream;

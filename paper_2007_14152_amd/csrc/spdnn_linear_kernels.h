@@ -600,7 +600,7 @@ struct TileProduct {
         for (int m = 1; m < kPart; ++m) own |= __builtin_bit_cast(Bits, a[m]) & (wn == m ? -1 : 0);
         sums[PART] = mma(ones, __builtin_bit_cast(Frag<T>, own), sums[PART]);
     }
-    template <int PART, int OF>
+    template <int PART>
     __device__ __forceinline__ void multiply_line(int m, const Frag<T>& a, const Frag<T> (&b)[NF]) {
 #pragma unroll
         for (int n = 0; n < NF; ++n) acc[PART * kPart + m][n] = mma(b[n], a, acc[PART * kPart + m][n]);
@@ -726,7 +726,7 @@ struct TileProduct {
 #pragma unroll
                         for (int n = m * NF / kPart; n < (m + 1) * NF / kPart; ++n) fb[0][n] = B::read(now + A::kBytes, (wn * NF + n) * 16, 0, lane);
                         fa[0][m] = A::read(now, (wm * MF + m) * 16, 0, lane);
-                        multiply_line<1, OF>(m, fa[1][m], fb[1]);
+                        multiply_line<1>(m, fa[1][m], fb[1]);
                     }
 #pragma unroll
                     for (int c = m * kLoads / kPart; c < (m + 1) * kLoads / kPart; ++c) {
