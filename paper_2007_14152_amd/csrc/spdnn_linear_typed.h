@@ -47,10 +47,12 @@ template <typename T>
 void launch_slope_sums(bool dout_f32, const void* dout, int64_t dout_stride, const void* pre, int64_t pre_stride, int act, int32_t rows, int32_t cols,
                        const int32_t* offsets, int32_t experts, void* d, int64_t d_stride, int32_t each, int32_t lanes, float* parts, void* dbias, bool f32, hipStream_t s) {
     const dim3 grid((unsigned)((cols - 1) / (lanes * 8) + 1), (unsigned)((rows - 1) / each + 1));
+    if (!offsets && grid.y == 1) parts = nullptr;
     if (dout_f32)
-        slope_sums_kernel<T, float><<<grid, 256, 0, s>>>((const float*)dout, dout_stride, (const float*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)d, d_stride, each, lanes, parts);
+        slope_sums_kernel<T, float><<<grid, 256, 0, s>>>((const float*)dout, dout_stride, (const float*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)d, d_stride, each, lanes, parts, dbias, f32);
     else
-        slope_sums_kernel<T, T><<<grid, 256, 0, s>>>((const T*)dout, dout_stride, (const T*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)d, d_stride, each, lanes, parts);
+        slope_sums_kernel<T, T><<<grid, 256, 0, s>>>((const T*)dout, dout_stride, (const T*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)d, d_stride, each, lanes, parts, dbias, f32);
+    if (!parts) return;
     const int64_t blocks = (int64_t)experts * ((cols - 1) / 64 + 1);
     slope_join_kernel<T><<<(unsigned)std::min(blocks, kMostLoopGroups), 256, 0, s>>>(parts, rows, cols, offsets, experts, each, dbias, f32);
 }
