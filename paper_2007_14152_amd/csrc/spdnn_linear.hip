@@ -101,12 +101,12 @@ int grad_work(int32_t rows, int32_t width, int32_t cols, bool grouped, int32_t e
         CHECK(check_tiles(p, experts));
         parts = std::max(parts, p.parts + (p.splits > 1 ? aligned((size_t)p.splits * experts * cols * sizeof(float)) : 0));
     }
-    // Chunks of rows: up to four workgroups a CU and 512 chunks, whose parts are added up; a row to eight for each team as long as CUs are idle, but
+    // Chunks of rows: up to four workgroups a CU and 512 chunks, whose parts are added up; a row to four for each team as long as CUs are idle, but
     // no more than an expert's on average, as a chunk takes experts one after the other.  Up to eight rows a team are one chunk, without parts.
     w->slope_lanes = 64;
     while (w->slope_lanes > 1 && w->slope_lanes / 2 * 8 >= cols) w->slope_lanes /= 2;
     const int64_t teams = 256 / w->slope_lanes, blocks = ceil_div(cols, w->slope_lanes * 8);
-    int64_t least = std::max(teams, std::min(8 * teams, ceil_div(rows * blocks, 256)));
+    int64_t least = std::max(teams, std::min(4 * teams, ceil_div(rows * blocks, 256)));
     if (grouped) least = std::min(least, std::max<int64_t>(1, ceil_div(rows, experts)));
     else if (rows <= 8 * teams) least = 8 * teams;
     w->slope_rows = std::max({least, ceil_div(rows * blocks, 1024), ceil_div(rows, 512)});

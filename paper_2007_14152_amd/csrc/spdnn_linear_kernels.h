@@ -1209,23 +1209,25 @@ __global__ __launch_bounds__(256) void slope_sums_kernel(const D* dout, int64_t 
         first = last;
     }
 }
-// The parts added up: a workgroup has 64 columns of an expert, its four waves every fourth part, added in order.
+// The parts added up: a workgroup has 64 columns of an expert, its 16 waves every 16th part, added in order.
 template <typename T>
-__global__ __launch_bounds__(256) void slope_join_kernel(const float* parts, int32_t rows, int32_t cols, const int32_t* offsets, int32_t experts,
-                                                         int32_t each, void* dbias, bool f32) {
-    __shared__ float sums[4][64];
+__global__ __launch_bounds__(1024) void slope_join_kernel(const float* parts, int32_t rows, int32_t cols, const int32_t* offsets, int32_t experts,
+                                                          int32_t each, void* dbias, bool f32) {
+    constexpr int WAVES = 16;
+    __shared__ float sums[WAVES][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int blocks = (cols - 1) / 64 + 1;
-    for (int64_t b = blockIdx.x; b < (int64_t)experts * blocks; b += gridDim.x) {
-        const int set = (int)(b / blocks), col = (int)(b - (int64_t)set * blocks) * 64 + lane;
-        const RowRange r = grad_rows<1>(offsets, rows, set, 0, 1);
-        const int chunk = (int)(r.first / each) + wave, chunks = r.last > r.first ? (int)((r.last - 1) / each) + 1 : 0;
+    const int set = blockIdx.y;
+    for (int block = blockIdx.x; block <= (cols - 1) / 64; block += gridDim.x) {
+        const int col = block * 64 + lane;
+        const int first = offsets ? min(max(offsets[set], 0), rows) : 0, last = offsets ? min(max(offsets[set + 1], first), rows) : rows;
+        const int chunk = first / each + wave, chunks = last > first ? (last - 1) / each + 1 : 0;
         float sum = 0;
-        if (col < cols && chunk < chunks) sum = sum_parts(parts + ((int64_t)chunk + set) * cols + col, 4 * (int64_t)cols, (chunks - chunk + 3) / 4);
+        if (col < cols && chunk < chunks) sum = sum_parts(parts + ((int64_t)chunk + set) * cols + col, WAVES * (int64_t)cols, (chunks - chunk + WAVES - 1) / WAVES);
         sums[wave][lane] = sum;
         __syncthreads();
         if (wave == 0 && col < cols) {
-            for (int w = 1; w < 4; ++w) sum += sums[w][lane];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) sum += sums[w][lane];
             const int64_t at = (int64_t)set * cols + col;
             if (f32) ((float*)dbias)[at] = sum;
             else ((T*)dbias)[at] = rounded<T>(sum);

@@ -53,8 +53,7 @@ void launch_slope_sums(bool dout_f32, const void* dout, int64_t dout_stride, con
     else
         slope_sums_kernel<T, T><<<grid, 256, 0, s>>>((const T*)dout, dout_stride, (const T*)pre, pre_stride, act, rows, cols, offsets, experts, (T*)d, d_stride, each, lanes, parts, dbias, f32);
     if (!parts) return;
-    const int64_t blocks = (int64_t)experts * ((cols - 1) / 64 + 1);
-    slope_join_kernel<T><<<(unsigned)std::min(blocks, kMostLoopGroups), 256, 0, s>>>(parts, rows, cols, offsets, experts, each, dbias, f32);
+    slope_join_kernel<T><<<dim3((unsigned)std::min((cols - 1) / 64 + 1, 1 << 16), (unsigned)experts), 1024, 0, s>>>(parts, rows, cols, offsets, experts, each, dbias, f32);
 }
 
 template <typename T>
