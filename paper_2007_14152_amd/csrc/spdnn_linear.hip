@@ -70,6 +70,7 @@ bool dma_side(const Side& s, Adjacent adj, int32_t along, int32_t type) {
 }
 
 Plan plan_of(int32_t type, Adjacent adj, Product& p) {
+    if (p.rows == 1) p.x.line = (int64_t)p.width * size_of(type);  // whatever the stride of one row is
     const bool dma = dma_side(p.x, Adjacent::K, p.width, type) && dma_side(p.w, adj, adj == Adjacent::K ? p.width : p.cols, type);
     const Plan c = plan_product(p.rows, p.width, p.cols, p.offsets != nullptr, p.experts, type, dma, adj);
     p.mtiles = (int32_t)c.mtiles;

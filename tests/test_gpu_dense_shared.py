@@ -26,7 +26,7 @@ def whole(g, shape, dtype):
 
 @pytest.mark.parametrize("transposed", [False, True])
 @pytest.mark.parametrize("dtype", ref.TYPES)
-@pytest.mark.parametrize("rows,width,cols", [(2, 1, 9), (70, 33, 20), (70, 64, 20), (5, 777, 300), (300, 777, 129), (257, 65, 300), (3000, 71, 2903), (20, 8201, 64)])
+@pytest.mark.parametrize("rows,width,cols", [(1, 33, 20), (1, 4097, 300), (2, 1, 9), (70, 33, 20), (70, 64, 20), (5, 777, 300), (300, 777, 129), (257, 65, 300), (3000, 71, 2903), (20, 8201, 64)])
 def test_rows_that_are_one(sp, rows, width, cols, dtype, transposed):
     """x, and then dout, with the same row for all."""
     g = torch.Generator().manual_seed(rows + width)
